@@ -288,6 +288,85 @@ CKV_API ckv_status ckv_project(int32_t device, int32_t n, int32_t n_groups, int3
                                const void* x, const void* W, const float* bias, void* out, void* stream);
 
 /*
+ * Fitting the router and the pool (Sec. 4.3, training branch).  The router's arg-max has no gradient; the paper trains the
+ * picked row through a gate sigmoid(M[i][I_i]), and the router by a peak loss and a load-balance loss.  The calls of a
+ * training step, per side (keys, values):
+ *     ckv_route -> ckv_route_loss -> ckv_gather -> (the model) -> ckv_sort_indices -> ckv_gather_grad -> ckv_route_loss_grad
+ * and the pool goes back into service with ckv_pool_load.  They need no context, allocate nothing, are stream-ordered and can
+ * be captured into a graph.  `idx` is what ckv_route writes, int32 [n][n_groups]; an index outside [0, n_entries) marks a
+ * position without an entry (padding): it takes no part in the losses and gradients of its group, whatever its inputs hold.
+ * Results are the same bits from call to call.  Array arguments are device memory of `device` (or managed), aligned to
+ * their elements, W to 16 bytes.  `workspace` is device memory on a 256-byte boundary of at least the size that the _bytes
+ * function of the call gives, of any contents; calls that may overlap on the GPU, captured graphs among them, need one each.
+ * Errors of all of them: INVALID_ARG (sizes, null, host or misaligned pointers, workspace too small), UNSUPPORTED (d_in,
+ * head_dim, more than 65535 groups), SHAPE (d_shared outside [1, head_dim]), CUDA.
+ */
+
+/*
+ * Positions in the order of the entries they picked, for the gradients.
+ *   order   int32 [n_groups][n]              positions by (entry, position), those without an entry last
+ *   offset  int32 [n_groups][n_entries + 1]  entry j's positions are order[g][offset[j] .. offset[j + 1]): their number is
+ *                                            the entry's count, offset[n_entries] that of the positions that have one
+ */
+CKV_API ckv_status ckv_sort_indices_bytes(int32_t n, int32_t n_groups, int32_t n_entries, int64_t* bytes);
+CKV_API ckv_status ckv_sort_indices(int32_t device, int32_t n, int32_t n_groups, int32_t n_entries, const int32_t* idx,
+                                    int32_t* order, int32_t* offset, void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * The router's losses, with M[i][j] = x_i . W[g][j] + bias[g][j] (never written) and u = 1 / n_entries, over the `rows`
+ * positions of the group that have an entry:
+ *   lse   fp32 [n][n_groups]          log sum_j exp M[i][j]     (log probability of the picked entry: score - lse)
+ *   score fp32 [n][n_groups]          M[i][idx[i]]              (0 in both for a position without an entry)
+ *   mean  fp32 [n_groups][n_entries]  p_j = 1 / rows * sum_i softmax(M[i])_j
+ *   loss  fp32 [n_groups][2]          load balance sum_j p_j log(p_j / u), peak -1 / rows * sum_i log sigmoid(score_i)
+ * x bf16 [n][d_in], W bf16 [n_groups][n_entries][d_in], bias fp32 [n_groups][n_entries] or NULL, d_in in {32, 64, 128}.
+ * Products are exact, sums fp32 (the losses' fp64).  A group without rows has zeros.  A bias of -inf takes an entry out;
+ * a position whose scores are all -inf adds to no p_j.
+ */
+CKV_API ckv_status ckv_route_loss_bytes(int32_t n, int32_t n_groups, int32_t d_in, int32_t n_entries, int64_t* forward,
+                                        int64_t* grad);
+CKV_API ckv_status ckv_route_loss(int32_t device, int32_t n, int32_t n_groups, int32_t d_in, int32_t n_entries, const void* x,
+                                  const void* W, const float* bias, const int32_t* idx, float* loss, float* lse, float* score,
+                                  float* mean, void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * Gradient of  sum_g (balance_weight * balance_g + peak_weight * peak_g)  and of whatever else depends on the scores of the
+ * picked entries, by the router's inputs and parameters:
+ *   lse, score, mean  of ckv_route_loss;  order, offset  of ckv_sort_indices for the same idx
+ *   d_score fp32 [n][n_groups] or NULL: gradient by `score` from elsewhere (ckv_gather_grad's); ignored where there is no entry
+ *   dx      bf16 [n][d_in], all groups' sum;  dW bf16 [n_groups][n_entries][d_in];  dbias fp32 [n_groups][n_entries] or NULL
+ * Sums are fp32; the weights that multiply the rows of W and x are rounded to bf16, as dx and dW are.
+ */
+CKV_API ckv_status ckv_route_loss_grad(int32_t device, int32_t n, int32_t n_groups, int32_t d_in, int32_t n_entries,
+                                       const void* x, const void* W, const float* bias, const int32_t* idx, const int32_t* order,
+                                       const int32_t* offset, const float* lse, const float* score, const float* mean,
+                                       float balance_weight, float peak_weight, const float* d_score, void* dx, void* dW,
+                                       float* dbias, void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * Rows of one side's K or V as the training branch has them (Eq. Kc and K):
+ *   out[i][g] = concat(user[i][g], sigmoid(score[i][g]) * pool[g][idx[i][g]])      score NULL: without the gate (inference)
+ * pool [n_groups][n_entries][d_shared] as for ckv_pool_load, user [n][n_groups][head_dim - d_shared] (NULL iff that is 0), out
+ * [n][n_groups][head_dim], all of `dtype`; a position without an entry gets zeros behind its user part.  The product is
+ * rounded once.
+ */
+CKV_API ckv_status ckv_gather(int32_t device, int32_t dtype, int32_t n, int32_t n_groups, int32_t head_dim, int32_t d_shared,
+                              int32_t n_entries, const void* pool, const int32_t* idx, const void* user, const float* score,
+                              void* out, void* stream);
+
+/*
+ * Gradients of ckv_gather, d_out [n][n_groups][head_dim] of `dtype`, order and offset of ckv_sort_indices:
+ *   d_pool  fp32 [n_groups][n_entries][d_shared]   fp32 sums in the order of the positions (zeros for an entry without one)
+ *   d_user  `dtype` [n][n_groups][head_dim - d_shared], or NULL
+ *   d_score fp32 [n][n_groups], NULL iff score is (pool is read for it alone and may be NULL then)
+ */
+CKV_API ckv_status ckv_gather_grad_bytes(int32_t n, int32_t n_groups, int32_t head_dim, int64_t* bytes);
+CKV_API ckv_status ckv_gather_grad(int32_t device, int32_t dtype, int32_t n, int32_t n_groups, int32_t head_dim, int32_t d_shared,
+                                   int32_t n_entries, const void* pool, const int32_t* order, const int32_t* offset,
+                                   const float* score, const void* d_out, float* d_pool, void* d_user, float* d_score,
+                                   void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
  * Appends L_new positions (new interactions) behind a cached user's history; arguments as for
  * ckv_cache_put, describing only the new positions.  Histories are stored in multiples of 32
  * positions: new positions that fit behind the old ones are written there, otherwise the user's

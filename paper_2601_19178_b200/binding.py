@@ -27,6 +27,8 @@ EXPORTS = (
     "ckv_user_length", "ckv_cache_append", "ckv_cache_blob_bytes", "ckv_cache_export", "ckv_cache_import",
     "ckv_cache_bytes", "ckv_set_option", "ckv_get_option", "ckv_last_stat", "ckv_strerror",
     "ckv_last_cuda_error", "ckv_version", "ckv_route", "ckv_project", "ckv_pool_load_sides", "ckv_attend_visible",
+    "ckv_sort_indices_bytes", "ckv_sort_indices", "ckv_route_loss_bytes", "ckv_route_loss", "ckv_route_loss_grad",
+    "ckv_gather", "ckv_gather_grad_bytes", "ckv_gather_grad",
 )
 
 
@@ -78,6 +80,14 @@ def _load() -> ctypes.CDLL:
         "ckv_version": (i32, []),
         "ckv_route": (i32, [i32, i32, i32, i32, i32, vp, vp, vp, vp, i32, vp]),
         "ckv_project": (i32, [i32, i32, i32, i32, i32, vp, vp, vp, vp, vp]),
+        "ckv_sort_indices_bytes": (i32, [i32, i32, i32, p64]),
+        "ckv_sort_indices": (i32, [i32, i32, i32, i32, vp, vp, vp, vp, i64, vp]),
+        "ckv_route_loss_bytes": (i32, [i32, i32, i32, i32, p64, p64]),
+        "ckv_route_loss": (i32, [i32] * 5 + [vp] * 9 + [i64, vp]),
+        "ckv_route_loss_grad": (i32, [i32] * 5 + [vp] * 9 + [ctypes.c_float] * 2 + [vp] * 5 + [i64, vp]),
+        "ckv_gather": (i32, [i32] * 7 + [vp] * 6),
+        "ckv_gather_grad_bytes": (i32, [i32, i32, i32, p64]),
+        "ckv_gather_grad": (i32, [i32] * 7 + [vp] * 9 + [i64, vp]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
@@ -344,3 +354,62 @@ def ckv_project(device: int, n: int, n_groups: int, d_in: int, d_out: int, x, W,
         return _check(None, st, "ckv_project")
     _check(None, lib.ckv_project(device, n, n_groups, d_in, d_out, _ptr(x), _ptr(W), _ptr(bias), _ptr(out),
                                  _stream(stream)), "ckv_project")
+
+
+def ckv_sort_indices_bytes(n: int, n_groups: int, n_entries: int) -> int:
+    v = ctypes.c_int64()
+    _check(None, lib.ckv_sort_indices_bytes(n, n_groups, n_entries, ctypes.byref(v)), "ckv_sort_indices_bytes")
+    return v.value
+
+
+def ckv_sort_indices(device: int, n: int, n_groups: int, n_entries: int, idx, order, offset, workspace, workspace_bytes: int,
+                     stream=None) -> None:
+    """Positions by the entry they picked: idx [n][G] -> order [G][n], offset [G][n_entries + 1] (int32, device)."""
+    _check(None, lib.ckv_sort_indices(device, n, n_groups, n_entries, _ptr(idx), _ptr(order), _ptr(offset), _ptr(workspace),
+                                      int(workspace_bytes), _stream(stream)), "ckv_sort_indices")
+
+
+def ckv_route_loss_bytes(n: int, n_groups: int, d_in: int, n_entries: int):
+    """Workspace of ckv_route_loss and of ckv_route_loss_grad."""
+    a, b = ctypes.c_int64(), ctypes.c_int64()
+    _check(None, lib.ckv_route_loss_bytes(n, n_groups, d_in, n_entries, ctypes.byref(a), ctypes.byref(b)), "ckv_route_loss_bytes")
+    return a.value, b.value
+
+
+def ckv_route_loss(device: int, n: int, n_groups: int, d_in: int, n_entries: int, x, W, bias, idx, loss, lse, score, mean,
+                   workspace, workspace_bytes: int, stream=None) -> None:
+    """Router losses [G][2] (balance, peak), with lse and score [n][G] and mean [G][n_entries] for the gradient."""
+    _check(None, lib.ckv_route_loss(device, n, n_groups, d_in, n_entries, _ptr(x), _ptr(W), _ptr(bias), _ptr(idx), _ptr(loss),
+                                    _ptr(lse), _ptr(score), _ptr(mean), _ptr(workspace), int(workspace_bytes), _stream(stream)),
+           "ckv_route_loss")
+
+
+def ckv_route_loss_grad(device: int, n: int, n_groups: int, d_in: int, n_entries: int, x, W, bias, idx, order, offset, lse,
+                        score, mean, balance_weight: float, peak_weight: float, d_score, dx, dW, dbias, workspace,
+                        workspace_bytes: int, stream=None) -> None:
+    """Gradient of the router losses, and of what else depends on the picked scores (d_score), by x, W and bias."""
+    _check(None, lib.ckv_route_loss_grad(device, n, n_groups, d_in, n_entries, _ptr(x), _ptr(W), _ptr(bias), _ptr(idx),
+                                         _ptr(order), _ptr(offset), _ptr(lse), _ptr(score), _ptr(mean), balance_weight,
+                                         peak_weight, _ptr(d_score), _ptr(dx), _ptr(dW), _ptr(dbias), _ptr(workspace),
+                                         int(workspace_bytes), _stream(stream)), "ckv_route_loss_grad")
+
+
+def ckv_gather(device: int, dtype: int, n: int, n_groups: int, head_dim: int, d_shared: int, n_entries: int, pool, idx, user,
+               score, out, stream=None) -> None:
+    """out [n][G][head_dim] = (user part | sigmoid(score) * picked pool row); score None: without the gate."""
+    _check(None, lib.ckv_gather(device, dtype, n, n_groups, head_dim, d_shared, n_entries, _ptr(pool), _ptr(idx), _ptr(user),
+                                _ptr(score), _ptr(out), _stream(stream)), "ckv_gather")
+
+
+def ckv_gather_grad_bytes(n: int, n_groups: int, head_dim: int) -> int:
+    v = ctypes.c_int64()
+    _check(None, lib.ckv_gather_grad_bytes(n, n_groups, head_dim, ctypes.byref(v)), "ckv_gather_grad_bytes")
+    return v.value
+
+
+def ckv_gather_grad(device: int, dtype: int, n: int, n_groups: int, head_dim: int, d_shared: int, n_entries: int, pool, order,
+                    offset, score, d_out, d_pool, d_user, d_score, workspace, workspace_bytes: int, stream=None) -> None:
+    """Gradients of ckv_gather by the pool (fp32), the user parts and the scores."""
+    _check(None, lib.ckv_gather_grad(device, dtype, n, n_groups, head_dim, d_shared, n_entries, _ptr(pool), _ptr(order),
+                                     _ptr(offset), _ptr(score), _ptr(d_out), _ptr(d_pool), _ptr(d_user), _ptr(d_score),
+                                     _ptr(workspace), int(workspace_bytes), _stream(stream)), "ckv_gather_grad")

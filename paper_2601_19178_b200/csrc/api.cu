@@ -13,6 +13,7 @@
 #include <vector>
 
 #include "ckv_internal.h"
+#include "host_util.h"
 
 using namespace ckv;
 
@@ -231,21 +232,6 @@ HostFlag::Pool HostFlag::pool_;
 
 constexpr int kMaxPlans = 4;
 
-struct DeviceGuard {
-    int prev = -1;
-    bool ok;
-    explicit DeviceGuard(int dev)
-    {
-        ok = cudaGetDevice(&prev) == cudaSuccess;
-        if (ok && prev != dev) ok = cudaSetDevice(dev) == cudaSuccess;
-    }
-    ~DeviceGuard()
-    {
-        int cur = -1;
-        if (prev >= 0 && cudaGetDevice(&cur) == cudaSuccess && cur != prev) cudaSetDevice(prev);
-    }
-};
-
 }  // namespace
 
 struct ckv_ctx {
@@ -316,19 +302,6 @@ struct ckv_ctx {
     } while (0)
 
 namespace {
-
-// Whose memory `p` points to: a device's (its ordinal), managed, or neither.
-enum { kManagedMemory = -1, kNoDeviceMemory = -2 };
-int memory_of(const void* p)
-{
-    cudaPointerAttributes at;
-    if (cudaPointerGetAttributes(&at, p) != cudaSuccess) {
-        cudaGetLastError();
-        return kNoDeviceMemory;
-    }
-    return at.type == cudaMemoryTypeDevice ? at.device : at.type == cudaMemoryTypeManaged ? kManagedMemory : kNoDeviceMemory;
-}
-bool is_device_ptr(const void* p) { return memory_of(p) != kNoDeviceMemory; }
 
 cudaError_t grow(DevBuf& b, size_t bytes, int64_t* allocs = nullptr)
 {

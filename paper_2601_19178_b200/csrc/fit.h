@@ -1,0 +1,74 @@
+// Internal declarations of the training side: sorted indices, router losses, gated pool lookup, and their gradients.
+#pragma once
+
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "ckv_internal.h"
+
+namespace ckv {
+
+// Pieces of a caller's workspace, each on a 256-byte boundary.  A null base only adds up the size.
+struct Carve {
+    char* base;
+    int64_t used = 0;
+    explicit Carve(void* p) : base((char*)p) {}
+    template <typename T>
+    T* take(int64_t n)
+    {
+        T* p = base ? reinterpret_cast<T*>(base + used) : nullptr;
+        used += (n * (int64_t)sizeof(T) + 255) / 256 * 256;
+        return p;
+    }
+};
+
+// ---- kernels_sort.cu
+int64_t sort_workspace(int64_t n, int G, int64_t m);
+cudaError_t launch_sort_indices(int64_t n, int G, int64_t m, const int32_t* idx, int32_t* order, int32_t* offset, void* ws,
+                                cudaStream_t s);
+
+// ---- kernels_gather.cu
+// out[i][g] = (user[i][g] | gate * pool[g][idx[i][g]]), gate = sigmoid(score[i][g]) or 1, rows of D elements, D - ds of them the user's
+cudaError_t launch_gather(int dtype, int64_t n, int G, int D, int ds, int64_t m, const void* pool, const int32_t* idx,
+                          const void* user, const float* score, void* out, cudaStream_t s);
+
+// Sums of rows over the runs of equal entries in a sorted order, and what falls off on the way.
+struct SegmentArgs {
+    const int32_t* order;    // [G][n]
+    const int32_t* offset;   // [G][m + 1]
+    const void* rows;        // row of position i and group g at rows + i * stride + g * group_stride (elements)
+    int64_t stride, group_stride;
+    int64_t n, m;
+    int G, width, skip;      // elements of a row, of which the first `skip` are not summed
+    const float* score;      // [n][G] or null.  Weight of a row: sigmoid(score) if pool is given, else score itself; null: 1
+    const void* pool;        // [G][m][width - skip]: d_score wanted; else null
+    void* d_user;            // [n][G][skip] or null
+    float* d_score;          // [n][G] or null
+    float* sum;              // [G][m][width - skip]
+    float* weight_sum;       // [G][m] or null: the sum of the weights
+};
+int64_t segment_workspace(int64_t n, int G, int width);
+cudaError_t launch_segment_sum(int dtype, const SegmentArgs& a, void* ws, cudaStream_t s);
+
+// ---- kernels_route_loss.cu
+struct RouteLossArgs {
+    int64_t n, m;
+    int G, d;
+    const void *x, *W;
+    const float* bias;
+    const int32_t* idx;
+    float *loss, *lse, *score, *mean;  // outputs of the forward pass, inputs of the gradient
+};
+int64_t route_loss_workspace(int64_t n, int G, int d, int64_t m);
+cudaError_t launch_route_loss(const RouteLossArgs& a, void* ws, cudaStream_t s);
+struct RouteGradArgs {
+    const int32_t *order, *offset;
+    float w_balance, w_peak;
+    const float* d_score;  // or null
+    void *dx, *dW;
+    float* dbias;          // or null
+};
+int64_t route_grad_workspace(int64_t n, int G, int d, int64_t m);
+cudaError_t launch_route_grad(const RouteLossArgs& a, const RouteGradArgs& b, void* ws, cudaStream_t s);
+
+}  // namespace ckv
