@@ -50,6 +50,23 @@ struct SegmentArgs {
 int64_t segment_workspace(int64_t n, int G, int width);
 cudaError_t launch_segment_sum(int dtype, const SegmentArgs& a, void* ws, cudaStream_t s);
 
+// ---- kernels_route_sweep.cu: passes over the score matrix
+enum SweepMode { SWEEP_LSE, SWEEP_MEAN, SWEEP_R, SWEEP_DX, SWEEP_DW };
+constexpr int kSweepPad = 384;      // rows of the arrays by position and by entry are rounded up to this
+constexpr int kSweepMaxSplits = 64;
+inline int64_t sweep_padded(int64_t n) { return (n + kSweepPad - 1) / kSweepPad * kSweepPad; }
+struct SweepArgs {
+    int64_t n, m, np, mp;           // positions, entries; both padded
+    int G, splits;
+    const uint16_t *x, *W;          // [n][d], [G][m][d]
+    const float *b2, *h;            // [G][mp] bias log2(e) (-inf behind the last entry); h
+    const float *nl2, *r;           // [G][np] -lse log2(e) (-inf: no weight); r
+    float* part;    // LSE: float2 (maximum, sum) [splits][G][np]; MEAN [splits][G][mp]; R [splits][G][np]; DX [splits][n][d]; DW [splits][G][m][d]
+    float* part2;   // DW: sums of T [splits][G][mp]
+};
+int sweep_splits(int64_t n, int G, int d, int64_t m, int mode);
+cudaError_t launch_sweep(int mode, int d, SweepArgs& a, cudaStream_t s);  // sets a.splits
+
 // ---- kernels_route_loss.cu
 struct RouteLossArgs {
     int64_t n, m;

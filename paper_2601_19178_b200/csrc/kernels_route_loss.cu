@@ -26,8 +26,6 @@ namespace ckv {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr int kPad = 128;  // rows of the arrays by position and by entry are rounded up to this
-inline int64_t padded(int64_t n) { return (n + kPad - 1) / kPad * kPad; }
 
 __device__ __forceinline__ float bf(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
 __device__ __forceinline__ float sigmoid(float x) { return 1.f / (1.f + expf(-x)); }
@@ -49,21 +47,11 @@ struct Space {
 };
 constexpr int kPrepRows = 256;
 
-enum Mode { LSE, MEAN, R, DX, DW };
-int splits_of(int64_t n, int G, int64_t m, int mode)
-{
-    const int64_t stand = mode == MEAN || mode == DW ? m : n, stream = mode == MEAN || mode == DW ? n : m;
-    const int64_t blocks = (stand + 127) / 128 * (mode == DX ? 1 : G), tiles = (stream + 31) / 32 * (mode == DX ? G : 1);
-    int64_t s = 1;
-    while (s < 16 && blocks * s * 2 <= 592 && s * 2 <= tiles) s *= 2;
-    return (int)s;
-}
-
 Space layout(void* ws, int64_t n, int G, int d, int64_t m, bool grad)
 {
     Carve c(ws);
     Space s{};
-    const int64_t np = padded(n), mp = padded(m), blocks = (n + kPrepRows - 1) / kPrepRows;
+    const int64_t np = sweep_padded(n), mp = sweep_padded(m), blocks = (n + kPrepRows - 1) / kPrepRows;
     s.b2 = c.take<float>(G * mp);
     s.nl2 = c.take<float>(G * np);
     s.xs = c.take<uint16_t>(n * d);
@@ -71,15 +59,15 @@ Space layout(void* ws, int64_t n, int G, int d, int64_t m, bool grad)
         s.rows_part = c.take<int32_t>(blocks * G);
         s.peak_part = c.take<double>(blocks * G);
         s.live_part = c.take<int32_t>((np + 255) / 256 * G);
-        s.part = c.take<float>(std::max(2 * splits_of(n, G, m, LSE) * G * np, splits_of(n, G, m, MEAN) * G * mp));
+        s.part = c.take<float>(std::max(2 * sweep_splits(n, G, d, m, SWEEP_LSE) * G * np, sweep_splits(n, G, d, m, SWEEP_MEAN) * G * mp));
     } else {
         s.h = c.take<float>(G * mp);
         s.r = c.take<float>(G * np);
         s.ds = c.take<float>(n * G);
         s.sum = c.take<float>(G * m * d);
         s.wsum = c.take<float>(G * m);
-        s.part = c.take<float>(std::max(std::max(splits_of(n, G, m, R) * G * np, splits_of(n, G, m, DX) * n * d), splits_of(n, G, m, DW) * G * m * d));
-        s.part2 = c.take<float>(splits_of(n, G, m, DW) * G * mp);
+        s.part = c.take<float>(std::max(std::max(sweep_splits(n, G, d, m, SWEEP_R) * G * np, sweep_splits(n, G, d, m, SWEEP_DX) * n * d), sweep_splits(n, G, d, m, SWEEP_DW) * G * m * d));
+        s.part2 = c.take<float>(sweep_splits(n, G, d, m, SWEEP_DW) * G * mp);
         s.seg = c.take<char>(segment_workspace(n, G, d));
     }
     s.bytes = c.used;
@@ -106,7 +94,7 @@ __global__ void __launch_bounds__(256) entries_kernel(const float* __restrict__ 
 // coefficient.
 __global__ void __launch_bounds__(kPrepRows) positions_kernel(const RouteLossArgs a, const RouteGradArgs b, Space s, bool grad)
 {
-    const int64_t i = blockIdx.x * (int64_t)kPrepRows + threadIdx.x, np = (a.n + kPad - 1) / kPad * kPad;
+    const int64_t i = blockIdx.x * (int64_t)kPrepRows + threadIdx.x, np = (a.n + kSweepPad - 1) / kSweepPad * kSweepPad;
     bool any = false;
     for (int g = 0; g < a.G; ++g) {
         const int32_t k = i < a.n ? a.idx[i * a.G + g] : -1;
@@ -164,101 +152,8 @@ __global__ void __launch_bounds__(kPrepRows) positions_kernel(const RouteLossArg
         for (int c = 0; c < a.d; ++c) s.xs[i * a.d + c] = any ? ((const uint16_t*)a.x)[i * a.d + c] : (uint16_t)0;
 }
 
-// ---- the passes
-struct PassArgs {
-    int64_t n, m, np, mp;
-    int G, splits;
-    const uint16_t *x, *W;
-    const float *b2, *h, *nl2, *r;
-    float *part, *part2;
-};
-constexpr int kTile = 32;
-
-template <int D, int MODE>
-__global__ void __launch_bounds__(128) pass_kernel(const PassArgs a)
-{
-    constexpr bool kEntriesStand = MODE == MEAN || MODE == DW, kGrad = MODE == DX || MODE == DW;
-    __shared__ float tile[kTile][D], col0[kTile], col1[kTile];
-    const int64_t n_stand = kEntriesStand ? a.m : a.n, n_stream = kEntriesStand ? a.n : a.m;
-    const int64_t row = blockIdx.x * (int64_t)128 + threadIdx.x, sp = kEntriesStand ? a.mp : a.np;
-    const bool in = row < n_stand;
-    const int64_t per_group = (n_stream + kTile - 1) / kTile, tiles = per_group * (MODE == DX ? a.G : 1);
-    const int64_t t0 = tiles * blockIdx.z / a.splits, t1 = tiles * (blockIdx.z + 1) / a.splits;
-    int g = MODE == DX ? -1 : blockIdx.y;
-    float own[D], acc[kGrad ? D : 1] = {}, row0 = 0.f, row1 = 0.f, top = -CUDART_INF_F, sum = 0.f;
-    const uint16_t* stand = kEntriesStand ? a.W + ((int64_t)g * a.m + row) * D : a.x + row * D;
-    for (int c = 0; c < D; ++c) own[c] = in ? bf(stand[c]) : 0.f;
-    auto row_values = [&] {
-        row0 = !in ? -CUDART_INF_F : MODE == LSE ? 0.f : kEntriesStand ? a.b2[g * a.mp + row] : a.nl2[g * a.np + row];
-        row1 = !in ? 0.f : MODE == DX ? a.r[g * a.np + row] : MODE == DW ? a.h[g * a.mp + row] : 0.f;
-    };
-    if (MODE != DX) row_values();
-    for (int64_t t = t0; t < t1; ++t) {
-        if (MODE == DX && (int)(t / per_group) != g) {
-            g = (int)(t / per_group);
-            row_values();
-        }
-        const int64_t c0 = (t % per_group) * kTile;
-        const uint16_t* stream = kEntriesStand ? a.x : a.W + (int64_t)g * a.m * D;
-        __syncthreads();
-        for (int e = threadIdx.x; e < kTile * D; e += 128) tile[e / D][e % D] = c0 + e / D < n_stream ? bf(stream[c0 * D + e]) : 0.f;
-        if (threadIdx.x < kTile) {
-            const int64_t c = c0 + threadIdx.x;
-            col0[threadIdx.x] = c >= n_stream ? -CUDART_INF_F : kEntriesStand ? a.nl2[g * a.np + c] : a.b2[g * a.mp + c];
-            if (MODE == R || MODE == DX) col1[threadIdx.x] = c < n_stream ? a.h[g * a.mp + c] : 0.f;
-            if (MODE == DW) col1[threadIdx.x] = c < n_stream ? a.r[g * a.np + c] : 0.f;
-        }
-        __syncthreads();
-        for (int c = 0; c < kTile; ++c) {
-            float s = 0.f;
-#pragma unroll
-            for (int k = 0; k < D; k += 4) {
-                const float4 w = *reinterpret_cast<const float4*>(&tile[c][k]);
-                s = fmaf(own[k], w.x, s);
-                s = fmaf(own[k + 1], w.y, s);
-                s = fmaf(own[k + 2], w.z, s);
-                s = fmaf(own[k + 3], w.w, s);
-            }
-            const float u = fmaf(s, kLog2e, col0[c] + row0);
-            if (MODE == LSE) {
-                if (u > top) {
-                    sum *= exp2f(top - u);
-                    top = u;
-                }
-                if (top > -CUDART_INF_F) sum += exp2f(u - top);
-                continue;
-            }
-            const float p = exp2f(u);
-            if (MODE == MEAN) sum += p;
-            if (MODE == R) sum = fmaf(p, col1[c], sum);
-            if (kGrad) {
-                const float v = MODE == DX ? p * (col1[c] - row1) : p * (row1 - col1[c]);
-                sum += v;
-#pragma unroll
-                for (int k = 0; k < D; k += 4) {
-                    const float4 w = *reinterpret_cast<const float4*>(&tile[c][k]);
-                    acc[k] = fmaf(v, w.x, acc[k]);
-                    acc[k + 1] = fmaf(v, w.y, acc[k + 1]);
-                    acc[k + 2] = fmaf(v, w.z, acc[k + 2]);
-                    acc[k + 3] = fmaf(v, w.w, acc[k + 3]);
-                }
-            }
-        }
-    }
-    if (!in) return;
-    if (MODE == DX) {
-        for (int k = 0; k < D; ++k) a.part[((int64_t)blockIdx.z * a.n + row) * D + k] = acc[k];
-        return;
-    }
-    const int64_t at = ((int64_t)blockIdx.z * a.G + g) * sp + row;
-    if (MODE == LSE) reinterpret_cast<float2*>(a.part)[at] = make_float2(top, sum);
-    else (MODE == DW ? a.part2 : a.part)[at] = sum;
-    if (MODE == DW)
-        for (int k = 0; k < D; ++k) a.part[(((int64_t)blockIdx.z * a.G + g) * a.m + row) * D + k] = acc[k];
-}
-
 // ---- joins
-__global__ void __launch_bounds__(256) lse_join_kernel(const RouteLossArgs a, const PassArgs p, float* __restrict__ nl2,
+__global__ void __launch_bounds__(256) lse_join_kernel(const RouteLossArgs a, const SweepArgs p, float* __restrict__ nl2,
                                                        int32_t* __restrict__ live_part)
 {
     const int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x;
@@ -302,7 +197,7 @@ __device__ double block_sum(double v)
 // One block per group: the mean weights, and both losses.  mean log(mean m) is summed as (u log u - u + 1) / m with u = mean m:
 // the weights sum to one, so that nothing is added, and near balance, where u log u and the sum's other terms cancel, each
 // term is as small as what it stands for.  (They sum to less by the share of the positions that have no weight.)
-__global__ void __launch_bounds__(1024) mean_join_kernel(const RouteLossArgs a, const PassArgs p, const Space s, int blocks, int live_blocks)
+__global__ void __launch_bounds__(1024) mean_join_kernel(const RouteLossArgs a, const SweepArgs p, const Space s, int blocks, int live_blocks)
 {
     const int g = blockIdx.x;
     double peak = 0, rows_d = 0, live = 0;
@@ -331,7 +226,7 @@ __global__ void __launch_bounds__(1024) mean_join_kernel(const RouteLossArgs a, 
     }
 }
 
-__global__ void __launch_bounds__(256) r_join_kernel(const PassArgs p, float* __restrict__ r)
+__global__ void __launch_bounds__(256) r_join_kernel(const SweepArgs p, float* __restrict__ r)
 {
     const int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x;
     const int g = blockIdx.y;
@@ -343,7 +238,7 @@ __global__ void __launch_bounds__(256) r_join_kernel(const PassArgs p, float* __
 }
 
 // dx: the partial sums and the picked entries' rows
-__global__ void __launch_bounds__(256) dx_join_kernel(const RouteLossArgs a, const RouteGradArgs b, const PassArgs p, const float* __restrict__ ds)
+__global__ void __launch_bounds__(256) dx_join_kernel(const RouteLossArgs a, const RouteGradArgs b, const SweepArgs p, const float* __restrict__ ds)
 {
     for (int64_t e = blockIdx.x * (int64_t)256 + threadIdx.x; e < a.n * a.d; e += (int64_t)gridDim.x * 256) {
         const int64_t i = e / a.d;
@@ -358,7 +253,7 @@ __global__ void __launch_bounds__(256) dx_join_kernel(const RouteLossArgs a, con
     }
 }
 
-__global__ void __launch_bounds__(256) dw_join_kernel(const RouteLossArgs a, const RouteGradArgs b, const PassArgs p, const Space s)
+__global__ void __launch_bounds__(256) dw_join_kernel(const RouteLossArgs a, const RouteGradArgs b, const SweepArgs p, const Space s)
 {
     const int64_t total = a.G * a.m * a.d;
     for (int64_t e = blockIdx.x * (int64_t)256 + threadIdx.x; e < total; e += (int64_t)gridDim.x * 256) {
@@ -374,20 +269,9 @@ __global__ void __launch_bounds__(256) dw_join_kernel(const RouteLossArgs a, con
     }
 }
 
-template <int MODE>
-cudaError_t launch_pass(int d, PassArgs& p, cudaStream_t s)
+SweepArgs pass_args(const RouteLossArgs& a, const Space& s)
 {
-    p.splits = splits_of(p.n, p.G, p.m, MODE);
-    const int64_t stand = MODE == MEAN || MODE == DW ? p.m : p.n;
-    const dim3 grid((unsigned)((stand + 127) / 128), MODE == DX ? 1u : (unsigned)p.G, (unsigned)p.splits);
-    if (grid.x == 0) return cudaSuccess;
-    return launch_kernel(Launch{s, nullptr, nullptr}, d == 32 ? pass_kernel<32, MODE> : d == 64 ? pass_kernel<64, MODE> : pass_kernel<128, MODE>,
-                         grid, 128, 0, 1, p);
-}
-
-PassArgs pass_args(const RouteLossArgs& a, const Space& s)
-{
-    return PassArgs{a.n, a.m, padded(a.n), padded(a.m), a.G, 1, s.xs, (const uint16_t*)a.W, s.b2, s.h, s.nl2, s.r, s.part, s.part2};
+    return SweepArgs{a.n, a.m, sweep_padded(a.n), sweep_padded(a.m), a.G, 1, s.xs, (const uint16_t*)a.W, s.b2, s.h, s.nl2, s.r, s.part, s.part2};
 }
 
 }  // namespace
@@ -404,21 +288,21 @@ int64_t route_grad_workspace(int64_t n, int G, int d, int64_t m) { return layout
 cudaError_t launch_route_loss(const RouteLossArgs& a, void* ws, cudaStream_t st)
 {
     const Space s = layout(ws, a.n, a.G, a.d, a.m, false);
-    PassArgs p = pass_args(a, s);
+    SweepArgs p = pass_args(a, s);
     const Launch l{st, nullptr, nullptr};
     const unsigned blocks = (unsigned)((a.n + kPrepRows - 1) / kPrepRows), G = (unsigned)a.G;
     TRY(launch_kernel(l, entries_kernel, dim3((unsigned)((p.mp + 255) / 256), G), 256, 0, 1, a.bias, nullptr, nullptr, 0.f, a.m, p.mp, s.b2, nullptr));
     if (a.n) TRY(launch_kernel(l, positions_kernel, dim3(blocks), kPrepRows, 0, 1, a, RouteGradArgs{}, s, false));
-    TRY(launch_pass<LSE>(a.d, p, st));
+    TRY(launch_sweep(SWEEP_LSE, a.d, p, st));
     if (a.n) TRY(launch_kernel(l, lse_join_kernel, dim3((unsigned)((p.np + 255) / 256), G), 256, 0, 1, a, p, s.nl2, s.live_part));
-    TRY(launch_pass<MEAN>(a.d, p, st));
+    TRY(launch_sweep(SWEEP_MEAN, a.d, p, st));
     return launch_kernel(l, mean_join_kernel, dim3(G), 1024, 0, 1, a, p, s, (int)blocks, (int)((p.np + 255) / 256));
 }
 
 cudaError_t launch_route_grad(const RouteLossArgs& a, const RouteGradArgs& b, void* ws, cudaStream_t st)
 {
     const Space s = layout(ws, a.n, a.G, a.d, a.m, true);
-    PassArgs p = pass_args(a, s);
+    SweepArgs p = pass_args(a, s);
     const Launch l{st, nullptr, nullptr};
     const unsigned G = (unsigned)a.G;
     TRY(launch_kernel(l, entries_kernel, dim3((unsigned)((p.mp + 255) / 256), G), 256, 0, 1, a.bias, a.mean, b.offset, b.w_balance, a.m, p.mp, s.b2, s.h));
@@ -436,11 +320,11 @@ cudaError_t launch_route_grad(const RouteLossArgs& a, const RouteGradArgs& b, vo
     seg.sum = s.sum;
     seg.weight_sum = s.wsum;
     TRY(launch_segment_sum(CKV_BF16, seg, s.seg, st));
-    TRY(launch_pass<R>(a.d, p, st));
+    TRY(launch_sweep(SWEEP_R, a.d, p, st));
     if (a.n) TRY(launch_kernel(l, r_join_kernel, dim3((unsigned)((p.np + 255) / 256), G), 256, 0, 1, p, s.r));
-    TRY(launch_pass<DX>(a.d, p, st));
+    TRY(launch_sweep(SWEEP_DX, a.d, p, st));
     if (a.n) TRY(launch_kernel(l, dx_join_kernel, dim3((unsigned)std::min<int64_t>((a.n * a.d + 255) / 256, 148 * 16)), 256, 0, 1, a, b, p, s.ds));
-    TRY(launch_pass<DW>(a.d, p, st));
+    TRY(launch_sweep(SWEEP_DW, a.d, p, st));
     return launch_kernel(l, dw_join_kernel, dim3((unsigned)std::min<int64_t>((a.G * a.m * a.d + 255) / 256, 148 * 16)), 256, 0, 1, a, b, p, s);
 }
 

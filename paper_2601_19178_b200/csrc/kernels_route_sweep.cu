@@ -1,0 +1,739 @@
+// The passes of the router losses over the score matrix, on the tcgen05 tensor cores (kernels_route_loss.cu has the formulas).
+//
+// One side's rows stand: 128 to a block, a thread each (TMEM lane), their inputs as an A operand in TMEM.  The other side's stream
+// through a ring of shared-memory stages, as B operand (a swizzled TMA box per 64 inputs) with up to two numbers for each
+// row beside it (bulk copies).  A tile of scores appears in TMEM, its thread reads its row of it, and:
+//   sweep_kernel (LSE, MEAN, R)  keeps a running sum.  Three blocks per CTA, two accumulators of 64 columns each (one of 96 at d_in = 128).
+//   grad_kernel (DX, DW)         turns it into weights T (bf16, over the head of the scores they came from), which multiply the
+//                                same tile once more, now as MN-major operand:  O += T tile.  Two blocks per CTA (one at d_in =
+//                                128), each with two score buffers whose turns belong to four warps each.
+// Every wait is bounded: a time-out raises the CTA's abort flag, which ends all others; the CTA waits for its copies and
+// products in flight, frees its TMEM, and its results are NaN.
+#include <cuda_bf16.h>
+#include <math_constants.h>
+
+#include <algorithm>
+
+#include "fit.h"
+#include "ptx_helpers.cuh"
+#include "tensor_map.h"
+
+namespace ckv {
+namespace {
+
+constexpr uint32_t kSpin = 1u << 18, kSuspend = 4000;
+constexpr float kLog2e = 1.4426950408889634f;
+
+__device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count)
+{
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(uint32_t bar)
+{
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ bool bar_test(uint32_t bar, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile(
+        "{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\nselp.u32 %0, 1, 0, p;\n}\n"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity), "r"(kSuspend)
+        : "memory");
+    return ok != 0;
+}
+// By all lanes of a warp: waits for the phase; false when the wait ran out or another one has.
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag)
+{
+    bool ok = bar_test(bar, parity);
+    for (uint32_t i = 0; !ok && i < kSpin; ++i) {
+        ok = bar_test(bar, parity);
+        if ((i & 31u) == 31u && *abort_flag) break;
+    }
+    ok = __all_sync(0xffffffffu, ok);
+    if (!ok) *abort_flag = 1;
+    return ok;
+}
+__device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_commit_to(uint32_t bar)
+{
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t acc)
+{
+    asm volatile(
+        "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d_tmem),
+        "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(acc)
+        : "memory");
+}
+// instruction descriptor, kind::f16: fp32 accumulate, bf16 A and B, A K-major
+__host__ __device__ constexpr uint32_t idesc_bf16(int M, int N, bool b_mn_major)
+{
+    return (1u << 4) | (1u << 7) | (1u << 10) | ((b_mn_major ? 1u : 0u) << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+// A tile of rows of ROWB bytes as a TMA box with a swizzle of that span writes it, groups of eight rows ROWB * 8 bytes apart: as K-major
+// operand (rows are N) and as MN-major operand (rows are K) alike.
+template <int ROWB>
+__device__ __forceinline__ uint64_t tile_desc(uint32_t addr)
+{
+    constexpr uint64_t layout = ROWB == 128 ? 2 : 4;  // 128-byte / 64-byte swizzle
+    return (uint64_t)((addr & 0x3ffffu) >> 4) | (1ull << 16) | ((uint64_t)(ROWB * 8 >> 4) << 32) | (1ull << 46) | (layout << 61);
+}
+__device__ __forceinline__ void ld32(uint32_t taddr, uint32_t (&r)[32])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,"
+        "%29,%30,%31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr)
+        : "memory");
+}
+// Waits for this thread's loads; the registers are operands so that nothing reads them earlier.
+__device__ __forceinline__ void wait_ld32(uint32_t (&r)[32])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                   "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]),
+                   "+r"(r[15]), "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]),
+                   "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]),
+                   "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
+                 :
+                 : "memory");
+}
+// 16 consecutive columns of this thread's lane
+__device__ __forceinline__ void st16(uint32_t taddr, const uint32_t* r)
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(
+            taddr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
+}
+__device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void expect_bytes(uint32_t bar, uint32_t bytes)
+{
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, int col, int row, int group, uint32_t bar)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+        "l"(map), "r"(col), "r"(row), "r"(group), "r"(bar)
+        : "memory");
+}
+__device__ __forceinline__ void load_bytes(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
+                 "r"(bytes), "r"(bar)
+                 : "memory");
+}
+
+// Two fp32 operations in one instruction.
+struct F2 {
+    float x, y;
+};
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c)
+{
+    F2 d;
+    asm("{\n.reg .b64 ra, rb, rc, rd;\nmov.b64 ra, {%2, %3};\nmov.b64 rb, {%4, %5};\nmov.b64 rc, {%6, %7};\n"
+        "fma.rn.f32x2 rd, ra, rb, rc;\nmov.b64 {%0, %1}, rd;\n}\n"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ F2 add2(F2 a, F2 b)
+{
+    F2 d;
+    asm("{\n.reg .b64 ra, rb, rd;\nmov.b64 ra, {%2, %3};\nmov.b64 rb, {%4, %5};\nadd.rn.f32x2 rd, ra, rb;\nmov.b64 {%0, %1}, rd;\n}\n"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ F2 mul2(F2 a, F2 b)
+{
+    F2 d;
+    asm("{\n.reg .b64 ra, rb, rd;\nmov.b64 ra, {%2, %3};\nmov.b64 rb, {%4, %5};\nmul.rn.f32x2 rd, ra, rb;\nmov.b64 {%0, %1}, rd;\n}\n"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ float max3f(float a, float b, float c)
+{
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ F2 pair(const uint32_t (&v)[32], int e) { return {__uint_as_float(v[e]), __uint_as_float(v[e + 1])}; }
+__device__ __forceinline__ F2 both(float v) { return {v, v}; }
+
+// A sum of many parts: what an addition loses is added with the next part.
+struct LongSum {
+    float s = 0.f, lost = 0.f;
+    __device__ __forceinline__ void add(float v)
+    {
+        const float y = v - lost, t = s + y;
+        lost = (t - s) - y;
+        s = t;
+    }
+};
+
+// Where a row's inputs come from, and its A operand: two bf16 per TMEM column, zeros for a row that is none.
+template <int DIN>
+__device__ __forceinline__ void load_inputs(uint32_t taddr, const uint16_t* row, bool in)
+{
+    const uint4* src = reinterpret_cast<const uint4*>(row);
+#pragma unroll
+    for (int h = 0; h < DIN / 32; ++h) {
+        uint32_t v[16];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const uint4 w = in ? __ldg(src + 4 * h + q) : make_uint4(0, 0, 0, 0);
+            v[4 * q] = w.x;
+            v[4 * q + 1] = w.y;
+            v[4 * q + 2] = w.z;
+            v[4 * q + 3] = w.w;
+        }
+        st16(taddr + 16 * h, v);
+    }
+    wait_st();
+}
+
+// ---- LSE, MEAN, R
+constexpr int kBlocks = 3, kRows = 128 * kBlocks;
+constexpr int kReadWarps = 4 * kBlocks, kIssueWarp = kReadWarps, kLoadWarp = kIssueWarp + kBlocks;
+constexpr int kSweepThreads = (kLoadWarp + 1) * 32;
+constexpr int kStages = 6;
+
+template <int DIN>
+struct Sweep {
+    static constexpr int AN = DIN == 128 ? 96 : 64;    // columns of an accumulator
+    static constexpr int ACCS = DIN == 128 ? 1 : 2;    // accumulators of a block
+    static constexpr int TN = ACCS * AN;               // rows of a tile
+    static constexpr int ROWB = DIN >= 64 ? 128 : 64;
+    static constexpr int BOXES = DIN == 128 ? 2 : 1;
+    static constexpr int BOX = TN * ROWB, TILE = BOXES * BOX;
+    static constexpr int OFF_NUM = kStages * TILE, NUM = TN * 4, OFF_BAR = OFF_NUM + kStages * 2 * NUM;
+    enum { FULL = 0, EMPTY = kStages, AFULL = 2 * kStages, AFREE = AFULL + kBlocks * ACCS, DRAIN = AFREE + kBlocks * ACCS, COUNT };
+    static constexpr int OFF_ABORT = OFF_BAR + COUNT * 8, SMEM = OFF_ABORT + 16;
+    static_assert(SMEM <= 226 * 1024 && BOX % 1024 == 0, "shared memory");
+    static constexpr uint32_t COL_A = kBlocks * TN;
+    static_assert(COL_A + kBlocks * (DIN / 2) <= 512, "TMEM columns");
+    static_assert(kSweepPad % TN == 0, "numbers are copied a tile at a time");
+};
+
+template <int DIN, int MODE>
+__global__ void __launch_bounds__(kSweepThreads, 1) sweep_kernel(const __grid_constant__ CUtensorMap map, const SweepArgs a)
+{
+    using L = Sweep<DIN>;
+    constexpr int TN = L::TN, AN = L::AN, ACCS = L::ACCS;
+    constexpr bool kEntriesStand = MODE == SWEEP_MEAN;
+    constexpr uint32_t kTileBytes = L::TILE + (MODE == SWEEP_R ? 2 : 1) * L::NUM;
+    extern __shared__ __align__(1024) unsigned char sm[];
+    __shared__ uint32_t tmem_slot;
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
+    const uint32_t sb = smem_u32(sm);
+    auto bar = [&](int i) { return sb + L::OFF_BAR + 8u * (uint32_t)i; };
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(sm + L::OFF_ABORT);
+    const int grp = blockIdx.y, split = (int)(blockIdx.x % (uint32_t)a.splits);
+    const int64_t n_stand = kEntriesStand ? a.m : a.n, n_stream = kEntriesStand ? a.n : a.m;
+    const int64_t row0 = (int64_t)(blockIdx.x / (uint32_t)a.splits) * kRows;
+    const int n_blocks = (int)min((n_stand - row0 + 127) / 128, (int64_t)kBlocks);
+    const int all_tiles = (int)((n_stream + TN - 1) / TN);
+    const int tile0 = (int)((int64_t)all_tiles * split / a.splits), n_tiles = (int)((int64_t)all_tiles * (split + 1) / a.splits) - tile0;
+
+    const int e = warp >> 2;
+    const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
+    const int64_t row = row0 + 128 * e + (warp & 3) * 32 + lane;
+    const bool in = warp < kReadWarps && row < n_stand;
+    if (tid == 0) {
+        for (int s = 0; s < kStages; ++s) {
+            bar_init(bar(L::FULL + s), 1);
+            bar_init(bar(L::EMPTY + s), 4 * (uint32_t)n_blocks);
+        }
+        for (int i = 0; i < kBlocks * ACCS; ++i) {
+            bar_init(bar(L::AFULL + i), 1);
+            bar_init(bar(L::AFREE + i), 4);
+        }
+        bar_init(bar(L::DRAIN), kBlocks);
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == kIssueWarp) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_before();
+    __syncthreads();
+    tc_after();
+    const uint32_t tmem = tmem_slot;
+    if (warp < 4 * n_blocks)
+        load_inputs<DIN>(tmem + lane_base + L::COL_A + e * (DIN / 2), (kEntriesStand ? a.W + ((int64_t)grp * a.m + row) * DIN : a.x + row * DIN), in);
+    if (warp < kLoadWarp) {  // (the loading warp is on its way)
+        tc_before();
+        asm volatile("bar.sync 1, %0;" ::"n"(kLoadWarp * 32) : "memory");
+        tc_after();
+    }
+
+    LongSum sum;
+    float top = -CUDART_INF_F;
+    if (warp < kReadWarps) {
+        // ------------------------------------------------------------ thread = standing row
+        // log2 of a weight is  s log2(e) + own + number of the column
+        const float own = !in || MODE == SWEEP_LSE ? 0.f : kEntriesStand ? a.b2[grp * a.mp + row] : a.nl2[grp * a.np + row];
+        const uint32_t tacc = tmem + lane_base + (uint32_t)(TN * e);
+        int s = 0;
+        uint32_t par = 0;
+        for (int t = 0; e < n_blocks && t < n_tiles; ++t) {
+            if (!bar_wait(bar(L::FULL + s), par, abort_flag)) break;  // (the numbers; the products wait for the tile themselves)
+            const float* num = reinterpret_cast<const float*>(sm + L::OFF_NUM + s * 2 * L::NUM);
+            bool ok = true;
+#pragma unroll
+            for (int h = 0; h < ACCS; ++h) {
+                const int acc = ACCS * e + h;
+                ok = ok && bar_wait(bar(L::AFULL + acc), t & 1, abort_flag);
+                if (!ok) break;
+                tc_after();
+                uint32_t v[AN / 32][32];
+#pragma unroll
+                for (int c = 0; c < AN / 32; ++c) ld32(tacc + AN * h + 32 * c, v[c]);
+#pragma unroll
+                for (int c = 0; c < AN / 32; ++c) wait_ld32(v[c]);
+                tc_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(bar(L::AFREE + acc));
+#pragma unroll
+                for (int c = 0; c < AN / 32; ++c) {
+                    const float4* n0 = reinterpret_cast<const float4*>(num + AN * h + 32 * c);
+                    const float4* n1 = n0 + TN / 4;
+                    F2 u[16];
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) {
+                        const float4 k = n0[q];
+                        F2 k0{k.x, k.y}, k1{k.z, k.w};
+                        if (MODE != SWEEP_LSE) {
+                            k0 = add2(k0, both(own));
+                            k1 = add2(k1, both(own));
+                        }
+                        u[2 * q] = fma2(pair(v[c], 4 * q), both(kLog2e), k0);
+                        u[2 * q + 1] = fma2(pair(v[c], 4 * q + 2), both(kLog2e), k1);
+                    }
+                    if (MODE == SWEEP_LSE) {
+                        float m0 = u[0].x, m1 = u[0].y;
+#pragma unroll
+                        for (int q = 1; q < 15; q += 2) {
+                            m0 = max3f(m0, u[q].x, u[q].y);
+                            m1 = max3f(m1, u[q + 1].x, u[q + 1].y);
+                        }
+                        m0 = max3f(fmaxf(m0, m1), u[15].x, u[15].y);
+                        if (m0 > top) {
+                            const float f = ex2(top - m0);
+                            sum.s *= f;
+                            sum.lost *= f;
+                            top = m0;
+                        }
+                        const float off = top == -CUDART_INF_F ? 0.f : -top;
+#pragma unroll
+                        for (int q = 0; q < 16; ++q) u[q] = add2(u[q], both(off));
+                    }
+                    F2 part{0.f, 0.f};
+#pragma unroll
+                    for (int q = 0; q < 16; ++q) {
+                        const F2 p{ex2(u[q].x), ex2(u[q].y)};
+                        if (MODE == SWEEP_R) {
+                            const F2 w = reinterpret_cast<const F2*>(n1)[q];
+                            part = fma2(p, w, part);
+                        } else {
+                            part = add2(part, p);
+                        }
+                    }
+                    sum.add(part.x + part.y);
+                }
+            }
+            if (!ok) break;
+            __syncwarp();
+            if (lane == 0) bar_arrive(bar(L::EMPTY + s));
+            if (++s == kStages) {
+                s = 0;
+                par ^= 1;
+            }
+        }
+    } else if (warp < kIssueWarp + kBlocks) {
+        // ------------------------------------------------------------ products, one warp per block
+        constexpr uint32_t idesc = idesc_bf16(128, AN, false);
+        const int blk = warp - kIssueWarp;
+        const uint32_t d = tmem + (uint32_t)(TN * blk), at = tmem + L::COL_A + blk * (DIN / 2);
+        int s = 0;
+        uint32_t par = 0;
+        bool ok = true;
+        for (int t = 0; ok && blk < n_blocks && t < n_tiles; ++t) {
+            ok = bar_wait(bar(L::FULL + s), par, abort_flag);
+#pragma unroll
+            for (int h = 0; h < ACCS; ++h) {
+                if (t > 0) ok = ok && bar_wait(bar(L::AFREE + ACCS * blk + h), (t - 1) & 1, abort_flag);
+                if (ok && elect_one()) {
+                    tc_after();
+                    const uint64_t w = tile_desc<L::ROWB>(sb + s * L::TILE + AN * h * L::ROWB);
+#pragma unroll
+                    for (int ks = 0; ks < DIN / 16; ++ks)
+                        mma_ts(d + AN * h, at + 8 * ks, w + (uint64_t)(((ks & 3) * 32 + (ks >> 2) * L::BOX) >> 4), idesc, ks > 0);
+                    tc_commit_to(bar(L::AFULL + ACCS * blk + h));
+                }
+                __syncwarp();
+            }
+            if (++s == kStages) {
+                s = 0;
+                par ^= 1;
+            }
+        }
+        // nothing of this CTA may still run on the tensor core at its end
+        if (elect_one()) tc_commit_to(bar(L::DRAIN));
+        int never = 0;
+        if (!bar_wait(bar(L::DRAIN), 0, &never)) *abort_flag = 1;
+        __syncwarp();
+    } else {
+        // ------------------------------------------------------------ tiles
+        int issued = 0;
+        bool ok = true;
+        for (int t = 0; t < n_tiles; ++t) {
+            const int s = t % kStages;
+            ok = bar_wait(bar(L::EMPTY + s), ((t / kStages) & 1) ^ 1, abort_flag);
+            if (!ok) break;
+            if (lane == 0) {
+                const int64_t c0 = (int64_t)(tile0 + t) * TN;
+                expect_bytes(bar(L::FULL + s), kTileBytes);
+#pragma unroll
+                for (int i = 0; i < L::BOXES; ++i)
+                    load_box(sb + s * L::TILE + i * L::BOX, &map, 64 * i, (int)c0, kEntriesStand ? 0 : grp, bar(L::FULL + s));
+                const uint32_t num = sb + L::OFF_NUM + s * 2 * L::NUM;
+                load_bytes(num, kEntriesStand ? a.nl2 + grp * a.np + c0 : a.b2 + grp * a.mp + c0, L::NUM, bar(L::FULL + s));
+                if (MODE == SWEEP_R) load_bytes(num + L::NUM, a.h + grp * a.mp + c0, L::NUM, bar(L::FULL + s));
+            }
+            __syncwarp();
+            ++issued;
+        }
+        if (!ok) {  // the copies in flight land before the CTA ends
+            int never = 0;
+            for (int k = issued > kStages ? issued - kStages : 0; k < issued; ++k) bar_wait(bar(L::FULL + k % kStages), (k / kStages) & 1, &never);
+        }
+    }
+
+    tc_before();
+    __syncthreads();
+    tc_after();
+    if (warp == kIssueWarp)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+    if (in) {
+        const int64_t at = ((int64_t)split * a.G + grp) * (kEntriesStand ? a.mp : a.np) + row;
+        const float r = *abort_flag ? CUDART_NAN_F : sum.s;
+        if (MODE == SWEEP_LSE) reinterpret_cast<float2*>(a.part)[at] = make_float2(*abort_flag ? CUDART_INF_F : top, r);
+        else a.part[at] = r;
+    }
+}
+
+// ---- DX, DW
+template <int DIN>
+struct Grad {
+    static constexpr int BLOCKS = DIN == 128 ? 1 : 2;
+    static constexpr int TN = 64;                      // rows of a tile, columns of a score buffer
+    static constexpr int READ_WARPS = 8 * BLOCKS, ISSUE_WARP = READ_WARPS, LOAD_WARP = ISSUE_WARP + BLOCKS, THREADS = (LOAD_WARP + 1) * 32;
+    static constexpr int ROWB = DIN >= 64 ? 128 : 64;
+    static constexpr int BOXES = DIN == 128 ? 2 : 1;
+    static constexpr int BOX = TN * ROWB, TILE = BOXES * BOX, STAGES = 8;
+    static constexpr int ON = DIN < 64 ? DIN : 64;     // columns of O that one product covers: a box
+    static constexpr int OFF_NUM = STAGES * TILE, NUM = TN * 4, OFF_SUM = OFF_NUM + STAGES * 2 * NUM, OFF_BAR = OFF_SUM + BLOCKS * 128 * 4;
+    enum { FULL = 0, EMPTY = STAGES, SFULL = 2 * STAGES, TREADY = SFULL + 2 * BLOCKS, OFULL = TREADY + 2 * BLOCKS, COUNT = OFULL + BLOCKS };
+    static constexpr int OFF_ABORT = OFF_BAR + COUNT * 8, SMEM = OFF_ABORT + 16;
+    static_assert(SMEM <= 226 * 1024 && BOX % 1024 == 0, "shared memory");
+    static constexpr uint32_t COL_O = 2 * TN, COL_A = COL_O + DIN, COL_BLOCK = COL_A + DIN / 2;  // a block's: two buffers, O, inputs
+    static_assert(BLOCKS * COL_BLOCK <= 512, "TMEM columns");
+    static_assert(kSweepPad % TN == 0, "numbers are copied a tile at a time");
+};
+
+template <int DIN, int MODE>
+__global__ void __launch_bounds__(Grad<DIN>::THREADS, 1) grad_kernel(const __grid_constant__ CUtensorMap map, const SweepArgs a)
+{
+    using L = Grad<DIN>;
+    constexpr int TN = L::TN;
+    constexpr bool kEntriesStand = MODE == SWEEP_DW;
+    extern __shared__ __align__(1024) unsigned char sm[];
+    __shared__ uint32_t tmem_slot;
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
+    const uint32_t sb = smem_u32(sm);
+    auto bar = [&](int i) { return sb + L::OFF_BAR + 8u * (uint32_t)i; };
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(sm + L::OFF_ABORT);
+    const int split = (int)(blockIdx.x % (uint32_t)a.splits);
+    const int64_t n_stand = kEntriesStand ? a.m : a.n, n_stream = kEntriesStand ? a.n : a.m;
+    const int64_t row0 = (int64_t)(blockIdx.x / (uint32_t)a.splits) * (128 * L::BLOCKS);
+    const int n_blocks = (int)min((n_stand - row0 + 127) / 128, (int64_t)L::BLOCKS);
+    // tiles of one group after the other (DW: the block's group alone)
+    const int per_group = (int)((n_stream + TN - 1) / TN);
+    const int64_t all_tiles = (int64_t)per_group * (kEntriesStand ? 1 : a.G);
+    const int64_t tile0 = all_tiles * split / a.splits;
+    const int n_tiles = (int)(all_tiles * (split + 1) / a.splits - tile0);
+    const int first_group = kEntriesStand ? (int)blockIdx.y : (int)(tile0 / max(per_group, 1)), first_tile = (int)(tile0 - (kEntriesStand ? 0 : (int64_t)first_group * per_group));
+
+    const int e = warp >> 3, buf = (warp >> 2) & 1;
+    const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
+    const int at_row = 128 * e + (warp & 3) * 32 + lane;
+    const int64_t row = row0 + at_row;
+    const bool in = warp < L::READ_WARPS && row < n_stand;
+    if (tid == 0) {
+        for (int s = 0; s < L::STAGES; ++s) {
+            bar_init(bar(L::FULL + s), 1);
+            bar_init(bar(L::EMPTY + s), (uint32_t)n_blocks);
+        }
+        for (int i = 0; i < 2 * L::BLOCKS; ++i) {
+            bar_init(bar(L::SFULL + i), 1);
+            bar_init(bar(L::TREADY + i), 4);
+        }
+        for (int i = 0; i < L::BLOCKS; ++i) bar_init(bar(L::OFULL + i), 1);
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == L::ISSUE_WARP) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_before();
+    __syncthreads();
+    tc_after();
+    const uint32_t tmem = tmem_slot, tblock = tmem + (uint32_t)e * L::COL_BLOCK;
+    if (warp < 8 * n_blocks && buf == 0)
+        load_inputs<DIN>(tblock + lane_base + L::COL_A, (kEntriesStand ? a.W + ((int64_t)blockIdx.y * a.m + row) * DIN : a.x + row * DIN), in);
+    if (warp < L::LOAD_WARP) {  // (the loading warp is on its way)
+        tc_before();
+        asm volatile("bar.sync 1, %0;" ::"n"(L::LOAD_WARP * 32) : "memory");
+        tc_after();
+    }
+
+    LongSum sum;
+    if (warp < L::READ_WARPS) {
+        // ------------------------------------------------------------ weights, thread = standing row, every second tile
+        int g = first_group, in_group = first_tile;
+        auto own0 = [&] { return !in ? -CUDART_INF_F : kEntriesStand ? a.b2[g * a.mp + row] : a.nl2[g * a.np + row]; };
+        auto own1 = [&] { return !in ? 0.f : kEntriesStand ? a.h[g * a.mp + row] : -a.r[g * a.np + row]; };
+        float log_own = 0.f, h_own = 0.f;
+        if (n_tiles > 0) {
+            log_own = own0();
+            h_own = own1();
+        }
+        const uint32_t ts = tblock + lane_base + (uint32_t)(TN * buf);
+        if (buf == 1) ++in_group;
+        for (int t = buf; e < n_blocks && t < n_tiles; t += 2, in_group += 2) {
+            if (!kEntriesStand && in_group >= per_group) {
+                do {
+                    in_group -= per_group;
+                    ++g;
+                } while (in_group >= per_group);
+                log_own = own0();
+                h_own = own1();
+            }
+            const int s = t % L::STAGES;
+            if (!bar_wait(bar(L::SFULL + 2 * e + buf), (t >> 1) & 1, abort_flag)) break;
+            if (!bar_wait(bar(L::FULL + s), (t / L::STAGES) & 1, abort_flag)) break;  // (long complete: the numbers are to be seen)
+            tc_after();
+            const float* num = reinterpret_cast<const float*>(sm + L::OFF_NUM + s * 2 * L::NUM);
+#pragma unroll
+            for (int c = 0; c < TN / 32; ++c) {
+                uint32_t v[32], w[16];
+                ld32(ts + 32 * c, v);
+                wait_ld32(v);
+                const float4 *n0 = reinterpret_cast<const float4*>(num + 32 * c), *n1 = n0 + TN / 4;
+                F2 part{0.f, 0.f};
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    const float4 k = n0[q], hk = n1[q];
+                    const F2 u0 = fma2(pair(v, 4 * q), both(kLog2e), add2({k.x, k.y}, both(log_own)));
+                    const F2 u1 = fma2(pair(v, 4 * q + 2), both(kLog2e), add2({k.z, k.w}, both(log_own)));
+                    // DX: p (h_j - r_i), own is -r_i;  DW: p (h_j - r_i), own is h_j and the column's number r_i
+                    const F2 d0 = kEntriesStand ? fma2({hk.x, hk.y}, both(-1.f), both(h_own)) : add2({hk.x, hk.y}, both(h_own));
+                    const F2 d1 = kEntriesStand ? fma2({hk.z, hk.w}, both(-1.f), both(h_own)) : add2({hk.z, hk.w}, both(h_own));
+                    const F2 w0 = mul2({ex2(u0.x), ex2(u0.y)}, d0), w1 = mul2({ex2(u1.x), ex2(u1.y)}, d1);
+                    if (kEntriesStand) part = add2(part, add2(w0, w1));
+                    w[2 * q] = pack_bf16(w0.x, w0.y);
+                    w[2 * q + 1] = pack_bf16(w1.x, w1.y);
+                }
+                if (kEntriesStand) sum.add(part.x + part.y);
+                st16(ts + 16 * c, w);  // over columns whose scores have been read
+            }
+            wait_st();
+            tc_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive(bar(L::TREADY + 2 * e + buf));
+        }
+    } else if (warp < L::LOAD_WARP) {
+        // ------------------------------------------------------------ products, one warp per block
+        // The weighted sum of tile t, then the scores of tile t + 2 into the buffer that it has read: one thread's products run in order.
+        constexpr uint32_t idesc_s = idesc_bf16(128, TN, false), idesc_o = idesc_bf16(128, L::ON, true);
+        const int blk = warp - L::ISSUE_WARP;
+        const uint32_t tb = tmem + (uint32_t)blk * L::COL_BLOCK;
+        bool ok = blk < n_blocks;
+        for (int t = -2; ok && t < n_tiles; ++t) {
+            const int nxt = t + 2;
+            if (t >= 0) {
+                ok = bar_wait(bar(L::TREADY + 2 * blk + (t & 1)), (t >> 1) & 1, abort_flag);
+                if (ok && elect_one()) {
+                    tc_after();
+                    const uint32_t tile = sb + (t % L::STAGES) * L::TILE, tw = tb + (uint32_t)(TN * (t & 1));
+#pragma unroll
+                    for (int ks = 0; ks < TN / 16; ++ks)
+#pragma unroll
+                        for (int o = 0; o < L::BOXES; ++o)
+                            mma_ts(tb + L::COL_O + 64 * o, tw + 8 * ks, tile_desc<L::ROWB>(tile + o * L::BOX + ks * 16 * L::ROWB), idesc_o, (t > 0) | (ks > 0));
+                    tc_commit_to(bar(L::EMPTY + t % L::STAGES));
+                }
+                __syncwarp();
+            }
+            if (nxt >= n_tiles) continue;
+            ok = ok && bar_wait(bar(L::FULL + nxt % L::STAGES), (nxt / L::STAGES) & 1, abort_flag);
+            if (ok && elect_one()) {
+                tc_after();
+                const uint64_t w = tile_desc<L::ROWB>(sb + (nxt % L::STAGES) * L::TILE);
+#pragma unroll
+                for (int ks = 0; ks < DIN / 16; ++ks)
+                    mma_ts(tb + (uint32_t)(TN * (nxt & 1)), tb + L::COL_A + 8 * ks, w + (uint64_t)(((ks & 3) * 32 + (ks >> 2) * L::BOX) >> 4), idesc_s, ks > 0);
+                tc_commit_to(bar(L::SFULL + 2 * blk + (nxt & 1)));
+            }
+            __syncwarp();
+        }
+        // O is complete, and nothing of this CTA may still run on the tensor core at its end
+        if (elect_one()) tc_commit_to(bar(L::OFULL + blk));
+        int never = 0;
+        if (!bar_wait(bar(L::OFULL + blk), 0, &never)) *abort_flag = 1;
+        __syncwarp();
+    } else {
+        // ------------------------------------------------------------ tiles
+        int issued = 0, g = first_group, in_group = first_tile;
+        bool ok = true;
+        for (int t = 0; t < n_tiles; ++t, ++in_group) {
+            if (!kEntriesStand && in_group == per_group) {
+                in_group = 0;
+                ++g;
+            }
+            const int s = t % L::STAGES;
+            ok = bar_wait(bar(L::EMPTY + s), ((t / L::STAGES) & 1) ^ 1, abort_flag);
+            if (!ok) break;
+            if (lane == 0) {
+                const int64_t c0 = (int64_t)in_group * TN;
+                expect_bytes(bar(L::FULL + s), L::TILE + 2 * L::NUM);
+#pragma unroll
+                for (int i = 0; i < L::BOXES; ++i)
+                    load_box(sb + s * L::TILE + i * L::BOX, &map, 64 * i, (int)c0, kEntriesStand ? 0 : g, bar(L::FULL + s));
+                const uint32_t num = sb + L::OFF_NUM + s * 2 * L::NUM;
+                load_bytes(num, kEntriesStand ? a.nl2 + g * a.np + c0 : a.b2 + g * a.mp + c0, L::NUM, bar(L::FULL + s));
+                load_bytes(num + L::NUM, kEntriesStand ? a.r + g * a.np + c0 : a.h + g * a.mp + c0, L::NUM, bar(L::FULL + s));
+            }
+            __syncwarp();
+            ++issued;
+        }
+        if (!ok) {  // the copies in flight land before the CTA ends
+            int never = 0;
+            for (int k = issued > L::STAGES ? issued - L::STAGES : 0; k < issued; ++k) bar_wait(bar(L::FULL + k % L::STAGES), (k / L::STAGES) & 1, &never);
+        }
+    }
+
+    float* const half = reinterpret_cast<float*>(sm + L::OFF_SUM);
+    if (warp < L::READ_WARPS && buf == 1) half[at_row] = sum.s;
+    tc_before();
+    __syncthreads();
+    tc_after();
+    if (warp < 8 * n_blocks && buf == 0) {
+        const bool bad = *abort_flag != 0;
+        float* out = kEntriesStand ? a.part + (((int64_t)split * a.G + blockIdx.y) * a.m + row) * DIN : a.part + ((int64_t)split * a.n + row) * DIN;
+#pragma unroll
+        for (int c = 0; c < DIN / 32; ++c) {
+            uint32_t v[32];
+            ld32(tblock + lane_base + L::COL_O + 32 * c, v);
+            wait_ld32(v);
+            if (!in) continue;
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                float4 o = make_float4(__uint_as_float(v[4 * q]), __uint_as_float(v[4 * q + 1]), __uint_as_float(v[4 * q + 2]), __uint_as_float(v[4 * q + 3]));
+                if (n_tiles == 0) o = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (bad) o.x = o.y = o.z = o.w = CUDART_NAN_F;
+                reinterpret_cast<float4*>(out)[8 * c + q] = o;
+            }
+        }
+        if (kEntriesStand && in) a.part2[((int64_t)split * a.G + blockIdx.y) * a.mp + row] = bad ? CUDART_NAN_F : sum.s + half[at_row];
+    }
+    tc_before();
+    __syncthreads();
+    tc_after();
+    if (warp == L::ISSUE_WARP)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+}
+
+struct Shape {
+    int rows, tile;     // standing rows of a CTA, streaming rows of a tile
+    int64_t start;      // what a CTA costs besides its tiles, in tiles
+};
+Shape shape_of(int d, int mode)
+{
+    if (mode == SWEEP_DX || mode == SWEEP_DW) return Shape{d == 128 ? 128 : 256, 64, 8};
+    return Shape{kRows, d == 128 ? 96 : 128, 4};
+}
+
+template <int DIN>
+cudaError_t launch_t(int mode, const SweepArgs& a, const CUtensorMap& map, dim3 grid, cudaStream_t s)
+{
+    const Launch l{s, nullptr, nullptr};
+    switch (mode) {
+        case SWEEP_LSE: return launch_kernel(l, sweep_kernel<DIN, SWEEP_LSE>, grid, kSweepThreads, Sweep<DIN>::SMEM, 1, map, a);
+        case SWEEP_MEAN: return launch_kernel(l, sweep_kernel<DIN, SWEEP_MEAN>, grid, kSweepThreads, Sweep<DIN>::SMEM, 1, map, a);
+        case SWEEP_R: return launch_kernel(l, sweep_kernel<DIN, SWEEP_R>, grid, kSweepThreads, Sweep<DIN>::SMEM, 1, map, a);
+        case SWEEP_DX: return launch_kernel(l, grad_kernel<DIN, SWEEP_DX>, grid, Grad<DIN>::THREADS, Grad<DIN>::SMEM, 1, map, a);
+        default: return launch_kernel(l, grad_kernel<DIN, SWEEP_DW>, grid, Grad<DIN>::THREADS, Grad<DIN>::SMEM, 1, map, a);
+    }
+}
+
+}  // namespace
+
+// Blocks that share a standing row's streaming ones: the number with the shortest run, counting whole rounds of blocks over the SMs.
+int sweep_splits(int64_t n, int G, int d, int64_t m, int mode)
+{
+    const Shape sh = shape_of(d, mode);
+    const bool entries = mode == SWEEP_MEAN || mode == SWEEP_DW;
+    const int64_t groups = mode == SWEEP_DX ? G : 1;
+    const int64_t blocks = ((entries ? m : n) + sh.rows - 1) / sh.rows * (mode == SWEEP_DX ? 1 : G);
+    const int64_t tiles = ((entries ? n : m) + sh.tile - 1) / sh.tile * groups;
+    int best = 1;
+    int64_t best_cost = INT64_MAX;
+    for (int sp = 1; sp <= kSweepMaxSplits && sp <= std::max<int64_t>(tiles, 1); ++sp) {
+        const int64_t rounds = (blocks * sp + 147) / 148, cost = rounds * ((tiles + sp - 1) / sp + sh.start);
+        if (cost < best_cost) {
+            best_cost = cost;
+            best = sp;
+        }
+    }
+    return best;
+}
+
+cudaError_t launch_sweep(int mode, int d, SweepArgs& a, cudaStream_t s)
+{
+    const Shape sh = shape_of(d, mode);
+    const bool entries = mode == SWEEP_MEAN || mode == SWEEP_DW;
+    a.splits = sweep_splits(a.n, a.G, d, a.m, mode);
+    const int64_t stand = entries ? a.m : a.n;
+    if (stand == 0) return cudaSuccess;
+    CUtensorMap map;
+    const CUtensorMapSwizzle swizzle = d < 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B;
+    // (without positions nothing streams, and the map is not used)
+    if (!encode_groups(&map, entries && a.n > 0 ? (const void*)a.x : a.W, d, entries && a.n > 0 ? a.n : a.m, entries && a.n > 0 ? 1 : a.G, d < 64 ? d : 64,
+                       sh.tile, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_128B))
+        return cudaErrorInvalidValue;
+    const dim3 grid((unsigned)((stand + sh.rows - 1) / sh.rows * a.splits), mode == SWEEP_DX ? 1u : (unsigned)a.G);
+    switch (d) {
+        case 32: return launch_t<32>(mode, a, map, grid, s);
+        case 64: return launch_t<64>(mode, a, map, grid, s);
+        default: return launch_t<128>(mode, a, map, grid, s);
+    }
+}
+
+}  // namespace ckv
