@@ -296,7 +296,7 @@ CKV_API ckv_status ckv_project(int32_t device, int32_t n, int32_t n_groups, int3
  * be captured into a graph.  `idx` is what ckv_route writes, int32 [n][n_groups]; an index outside [0, n_entries) marks a
  * position without an entry (padding): it takes no part in the losses and gradients of its group, whatever its inputs hold.
  * Results are the same bits from call to call.  Array arguments are device memory of `device` (or managed), aligned to
- * their elements, W to 16 bytes.  `workspace` is device memory on a 256-byte boundary of at least the size that the _bytes
+ * their elements, W and d_out to 16 bytes.  `workspace` is device memory on a 256-byte boundary of at least the size that the _bytes
  * function of the call gives, of any contents; calls that may overlap on the GPU, captured graphs among them, need one each.
  * Errors of all of them: INVALID_ARG (sizes, null, host or misaligned pointers, workspace too small), UNSUPPORTED (d_in,
  * head_dim, more than 65535 groups), SHAPE (d_shared outside [1, head_dim]), CUDA.

@@ -168,7 +168,7 @@ ckv_status ckv_gather_grad(int32_t device, int32_t dtype, int32_t n, int32_t n_g
     if (!dg.ok) return CKV_ERR_CUDA;
     const int e = dtype == CKV_F32 ? 4 : 2;
     const bool none = n == 0;
-    if (!on_device(Arg{pool, e, !score}, Arg{order, 4, none}, Arg{offset, 4}, Arg{score, 4, true}, Arg{d_out, e, none}, Arg{d_pool, 4},
+    if (!on_device(Arg{pool, e, !score}, Arg{order, 4, none}, Arg{offset, 4}, Arg{score, 4, true}, Arg{d_out, 16, none}, Arg{d_pool, 4},
                    Arg{d_user, e, true}, Arg{d_score, 4, none || !score}) ||
         (d_score && !score))
         return CKV_ERR_INVALID_ARG;

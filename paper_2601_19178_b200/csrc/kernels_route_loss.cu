@@ -27,7 +27,6 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
-__device__ __forceinline__ float bf(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
 __device__ __forceinline__ float sigmoid(float x) { return 1.f / (1.f + expf(-x)); }
 
 struct Space {
@@ -38,27 +37,31 @@ struct Space {
     uint16_t* xs;        // x with zeros for a position that takes part in no group
     float* part;         // partial results of a pass
     float* part2;
-    int32_t* rows_part;  // [blocks][G] positions that take part, and their -log sigmoid(score)
-    double* peak_part;
-    int32_t* live_part;  // [blocks of 256][G] positions of them that have a weight (scores that are not all -inf)
+    // forward, per block of 256 positions and group: those that take part, those of them that have a weight (scores that are not all
+    // -inf), the sum of -log sigmoid(score);  per block of entries and group: the sum for the balance loss
+    int32_t *rows_part, *live_part;
+    double *peak_part, *balance_part;
+    unsigned* done;      // [G] blocks of entries that are done
     float *ds, *sum, *wsum;  // gradient: coefficient of the picked entry [n][G], sums over an entry's positions
     void* seg;
     int64_t bytes;
 };
-constexpr int kPrepRows = 256;
+constexpr int kMeanEntries = 1024;  // of a block of mean_join_kernel
 
 Space layout(void* ws, int64_t n, int G, int d, int64_t m, bool grad)
 {
     Carve c(ws);
     Space s{};
-    const int64_t np = sweep_padded(n), mp = sweep_padded(m), blocks = (n + kPrepRows - 1) / kPrepRows;
+    const int64_t np = sweep_padded(n), mp = sweep_padded(m), blocks = (np + 255) / 256;
     s.b2 = c.take<float>(G * mp);
     s.nl2 = c.take<float>(G * np);
     s.xs = c.take<uint16_t>(n * d);
     if (!grad) {
         s.rows_part = c.take<int32_t>(blocks * G);
+        s.live_part = c.take<int32_t>(blocks * G);
         s.peak_part = c.take<double>(blocks * G);
-        s.live_part = c.take<int32_t>((np + 255) / 256 * G);
+        s.balance_part = c.take<double>((m + kMeanEntries - 1) / kMeanEntries * G);
+        s.done = c.take<unsigned>(G);
         s.part = c.take<float>(std::max(2 * sweep_splits(n, G, d, m, SWEEP_LSE) * G * np, sweep_splits(n, G, d, m, SWEEP_MEAN) * G * mp));
     } else {
         s.h = c.take<float>(G * mp);
@@ -77,10 +80,11 @@ Space layout(void* ws, int64_t n, int G, int d, int64_t m, bool grad)
 // ---- what the passes read
 __global__ void __launch_bounds__(256) entries_kernel(const float* __restrict__ bias, const float* __restrict__ mean,
                                                       const int32_t* __restrict__ offset, float w_balance, int64_t m, int64_t mp,
-                                                      float* __restrict__ b2, float* __restrict__ h)
+                                                      float* __restrict__ b2, float* __restrict__ h, unsigned* __restrict__ done)
 {
     const int64_t j = blockIdx.x * (int64_t)256 + threadIdx.x;
     const int g = blockIdx.y;
+    if (j == 0 && done) done[g] = 0;
     if (j >= mp) return;
     b2[g * mp + j] = j < m ? (bias ? bias[g * m + j] * kLog2e : 0.f) : -CUDART_INF_F;
     if (!h) return;
@@ -90,128 +94,143 @@ __global__ void __launch_bounds__(256) entries_kernel(const float* __restrict__ 
     h[g * mp + j] = u > 0.f ? w_balance / (float)max(rows, 1) * logf(u) : 0.f;
 }
 
-// Positions: x for the passes; forward: the picked entry's score and the sums for the peak loss; gradient: -lse and the picked entry's
-// coefficient.
-__global__ void __launch_bounds__(kPrepRows) positions_kernel(const RouteLossArgs a, const RouteGradArgs b, Space s, bool grad)
+// Positions: x for the passes (zeros for one that takes part in no group, whose inputs may be anything); forward: the picked entry's
+// score; gradient: -lse and the picked entry's coefficient.  A position to D / 8 lanes, 16 bytes of it to each.
+template <int D, bool GRAD>
+__global__ void __launch_bounds__(256) positions_kernel(const RouteLossArgs a, const RouteGradArgs b, const Space s, int64_t np, bool whole)
 {
-    const int64_t i = blockIdx.x * (int64_t)kPrepRows + threadIdx.x, np = (a.n + kSweepPad - 1) / kSweepPad * kSweepPad;
-    bool any = false;
-    for (int g = 0; g < a.G; ++g) {
-        const int32_t k = i < a.n ? a.idx[i * a.G + g] : -1;
-        const bool real = k >= 0 && k < a.m;
-        any |= real;
-        if (grad) {
+    constexpr int LANES = D / 8;
+    const int64_t i = blockIdx.x * (int64_t)(256 / LANES) + threadIdx.x / LANES;
+    const int sub = threadIdx.x % LANES;
+    const bool there = i < a.n;
+    uint4 raw = make_uint4(0, 0, 0, 0);
+    if (there) {
+        const uint16_t* x = (const uint16_t*)a.x + i * D + 8 * sub;
+        if (whole) raw = __ldg(reinterpret_cast<const uint4*>(x));
+        else {
+            uint32_t w[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) w[q] = x[2 * q] | (uint32_t)x[2 * q + 1] << 16;
+            raw = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    }
+    const uint32_t xw[4] = {raw.x, raw.y, raw.z, raw.w};
+    int any = 0;
+    if (GRAD) {
+        for (int g = sub; g < a.G; g += LANES) {
+            const int32_t k = there ? __ldg(a.idx + i * a.G + g) : -1;
+            const bool real = k >= 0 && k < a.m;
+            any |= real;
             if (i < np) {
-                const float lse = real ? a.lse[i * a.G + g] : -CUDART_INF_F;
+                const float lse = real ? __ldg(a.lse + i * a.G + g) : -CUDART_INF_F;
                 s.nl2[g * np + i] = lse == -CUDART_INF_F ? lse : -lse * kLog2e;
             }
-            if (i < a.n) {
+            if (there) {
                 float v = 0.f;
                 if (real) {
-                    const int32_t rows = b.offset[(int64_t)g * (a.m + 1) + a.m];
-                    v = -b.w_peak / (float)max(rows, 1) * sigmoid(-a.score[i * a.G + g]);
-                    if (b.d_score) v += b.d_score[i * a.G + g];
+                    const int32_t rows = __ldg(b.offset + (int64_t)g * (a.m + 1) + a.m);
+                    v = -b.w_peak / (float)max(rows, 1) * sigmoid(-__ldg(a.score + i * a.G + g));
+                    if (b.d_score) v += __ldg(b.d_score + i * a.G + g);
                 }
                 s.ds[i * a.G + g] = v;
             }
-        } else {
+        }
+#pragma unroll
+        for (int d = LANES / 2; d > 0; d /= 2) any |= __shfl_xor_sync(0xffffffffu, any, d);
+    } else {
+#pragma unroll 2
+        for (int g = 0; g < a.G; ++g) {
+            const int32_t k = there ? __ldg(a.idx + i * a.G + g) : -1;
+            const bool real = k >= 0 && k < a.m;
+            any |= real;
             float sc = 0.f;
             if (real) {
-                const uint16_t *x = (const uint16_t*)a.x + i * a.d, *w = (const uint16_t*)a.W + ((int64_t)g * a.m + k) * a.d;
-                for (int c = 0; c < a.d; ++c) sc = fmaf(bf(x[c]), bf(w[c]), sc);
-                if (a.bias) sc += a.bias[(int64_t)g * a.m + k];
-            }
-            if (i < a.n) a.score[i * a.G + g] = sc;
-            // -log sigmoid(sc)
-            double soft = real ? (double)(fmaxf(-sc, 0.f) + log1pf(expf(-fabsf(sc)))) : 0.0;
-            __shared__ double sum[8];
-            __shared__ int count[8];
-            const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+                const uint4 w = __ldg(reinterpret_cast<const uint4*>((const uint16_t*)a.W + ((int64_t)g * a.m + k) * D) + sub);
+                const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-            for (int d = 16; d > 0; d /= 2) soft += __shfl_xor_sync(0xffffffffu, soft, d);
-            const int rows = __popc(__ballot_sync(0xffffffffu, real));
-            if (lane == 0) {
-                sum[warp] = soft;
-                count[warp] = rows;
-            }
-            __syncthreads();
-            if (threadIdx.x == 0) {
-                double t = 0;
-                int c = 0;
-                for (int w = 0; w < 8; ++w) {
-                    t += sum[w];
-                    c += count[w];
+                for (int q = 0; q < 4; ++q) {
+                    sc = fmaf(__uint_as_float(xw[q] << 16), __uint_as_float(ww[q] << 16), sc);
+                    sc = fmaf(__uint_as_float(xw[q] & 0xffff0000u), __uint_as_float(ww[q] & 0xffff0000u), sc);
                 }
-                s.peak_part[(int64_t)blockIdx.x * a.G + g] = t;
-                s.rows_part[(int64_t)blockIdx.x * a.G + g] = c;
             }
-            __syncthreads();
+#pragma unroll
+            for (int d = LANES / 2; d > 0; d /= 2) sc += __shfl_xor_sync(0xffffffffu, sc, d);
+            if (sub == 0 && there) a.score[i * a.G + g] = real && a.bias ? sc + __ldg(a.bias + (int64_t)g * a.m + k) : sc;
         }
     }
-    if (i < a.n)
-        for (int c = 0; c < a.d; ++c) s.xs[i * a.d + c] = any ? ((const uint16_t*)a.x)[i * a.d + c] : (uint16_t)0;
+    if (there) reinterpret_cast<uint4*>(s.xs + i * D)[sub] = any ? raw : make_uint4(0, 0, 0, 0);
 }
 
 // ---- joins
-__global__ void __launch_bounds__(256) lse_join_kernel(const RouteLossArgs a, const SweepArgs p, float* __restrict__ nl2,
-                                                       int32_t* __restrict__ live_part)
-{
-    const int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x;
-    const int g = blockIdx.y;
-    const int32_t k = i < a.n ? a.idx[i * a.G + g] : -1;
-    const bool real = k >= 0 && k < a.m;
-    float lse = 0.f, neg = -CUDART_INF_F;
-    if (real) {
-        float top = -CUDART_INF_F, sum = 0.f;
-        for (int z = 0; z < p.splits; ++z) top = fmaxf(top, reinterpret_cast<const float2*>(p.part)[((int64_t)z * a.G + g) * p.np + i].x);
-        for (int z = 0; z < p.splits; ++z) {
-            const float2 v = reinterpret_cast<const float2*>(p.part)[((int64_t)z * a.G + g) * p.np + i];
-            if (v.x > -CUDART_INF_F) sum = fmaf(v.y, exp2f(v.x - top), sum);
-        }
-        const float l2 = top + log2f(sum);
-        if (top == -CUDART_INF_F) lse = top;  // every entry's score is -inf: no weight anywhere
-        else {
-            lse = l2 * kLn2;
-            neg = -l2;
-        }
-    }
-    if (i < p.np) nl2[g * p.np + i] = neg;
-    if (i < a.n) a.lse[i * a.G + g] = lse;
-    const int live = __syncthreads_count(neg != -CUDART_INF_F);
-    if (threadIdx.x == 0) live_part[(int64_t)blockIdx.x * a.G + g] = live;
-}
-
 __device__ double block_sum(double v)
 {
-    __shared__ double part[32];
+    __shared__ double part[8];
     __syncthreads();
 #pragma unroll
     for (int d = 16; d > 0; d /= 2) v += __shfl_xor_sync(0xffffffffu, v, d);
     if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
     __syncthreads();
     double t = 0;
-    for (int w = 0; w < (int)blockDim.x / 32; ++w) t += part[w];
+#pragma unroll
+    for (int w = 0; w < 8; ++w) t += part[w];
     return t;
 }
 
-// One block per group: the mean weights, and both losses.  mean log(mean m) is summed as (u log u - u + 1) / m with u = mean m:
-// the weights sum to one, so that nothing is added, and near balance, where u log u and the sum's other terms cancel, each
-// term is as small as what it stands for.  (They sum to less by the share of the positions that have no weight.)
-__global__ void __launch_bounds__(1024) mean_join_kernel(const RouteLossArgs a, const SweepArgs p, const Space s, int blocks, int live_blocks)
+__global__ void __launch_bounds__(256) lse_join_kernel(const RouteLossArgs a, const SweepArgs p, const Space s)
 {
-    const int g = blockIdx.x;
-    double peak = 0, rows_d = 0, live = 0;
-    for (int b = threadIdx.x; b < blocks; b += 1024) {
-        peak += s.peak_part[(int64_t)b * a.G + g];
-        rows_d += s.rows_part[(int64_t)b * a.G + g];
+    const int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x;
+    const int g = blockIdx.y;
+    const int32_t k = i < a.n ? __ldg(a.idx + i * a.G + g) : -1;
+    const bool real = k >= 0 && k < a.m;
+    float lse = 0.f, neg = -CUDART_INF_F;
+    double soft = 0;
+    if (real) {
+        const float2* part = reinterpret_cast<const float2*>(p.part) + g * p.np + i;
+        const int64_t step = a.G * p.np;
+        float top = -CUDART_INF_F, sum = 0.f;
+        for (int z = 0; z < p.splits; ++z) {
+            const float2 v = part[z * step];
+            const float both = fmaxf(top, v.x);
+            if (both > -CUDART_INF_F) sum = sum * exp2f(top - both) + v.y * exp2f(v.x - both);
+            top = both;
+        }
+        if (top == -CUDART_INF_F) lse = top;  // every entry's score is -inf: no weight anywhere
+        else {
+            neg = -(top + log2f(sum));
+            lse = -neg * kLn2;
+        }
+        const float sc = a.score[i * a.G + g];
+        soft = fmaxf(-sc, 0.f) + log1pf(expf(-fabsf(sc)));  // -log sigmoid(sc)
     }
-    for (int b = threadIdx.x; b < live_blocks; b += 1024) live += s.live_part[(int64_t)b * a.G + g];
-    peak = block_sum(peak);
-    rows_d = block_sum(rows_d);
-    live = block_sum(live);
-    const float inv = rows_d > 0 ? (float)(1.0 / rows_d) : 0.f;
+    if (i < p.np) s.nl2[g * p.np + i] = neg;
+    if (i < a.n) a.lse[i * a.G + g] = lse;
+    const int rows = __syncthreads_count(real), live = __syncthreads_count(neg != -CUDART_INF_F);
+    soft = block_sum(soft);
+    if (threadIdx.x == 0) {
+        const int64_t at = (int64_t)g * gridDim.x + blockIdx.x;
+        s.rows_part[at] = rows;
+        s.live_part[at] = live;
+        s.peak_part[at] = soft;
+    }
+}
+
+// The mean weights, and in a group's last block both losses, from partial sums in the order of the blocks.  mean log(mean m) is
+// summed as (u log u - u + 1) / m with u = mean m: the weights sum to one, so that nothing is added, and near balance, where u
+// log u and the sum's other terms cancel, each term is as small as what it stands for.  (They sum to less by the share of the
+// positions that have no weight.)
+__global__ void __launch_bounds__(256) mean_join_kernel(const RouteLossArgs a, const SweepArgs p, const Space s, int blocks)
+{
+    __shared__ bool last;
+    const int g = blockIdx.y;
+    double rows = 0;
+    for (int b = threadIdx.x; b < blocks; b += 256) rows += s.rows_part[(int64_t)g * blocks + b];
+    rows = block_sum(rows);
+    const float inv = rows > 0 ? (float)(1.0 / rows) : 0.f;
     double balance = 0;
-    for (int64_t j = threadIdx.x; j < a.m; j += 1024) {
+#pragma unroll
+    for (int q = 0; q < kMeanEntries / 256; ++q) {
+        const int64_t j = blockIdx.x * (int64_t)kMeanEntries + q * 256 + threadIdx.x;
+        if (j >= a.m) continue;
         float sum = 0.f;
         for (int z = 0; z < p.splits; ++z) sum += p.part[((int64_t)z * a.G + g) * p.mp + j];
         const float mean = sum * inv;
@@ -221,8 +240,26 @@ __global__ void __launch_bounds__(1024) mean_join_kernel(const RouteLossArgs a, 
     }
     balance = block_sum(balance);
     if (threadIdx.x == 0) {
-        a.loss[2 * g] = rows_d > 0 ? (float)(balance / (double)a.m + (live - rows_d) / rows_d) : 0.f;
-        a.loss[2 * g + 1] = rows_d > 0 ? (float)(peak / rows_d) : 0.f;
+        s.balance_part[(int64_t)g * gridDim.x + blockIdx.x] = balance;
+        __threadfence();
+        last = atomicAdd(s.done + g, 1u) + 1 == gridDim.x;
+        __threadfence();
+    }
+    __syncthreads();
+    if (!last) return;
+    double peak = 0, live = 0;
+    for (int b = threadIdx.x; b < blocks; b += 256) {
+        live += s.live_part[(int64_t)g * blocks + b];
+        peak += s.peak_part[(int64_t)g * blocks + b];
+    }
+    balance = 0;
+    for (int b = threadIdx.x; b < (int)gridDim.x; b += 256) balance += *(volatile double*)(s.balance_part + (int64_t)g * gridDim.x + b);
+    live = block_sum(live);
+    peak = block_sum(peak);
+    balance = block_sum(balance);
+    if (threadIdx.x == 0) {
+        a.loss[2 * g] = rows > 0 ? (float)(balance / (double)a.m + (live - rows) / rows) : 0.f;
+        a.loss[2 * g + 1] = rows > 0 ? (float)(peak / rows) : 0.f;
     }
 }
 
@@ -237,36 +274,74 @@ __global__ void __launch_bounds__(256) r_join_kernel(const SweepArgs p, float* _
     r[g * p.np + i] = sum;
 }
 
-// dx: the partial sums and the picked entries' rows
-__global__ void __launch_bounds__(256) dx_join_kernel(const RouteLossArgs a, const RouteGradArgs b, const SweepArgs p, const float* __restrict__ ds)
+// Eight elements of a row: partial sums added in their order, and rounded.
+__device__ __forceinline__ void add8(float (&v)[8], const float* p)
 {
-    for (int64_t e = blockIdx.x * (int64_t)256 + threadIdx.x; e < a.n * a.d; e += (int64_t)gridDim.x * 256) {
-        const int64_t i = e / a.d;
-        const int c = (int)(e - i * a.d);
-        float sum = 0.f;
-        for (int z = 0; z < p.splits; ++z) sum += p.part[(int64_t)z * a.n * a.d + e];
-        for (int g = 0; g < a.G; ++g) {
-            const int32_t k = a.idx[i * a.G + g];
-            if (k >= 0 && k < a.m) sum = fmaf(ds[i * a.G + g], bf(((const uint16_t*)a.W)[((int64_t)g * a.m + k) * a.d + c]), sum);
-        }
-        ((__nv_bfloat16*)b.dx)[e] = __float2bfloat16_rn(sum);
+    const float4 x = __ldg(reinterpret_cast<const float4*>(p)), y = __ldg(reinterpret_cast<const float4*>(p) + 1);
+    v[0] += x.x, v[1] += x.y, v[2] += x.z, v[3] += x.w, v[4] += y.x, v[5] += y.y, v[6] += y.z, v[7] += y.w;
+}
+__device__ __forceinline__ void put8(uint16_t* out, const float (&v)[8], bool whole)
+{
+    const uint4 w = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+    if (whole) *reinterpret_cast<uint4*>(out) = w;
+    else {
+        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int q = 0; q < 8; ++q) out[q] = (uint16_t)(u[q / 2] >> (16 * (q & 1)));
     }
 }
 
-__global__ void __launch_bounds__(256) dw_join_kernel(const RouteLossArgs a, const RouteGradArgs b, const SweepArgs p, const Space s)
+// dx: the partial sums, and the picked entries' rows
+__global__ void __launch_bounds__(256) dx_join_kernel(const RouteLossArgs a, const RouteGradArgs b, const SweepArgs p, const float* __restrict__ ds)
 {
-    const int64_t total = a.G * a.m * a.d;
-    for (int64_t e = blockIdx.x * (int64_t)256 + threadIdx.x; e < total; e += (int64_t)gridDim.x * 256) {
-        float sum = s.sum[e];
-        for (int z = 0; z < p.splits; ++z) sum += p.part[z * total + e];
-        ((__nv_bfloat16*)b.dW)[e] = __float2bfloat16_rn(sum);
-        if (b.dbias && e % a.d == 0) {
-            const int64_t row = e / a.d, g = row / a.m;
-            float db = s.wsum[row];
-            for (int z = 0; z < p.splits; ++z) db += p.part2[((int64_t)z * a.G + g) * p.mp + (row - g * a.m)];
-            b.dbias[row] = db;
+    const int64_t e = (blockIdx.x * (int64_t)256 + threadIdx.x) * 8, total = a.n * a.d;
+    if (e >= total) return;
+    const int64_t i = e / a.d;
+    const int c = (int)(e - i * a.d);
+    float v[8] = {};
+#pragma unroll 4
+    for (int z = 0; z < p.splits; ++z) add8(v, p.part + z * total + e);
+#pragma unroll 4
+    for (int g = 0; g < a.G; ++g) {
+        const int32_t k = __ldg(a.idx + i * a.G + g);
+        if (k < 0 || k >= a.m) continue;
+        const float f = __ldg(ds + i * a.G + g);
+        const uint4 w = __ldg(reinterpret_cast<const uint4*>((const uint16_t*)a.W + ((int64_t)g * a.m + k) * a.d + c));
+        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            v[2 * q] = fmaf(f, __uint_as_float(u[q] << 16), v[2 * q]);
+            v[2 * q + 1] = fmaf(f, __uint_as_float(u[q] & 0xffff0000u), v[2 * q + 1]);
         }
     }
+    put8((uint16_t*)b.dx + e, v, ((uintptr_t)b.dx & 15) == 0);
+}
+
+// dW and db: the partial sums, and the sums over the positions that picked the entry
+__global__ void __launch_bounds__(256) dw_join_kernel(const RouteLossArgs a, const RouteGradArgs b, const SweepArgs p, const Space s)
+{
+    const int64_t e = (blockIdx.x * (int64_t)256 + threadIdx.x) * 8, total = a.G * a.m * a.d;
+    if (e >= total) return;
+    float v[8] = {};
+    add8(v, s.sum + e);
+#pragma unroll 4
+    for (int z = 0; z < p.splits; ++z) add8(v, p.part + z * total + e);
+    put8((uint16_t*)b.dW + e, v, ((uintptr_t)b.dW & 15) == 0);
+    if (b.dbias && e % a.d == 0) {
+        const int64_t row = e / a.d, g = row / a.m;
+        float db = s.wsum[row];
+        for (int z = 0; z < p.splits; ++z) db += p.part2[((int64_t)z * a.G + g) * p.mp + (row - g * a.m)];
+        b.dbias[row] = db;
+    }
+}
+
+template <bool GRAD>
+cudaError_t launch_positions(const RouteLossArgs& a, const RouteGradArgs& b, const Space& s, int64_t rows, int64_t np, cudaStream_t st)
+{
+    const bool whole = ((uintptr_t)a.x & 15) == 0;
+    return launch_kernel(Launch{st, nullptr, nullptr},
+                         a.d == 32 ? positions_kernel<32, GRAD> : a.d == 64 ? positions_kernel<64, GRAD> : positions_kernel<128, GRAD>,
+                         dim3((unsigned)((rows * (a.d / 8) + 255) / 256)), 256, 0, 1, a, b, s, np, whole);
 }
 
 SweepArgs pass_args(const RouteLossArgs& a, const Space& s)
@@ -290,13 +365,13 @@ cudaError_t launch_route_loss(const RouteLossArgs& a, void* ws, cudaStream_t st)
     const Space s = layout(ws, a.n, a.G, a.d, a.m, false);
     SweepArgs p = pass_args(a, s);
     const Launch l{st, nullptr, nullptr};
-    const unsigned blocks = (unsigned)((a.n + kPrepRows - 1) / kPrepRows), G = (unsigned)a.G;
-    TRY(launch_kernel(l, entries_kernel, dim3((unsigned)((p.mp + 255) / 256), G), 256, 0, 1, a.bias, nullptr, nullptr, 0.f, a.m, p.mp, s.b2, nullptr));
-    if (a.n) TRY(launch_kernel(l, positions_kernel, dim3(blocks), kPrepRows, 0, 1, a, RouteGradArgs{}, s, false));
+    const unsigned blocks = (unsigned)((p.np + 255) / 256), G = (unsigned)a.G;
+    TRY(launch_kernel(l, entries_kernel, dim3((unsigned)((p.mp + 255) / 256), G), 256, 0, 1, a.bias, nullptr, nullptr, 0.f, a.m, p.mp, s.b2, nullptr, s.done));
+    if (a.n) TRY(launch_positions<false>(a, RouteGradArgs{}, s, a.n, p.np, st));
     TRY(launch_sweep(SWEEP_LSE, a.d, p, st));
-    if (a.n) TRY(launch_kernel(l, lse_join_kernel, dim3((unsigned)((p.np + 255) / 256), G), 256, 0, 1, a, p, s.nl2, s.live_part));
+    if (a.n) TRY(launch_kernel(l, lse_join_kernel, dim3(blocks, G), 256, 0, 1, a, p, s));
     TRY(launch_sweep(SWEEP_MEAN, a.d, p, st));
-    return launch_kernel(l, mean_join_kernel, dim3(G), 1024, 0, 1, a, p, s, (int)blocks, (int)((p.np + 255) / 256));
+    return launch_kernel(l, mean_join_kernel, dim3((unsigned)((a.m + kMeanEntries - 1) / kMeanEntries), G), 256, 0, 1, a, p, s, (int)blocks);
 }
 
 cudaError_t launch_route_grad(const RouteLossArgs& a, const RouteGradArgs& b, void* ws, cudaStream_t st)
@@ -305,8 +380,8 @@ cudaError_t launch_route_grad(const RouteLossArgs& a, const RouteGradArgs& b, vo
     SweepArgs p = pass_args(a, s);
     const Launch l{st, nullptr, nullptr};
     const unsigned G = (unsigned)a.G;
-    TRY(launch_kernel(l, entries_kernel, dim3((unsigned)((p.mp + 255) / 256), G), 256, 0, 1, a.bias, a.mean, b.offset, b.w_balance, a.m, p.mp, s.b2, s.h));
-    if (a.n) TRY(launch_kernel(l, positions_kernel, dim3((unsigned)((p.np + kPrepRows - 1) / kPrepRows)), kPrepRows, 0, 1, a, b, s, true));
+    TRY(launch_kernel(l, entries_kernel, dim3((unsigned)((p.mp + 255) / 256), G), 256, 0, 1, a.bias, a.mean, b.offset, b.w_balance, a.m, p.mp, s.b2, s.h, nullptr));
+    if (a.n) TRY(launch_positions<true>(a, b, s, p.np, p.np, st));
     SegmentArgs seg{};
     seg.order = b.order;
     seg.offset = b.offset;
@@ -323,9 +398,9 @@ cudaError_t launch_route_grad(const RouteLossArgs& a, const RouteGradArgs& b, vo
     TRY(launch_sweep(SWEEP_R, a.d, p, st));
     if (a.n) TRY(launch_kernel(l, r_join_kernel, dim3((unsigned)((p.np + 255) / 256), G), 256, 0, 1, p, s.r));
     TRY(launch_sweep(SWEEP_DX, a.d, p, st));
-    if (a.n) TRY(launch_kernel(l, dx_join_kernel, dim3((unsigned)std::min<int64_t>((a.n * a.d + 255) / 256, 148 * 16)), 256, 0, 1, a, b, p, s.ds));
+    if (a.n) TRY(launch_kernel(l, dx_join_kernel, dim3((unsigned)((a.n * a.d / 8 + 255) / 256)), 256, 0, 1, a, b, p, s.ds));
     TRY(launch_sweep(SWEEP_DW, a.d, p, st));
-    return launch_kernel(l, dw_join_kernel, dim3((unsigned)std::min<int64_t>((a.G * a.m * a.d + 255) / 256, 148 * 16)), 256, 0, 1, a, b, p, s);
+    return launch_kernel(l, dw_join_kernel, dim3((unsigned)((a.G * a.m * a.d / 8 + 255) / 256)), 256, 0, 1, a, b, p, s);
 }
 
 }  // namespace ckv

@@ -3,10 +3,10 @@
 //   order[g]  = positions i by (key(i), i), key = idx[i][g] if it lies in [0, m), else m (no entry: behind all others)
 //   offset[g][j] = number of positions of the group with a key below j, j = 0..m
 //
-// The positions are cut into chunks.  A chunk counts its keys in shared memory (one word per key: `table[g][chunk][key]`),
-// the counts are added up over the chunks of a group and over the keys, and every chunk then places its positions in their order,
-// so that equal keys keep it and the result does not depend on how blocks are scheduled.  Keys of more than kDigitBits
-// bits are sorted digit by digit, the low ones first.
+// Up to kBlockSort positions a block sorts a group in shared memory.  More are cut into chunks: a chunk counts its keys in shared memory (one
+// word per key: `table[g][chunk][key]`), the counts are added up over the chunks of a group and over the keys, and a warp
+// per chunk then places its positions in their order, so that equal keys keep it and the result does not depend on how
+// blocks are scheduled.  Keys of more than kDigitBits bits are sorted digit by digit, the low ones first.
 #include <algorithm>
 
 #include "fit.h"
@@ -15,110 +15,200 @@
 namespace ckv {
 namespace {
 
-constexpr int kDigitBits = 15;
+constexpr int kDigitBits = 15, kBlockSort = 8192, kBlockThreads = 512;
+constexpr int kAhead = 8;  // batches of 32 positions whose keys a placing warp has on their way
+
+__device__ __forceinline__ uint32_t key_of(int32_t v, int64_t m) { return v >= 0 && v < m ? (uint32_t)v : (uint32_t)m; }
 
 // A pass over the keys: from the indices (first pass) or from the pass before.
 struct Pass {
     const int32_t* idx;    // [n][G], or null
-    const uint32_t* key;   // [G][n] keys and the positions they belong to, of the pass before
+    uint32_t* key;         // [G][n] keys (the first pass writes them) and the positions they belong to (null: 0, 1, ...)
     const int32_t* val;
     uint32_t* key_out;     // [G][n], or null: nothing reads them any more
     int32_t* val_out;
     int64_t n, m, chunk;
-    int G, chunks, bins, shift;
+    int G, chunks, bins, stride, shift;  // stride: of a row of the table, a multiple of four
 };
-__device__ __forceinline__ uint32_t key_at(const Pass& p, int g, int64_t i)
-{
-    if (!p.idx) return __ldg(p.key + (int64_t)g * p.n + i);
-    const int32_t v = __ldg(p.idx + i * p.G + g);
-    return v >= 0 && v < p.m ? (uint32_t)v : (uint32_t)p.m;
-}
-__device__ __forceinline__ int digit_of(const Pass& p, uint32_t key) { return (int)((key >> p.shift) & (uint32_t)((1 << kDigitBits) - 1)); }
+__device__ __forceinline__ int digit_of(uint32_t key, int shift) { return (int)((key >> shift) & (uint32_t)((1 << kDigitBits) - 1)); }
 
 __global__ void __launch_bounds__(256) count_kernel(const Pass p, int32_t* __restrict__ table)
 {
     extern __shared__ int32_t bins[];
     const int g = blockIdx.y;
-    for (int j = threadIdx.x; j < p.bins; j += 256) bins[j] = 0;
+    for (int j = threadIdx.x; j < p.stride; j += 256) bins[j] = 0;
     __syncthreads();
     const int64_t begin = blockIdx.x * p.chunk, end = min(begin + p.chunk, p.n);
-    for (int64_t i = begin + threadIdx.x; i < end; i += 256) atomicAdd(bins + digit_of(p, key_at(p, g, i)), 1);
+    uint32_t* keys = p.key + (int64_t)g * p.n;
+#pragma unroll 8
+    for (int64_t i = begin + threadIdx.x; i < end; i += 256) {
+        uint32_t k;
+        if (p.idx) keys[i] = k = key_of(__ldg(p.idx + i * p.G + g), p.m);
+        else k = keys[i];
+        atomicAdd(bins + digit_of(k, p.shift), 1);
+    }
     __syncthreads();
-    int32_t* t = table + ((int64_t)g * p.chunks + blockIdx.x) * p.bins;
-    for (int j = threadIdx.x; j < p.bins; j += 256) t[j] = bins[j];
+    int32_t* t = table + ((int64_t)g * p.chunks + blockIdx.x) * p.stride;
+    for (int j = threadIdx.x; j < p.stride; j += 256) t[j] = bins[j];
 }
+
+__device__ __forceinline__ int4 operator+(int4 a, int4 b) { return make_int4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w); }
 
 // table[g][c][j] becomes the count of the chunks before c, total[g][j] that of all
-__global__ void __launch_bounds__(256) chunk_scan_kernel(int32_t* __restrict__ table, int32_t* __restrict__ total, int chunks, int bins)
+__global__ void __launch_bounds__(64) chunk_scan_kernel(int32_t* __restrict__ table, int32_t* __restrict__ total, int chunks, int stride)
 {
-    const int j = blockIdx.x * 256 + threadIdx.x, g = blockIdx.y;
-    if (j >= bins) return;
-    int32_t* t = table + (int64_t)g * chunks * bins + j;
-    int32_t sum = 0;
-    for (int c = 0; c < chunks; ++c, t += bins) {
-        const int32_t v = *t;
-        *t = sum;
-        sum += v;
+    const int j = (blockIdx.x * 64 + threadIdx.x) * 4, g = blockIdx.y;
+    if (j >= stride) return;
+    int32_t* t = table + (int64_t)g * chunks * stride + j;
+    int4 sum = make_int4(0, 0, 0, 0);
+    for (int c0 = 0; c0 < chunks; c0 += 8) {
+        int4 v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = c0 + k < chunks ? *reinterpret_cast<int4*>(t + (int64_t)(c0 + k) * stride) : make_int4(0, 0, 0, 0);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            if (c0 + k < chunks) *reinterpret_cast<int4*>(t + (int64_t)(c0 + k) * stride) = sum;
+            sum = sum + v[k];
+        }
     }
-    total[(int64_t)g * bins + j] = sum;
+    *reinterpret_cast<int4*>(total + (int64_t)g * stride + j) = sum;
 }
 
-// exclusive prefix sums of a group's totals, in place; copied to offset (whose rows have as many entries) if given
-__global__ void __launch_bounds__(1024) bin_scan_kernel(int32_t* __restrict__ total, int32_t* __restrict__ offset, int bins)
+// Exclusive prefix sum over a block's threads of one number each; *all: the sum of all.
+template <int THREADS>
+__device__ __forceinline__ int32_t block_prefix(int32_t v, int32_t* all)
 {
-    __shared__ int32_t warp_sum[32];
-    const int g = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int32_t* t = total + (int64_t)g * bins;
-    int32_t carry = 0;
-    for (int j0 = 0; j0 < bins; j0 += 1024) {
-        const int j = j0 + threadIdx.x;
-        const int32_t v = j < bins ? t[j] : 0;
-        int32_t s = v;
+    __shared__ int32_t warp_sum[THREADS / 32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int32_t s = v;
 #pragma unroll
-        for (int d = 1; d < 32; d *= 2) {
-            const int32_t o = __shfl_up_sync(0xffffffffu, s, d);
-            if (lane >= d) s += o;
-        }
-        if (lane == 31) warp_sum[warp] = s;
-        __syncthreads();
-        int32_t before = 0, all = 0;
-        for (int w = 0; w < 32; ++w) {
-            if (w < warp) before += warp_sum[w];
-            all += warp_sum[w];
-        }
-        __syncthreads();
-        if (j < bins) {
-            t[j] = carry + before + s - v;
-            if (offset) offset[(int64_t)g * bins + j] = t[j];
-        }
+    for (int d = 1; d < 32; d *= 2) {
+        const int32_t o = __shfl_up_sync(0xffffffffu, s, d);
+        if (lane >= d) s += o;
+    }
+    __syncthreads();
+    if (lane == 31) warp_sum[warp] = s;
+    __syncthreads();
+    int32_t w = lane < THREADS / 32 ? warp_sum[lane] : 0;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+        const int32_t o = __shfl_up_sync(0xffffffffu, w, d);
+        if (lane >= d) w += o;
+    }
+    *all = __shfl_sync(0xffffffffu, w, 31);
+    const int32_t before = __shfl_sync(0xffffffffu, w, (warp + 31) & 31);
+    return s - v + (warp ? before : 0);
+}
+
+// exclusive prefix sums of a group's totals, in place; copied to offset (rows of `bins`) if given
+__global__ void __launch_bounds__(1024) bin_scan_kernel(int32_t* __restrict__ total, int32_t* __restrict__ offset, int bins, int stride)
+{
+    const int g = blockIdx.x;
+    int32_t* t = total + (int64_t)g * stride;
+    int32_t carry = 0;
+    for (int j0 = 0; j0 < bins; j0 += 4096) {
+        const int j = j0 + threadIdx.x * 4;
+        const int4 v = j < stride ? *reinterpret_cast<int4*>(t + j) : make_int4(0, 0, 0, 0);
+        int32_t all;
+        int32_t at = carry + block_prefix<1024>(v.x + v.y + v.z + v.w, &all);
+        const int32_t o[4] = {at, at + v.x, at + v.x + v.y, at + v.x + v.y + v.z};
+        if (j < stride) *reinterpret_cast<int4*>(t + j) = make_int4(o[0], o[1], o[2], o[3]);
+        if (offset)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                if (j + q < bins) offset[(int64_t)g * bins + j + q] = o[q];
         carry += all;
     }
 }
 
-// One warp per chunk: 32 positions at a time, the lanes with equal keys in the order of their positions.
-__global__ void __launch_bounds__(32) place_kernel(const Pass p, const int32_t* __restrict__ table, const int32_t* __restrict__ base)
+// One warp's turn with 32 positions: the place of each, next[] moved on.  Lanes with equal keys stay in order; the additions of successive
+// turns are made in order as well, so that a turn need not wait for the one before.
+__device__ __forceinline__ int32_t take_places(int32_t* next, int d)  // d < 0: none
+{
+    const int lane = threadIdx.x & 31;
+    const unsigned same = __match_any_sync(0xffffffffu, d);
+    const int leader = __ffs(same) - 1;
+    int32_t at = 0;
+    if (d >= 0 && lane == leader) at = atomicAdd(next + d, __popc(same));
+    return __shfl_sync(0xffffffffu, at, leader) + __popc(same & ((1u << lane) - 1));
+}
+
+__global__ void __launch_bounds__(128) place_kernel(const Pass p, const int32_t* __restrict__ table, const int32_t* __restrict__ base)
 {
     extern __shared__ int32_t next[];
-    const int g = blockIdx.y, lane = threadIdx.x;
-    const int32_t *t = table + ((int64_t)g * p.chunks + blockIdx.x) * p.bins, *b = base + (int64_t)g * p.bins;
-    for (int j = lane; j < p.bins; j += 32) next[j] = t[j] + b[j];
-    __syncwarp();
-    const int64_t begin = blockIdx.x * p.chunk, end = min(begin + p.chunk, p.n);
-    for (int64_t i0 = begin; i0 < end; i0 += 32) {
-        const int64_t i = i0 + lane;
-        const bool real = i < end;
-        const uint32_t key = real ? key_at(p, g, i) : 0;
-        const int d = real ? digit_of(p, key) : -1;
-        const unsigned same = __match_any_sync(0xffffffffu, d);
-        const int leader = __ffs(same) - 1;
-        int32_t at = 0;
-        if (real && lane == leader) at = atomicAdd(next + d, __popc(same));
-        at = __shfl_sync(0xffffffffu, at, leader) + __popc(same & ((1u << lane) - 1));
-        if (real) {
-            const int64_t o = (int64_t)g * p.n + at;
-            p.val_out[o] = p.val ? p.val[(int64_t)g * p.n + i] : (int32_t)i;
-            if (p.key_out) p.key_out[o] = key;
+    const int g = blockIdx.y, lane = threadIdx.x & 31;
+    const int32_t *t = table + ((int64_t)g * p.chunks + blockIdx.x) * p.stride, *b = base + (int64_t)g * p.stride;
+#pragma unroll 4
+    for (int j = threadIdx.x * 4; j < p.stride; j += 512)
+        *reinterpret_cast<int4*>(next + j) = __ldg(reinterpret_cast<const int4*>(t + j)) + __ldg(reinterpret_cast<const int4*>(b + j));
+    __syncthreads();
+    if (threadIdx.x >= 32) return;
+    const int64_t begin = blockIdx.x * p.chunk, end = min(begin + p.chunk, p.n), row = (int64_t)g * p.n;
+    uint32_t key[kAhead];
+    int32_t val[kAhead];
+    auto fetch = [&](int64_t i0) {
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int64_t i = i0 + 32 * k + lane;
+            key[k] = i < end ? __ldg(p.key + row + i) : 0xffffffffu;
+            val[k] = !p.val ? (int32_t)i : i < end ? __ldg(p.val + row + i) : 0;
         }
+    };
+    fetch(begin);
+    for (int64_t i0 = begin; i0 < end; i0 += 32 * kAhead) {
+        uint32_t k_now[kAhead];
+        int32_t v_now[kAhead], at[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            k_now[k] = key[k];
+            v_now[k] = val[k];
+        }
+        fetch(i0 + 32 * kAhead);
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) at[k] = take_places(next, i0 + 32 * k + lane < end ? digit_of(k_now[k], p.shift) : -1);
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            if (i0 + 32 * k + lane >= end) continue;
+            p.val_out[row + at[k]] = v_now[k];
+            if (p.key_out) p.key_out[row + at[k]] = k_now[k];
+        }
+    }
+}
+
+// The whole sort of a group by one block.
+__global__ void __launch_bounds__(kBlockThreads) block_sort_kernel(int n, int G, int64_t m, const int32_t* __restrict__ idx,
+                                                                   int32_t* __restrict__ order, int32_t* __restrict__ offset)
+{
+    extern __shared__ int32_t next[];
+    const int g = blockIdx.x, tid = threadIdx.x, lane = tid & 31, bins = (int)m + 1;
+    uint16_t* keys = reinterpret_cast<uint16_t*>(next + ((bins + 3) & ~3));
+    for (int j = tid; j < bins; j += kBlockThreads) next[j] = 0;
+    __syncthreads();
+#pragma unroll 4
+    for (int i = tid; i < n; i += kBlockThreads) {
+        const int k = (int)key_of(__ldg(idx + (int64_t)i * G + g), m);
+        keys[i] = (uint16_t)k;
+        atomicAdd(next + k, 1);
+    }
+    __syncthreads();
+    int32_t carry = 0;
+    for (int j0 = 0; j0 < bins; j0 += kBlockThreads) {
+        const int j = j0 + tid;
+        int32_t all;
+        const int32_t at = carry + block_prefix<kBlockThreads>(j < bins ? next[j] : 0, &all);
+        if (j < bins) {
+            next[j] = at;
+            offset[(int64_t)g * bins + j] = at;
+        }
+        carry += all;
+    }
+    __syncthreads();
+    if (tid >= 32) return;
+#pragma unroll 4
+    for (int i0 = 0; i0 < n; i0 += 32) {
+        const int i = i0 + lane;
+        const int32_t at = take_places(next, i < n ? keys[i] : -1);
+        if (i < n) order[(int64_t)g * n + at] = i;
     }
 }
 
@@ -145,30 +235,32 @@ int bits_of(int64_t m)  // of the largest key, m
 }
 int passes_of(int64_t m) { return (bits_of(m) + kDigitBits - 1) / kDigitBits; }
 int bins_of(int64_t m) { return passes_of(m) == 1 ? (int)m + 1 : 1 << kDigitBits; }
+int stride_of(int64_t m) { return (bins_of(m) + 3) & ~3; }
+bool by_block(int64_t n, int64_t m) { return n <= kBlockSort && passes_of(m) == 1; }
+// Chunks: some 1200 of them in all, but no shorter than half a row of counts, which every chunk writes, adds up and reads.
 int64_t chunk_of(int64_t n, int G, int64_t m)
 {
     int64_t c = 1024;
-    while (c * 592 < n * G || 2 * c < bins_of(m)) c *= 2;
+    while (c * 1184 < n * G || 2 * c < bins_of(m)) c *= 2;
     return c;
 }
 
 struct SortSpace {
-    int32_t *table, *total, *val[2];
-    uint32_t* key[2];
-    int64_t bytes;
+    int32_t *table = nullptr, *total = nullptr, *val[2] = {};
+    uint32_t* key[2] = {};
+    int64_t bytes = 0;
     SortSpace(void* ws, int64_t n, int G, int64_t m)
     {
+        if (by_block(n, m)) return;
         Carve c(ws);
         const int64_t chunks = (n + chunk_of(n, G, m) - 1) / chunk_of(n, G, m);
-        table = c.take<int32_t>(chunks * G * bins_of(m));
-        total = c.take<int32_t>((int64_t)G * bins_of(m));
-        val[0] = val[1] = nullptr;
-        key[0] = key[1] = nullptr;
-        if (passes_of(m) > 1)
-            for (int i = 0; i < 2; ++i) {
-                key[i] = c.take<uint32_t>(n * G);
-                val[i] = c.take<int32_t>(n * G);
-            }
+        table = c.take<int32_t>(chunks * G * stride_of(m));
+        total = c.take<int32_t>((int64_t)G * stride_of(m));
+        key[0] = c.take<uint32_t>(n * G);
+        if (passes_of(m) > 1) {
+            key[1] = c.take<uint32_t>(n * G);
+            for (int i = 0; i < 2; ++i) val[i] = c.take<int32_t>(n * G);
+        }
         bytes = c.used;
     }
 };
@@ -180,35 +272,39 @@ int64_t sort_workspace(int64_t n, int G, int64_t m) { return SortSpace(nullptr, 
 cudaError_t launch_sort_indices(int64_t n, int G, int64_t m, const int32_t* idx, int32_t* order, int32_t* offset, void* ws,
                                 cudaStream_t s)
 {
-    const SortSpace sp(ws, n, G, m);
-    const int passes = passes_of(m), bins = bins_of(m);
     const Launch l{s, nullptr, nullptr};
+    if (by_block(n, m))
+        return launch_kernel(l, block_sort_kernel, dim3((unsigned)G), kBlockThreads, stride_of(m) * 4 + (n + 1) / 2 * 4, 1, (int)n, G, m, idx, order, offset);
+    const SortSpace sp(ws, n, G, m);
+    const int passes = passes_of(m);
     Pass p{};
     p.n = n;
     p.m = m;
     p.G = G;
     p.chunk = chunk_of(n, G, m);
     p.chunks = (int)((n + p.chunk - 1) / p.chunk);
-    p.bins = bins;
+    p.bins = bins_of(m);
+    p.stride = stride_of(m);
+    const dim3 grid((unsigned)p.chunks, (unsigned)G);
+    // pass i reads keys i & 1 (the first writes them beforehand) and leaves the other ones
     for (int i = 0; i < passes; ++i) {
+        const bool last = i + 1 == passes;
         p.shift = i * kDigitBits;
         p.idx = i == 0 ? idx : nullptr;
-        p.key = i == 0 ? nullptr : sp.key[(i - 1) & 1];
-        p.val = i == 0 ? nullptr : sp.val[(i - 1) & 1];
-        p.key_out = passes == 1 ? nullptr : sp.key[i & 1];
-        p.val_out = i + 1 == passes ? order : sp.val[i & 1];
-        const dim3 grid((unsigned)p.chunks, (unsigned)G);
-        cudaError_t e = p.chunks ? launch_kernel(l, count_kernel, grid, 256, bins * 4, 1, p, sp.table) : cudaSuccess;
+        p.key = sp.key[i & 1];
+        p.val = i == 0 ? nullptr : sp.val[i & 1];
+        p.key_out = passes == 1 ? nullptr : sp.key[(i + 1) & 1];
+        p.val_out = last ? order : sp.val[(i + 1) & 1];
+        cudaError_t e = p.chunks ? launch_kernel(l, count_kernel, grid, 256, p.stride * 4, 1, p, sp.table) : cudaSuccess;
         if (e == cudaSuccess)
-            e = launch_kernel(l, chunk_scan_kernel, dim3((bins + 255) / 256, (unsigned)G), 256, 0, 1, sp.table, sp.total, p.chunks, bins);
+            e = launch_kernel(l, chunk_scan_kernel, dim3((p.stride + 255) / 256, (unsigned)G), 64, 0, 1, sp.table, sp.total, p.chunks, p.stride);
         if (e == cudaSuccess)
-            e = launch_kernel(l, bin_scan_kernel, dim3((unsigned)G), 1024, 0, 1, sp.total, passes == 1 ? offset : nullptr, bins);
-        if (e == cudaSuccess && p.chunks) e = launch_kernel(l, place_kernel, grid, 32, bins * 4, 1, p, sp.table, sp.total);
+            e = launch_kernel(l, bin_scan_kernel, dim3((unsigned)G), 1024, 0, 1, sp.total, passes == 1 ? offset : nullptr, p.bins, p.stride);
+        if (e == cudaSuccess && p.chunks) e = launch_kernel(l, place_kernel, grid, 128, p.stride * 4, 1, p, sp.table, sp.total);
         if (e != cudaSuccess) return e;
     }
     if (passes > 1)
-        return launch_kernel(l, bounds_kernel, dim3((unsigned)((m + 256) / 256), (unsigned)G), 256, 0, 1, sp.key[(passes - 1) & 1],
-                             offset, n, m);
+        return launch_kernel(l, bounds_kernel, dim3((unsigned)((m + 256) / 256), (unsigned)G), 256, 0, 1, sp.key[passes & 1], offset, n, m);
     return cudaSuccess;
 }
 

@@ -269,6 +269,54 @@ def test_gpu_route_loss_of_padding_and_excluded_entries():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("d", [32, 128])
+def test_gpu_router_inputs_and_gradients_off_the_16_byte_boundary(d):
+    import torch
+    import paper_2601_19178_b200 as ckv
+    n, m, G = 77, 90, 2
+    x, W, b, idx = [_dev(t) for t in _router(9, n, m, G, d)]
+
+    def moved(t):                                       # the same values, two bytes further on
+        flat = torch.zeros(t.numel() + 8, dtype=t.dtype, device="cuda")[1:t.numel() + 1]
+        return flat.view(t.shape).copy_(t)
+
+    want = ckv.route_loss(x, W, b, idx)
+    got = ckv.route_loss(moved(x), W, b, idx)
+    assert all(torch.equal(a, c) for a, c in zip(want, got))
+    order = ckv.sort_indices(idx, m)
+    want_grad = ckv.route_loss_grad(x, W, b, idx, order, *want[1:], 1.0, 0.1)
+    dx, dW, dbias = moved(x), moved(W), torch.empty((G, m), device="cuda")
+    need = ckv.ckv_route_loss_bytes(n, G, d, m)[1]
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    ckv.ckv_route_loss_grad(0, n, G, d, m, moved(x), W, b, idx, *order, *want[1:], 1.0, 0.1, None, dx, dW, dbias, ws, need)
+    assert all(torch.equal(a, c) for a, c in zip(want_grad, (dx, dW, dbias)))
+
+
+@pytest.mark.gpu
+def test_gpu_gather_off_the_word_boundary():
+    """bf16 arrays on odd multiples of two bytes."""
+    import torch
+    import paper_2601_19178_b200 as ckv
+    pool, idx, user, score, d_out = [_dev(t) for t in _gather_case(2, "bf16", 333, 2, 40, 32, 2, True)]
+
+    def moved(t):
+        return torch.zeros(t.numel() + 8, dtype=t.dtype, device="cuda")[1:t.numel() + 1].view(t.shape).copy_(t)
+
+    want = ckv.gather(pool, idx, user, score)
+    for p, u in ((moved(pool), user), (pool, moved(user)), (moved(pool), moved(user))):
+        assert torch.equal(ckv.gather(p, idx, u, score), want)
+        out = moved(torch.zeros_like(want))
+        ckv.ckv_gather(0, ckv.CKV_BF16, 333, 2, 32, 30, 40, p, idx, u, score, out)
+        assert torch.equal(out, want)
+    order = ckv.sort_indices(idx, 40)
+    want = ckv.gather_grad(pool, order, score, d_out)
+    assert all(torch.equal(a, c) for a, c in zip(ckv.gather_grad(moved(pool), order, score, d_out), want))
+    with pytest.raises(ckv.CkvError) as e:
+        ckv.gather_grad(pool, order, score, moved(d_out))
+    assert e.value.status == ckv.CKV_ERR_INVALID_ARG
+
+
+@pytest.mark.gpu
 def test_gpu_route_loss_without_positions():
     import torch
     import paper_2601_19178_b200 as ckv
