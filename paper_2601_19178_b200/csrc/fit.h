@@ -59,11 +59,25 @@ struct SweepArgs {
     int64_t n, m, np, mp;           // positions, entries; both padded
     int G, splits;
     const uint16_t *x, *W;          // [n][d], [G][m][d]
-    const float *b2, *h;            // [G][mp] bias log2(e) (-inf behind the last entry); h
-    const float *nl2, *r;           // [G][np] -lse log2(e) (-inf: no weight); r
+    const float *b, *h;             // [G][mp] bias (-inf behind the last entry); h
+    const float *nl, *nr;           // [G][np] -lse (-inf: no weight); -r
+    const uint16_t *b_step, *nl_step;  // b and nl as operands of a product, see put_step
     float* part;    // LSE: float2 (maximum, sum) [splits][G][np]; MEAN [splits][G][mp]; R [splits][G][np]; DX [splits][n][d]; DW [splits][G][m][d]
     float* part2;   // DW: sums of T [splits][G][mp]
 };
+#ifdef __CUDACC__
+// A number as three bf16 parts whose sum it is (16 elements per row: 8 rows of 16 bytes, of which the first six hold the parts, then
+// the rows' zero halves), as a K-major operand without swizzle wants it.
+__device__ __forceinline__ void put_step(uint16_t* step, int64_t row, float v)
+{
+    const uint32_t hi = (__float_as_uint(v) & 0xffff0000u) | (v != v ? 0x400000u : 0u);  // (a NaN whose upper half alone would be an infinity)
+    const float r1 = isfinite(v) ? v - __uint_as_float(hi) : 0.f;
+    const uint32_t mid = __float_as_uint(r1) & 0xffff0000u, lo = __float_as_uint(r1 - __uint_as_float(mid));
+    uint4* const to = reinterpret_cast<uint4*>(step) + (row >> 3) * 16 + (row & 7);
+    to[0] = make_uint4((hi >> 16) | mid, lo >> 16, 0, 0);
+    to[8] = make_uint4(0, 0, 0, 0);
+}
+#endif
 int sweep_splits(int64_t n, int G, int d, int64_t m, int mode);
 cudaError_t launch_sweep(int mode, int d, SweepArgs& a, cudaStream_t s);  // sets a.splits
 

@@ -25,15 +25,15 @@
 namespace ckv {
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 __device__ __forceinline__ float sigmoid(float x) { return 1.f / (1.f + expf(-x)); }
 
 struct Space {
-    // by entry, [G][mp]: bias log2(e), -inf behind the last; h
-    float *b2, *h;
-    // by position, [G][np]: -lse log2(e), -inf for a position that takes no part; r
-    float *nl2, *r;
+    // by entry, [G][mp]: bias, -inf behind the last; h
+    float *b, *h;
+    // by position, [G][np]: -lse, -inf for a position that takes no part; -r
+    float *nl, *nr;
+    uint16_t *b_step, *nl_step;  // b and nl as operands of a product
     uint16_t* xs;        // x with zeros for a position that takes part in no group
     float* part;         // partial results of a pass
     float* part2;
@@ -53,8 +53,10 @@ Space layout(void* ws, int64_t n, int G, int d, int64_t m, bool grad)
     Carve c(ws);
     Space s{};
     const int64_t np = sweep_padded(n), mp = sweep_padded(m), blocks = (np + 255) / 256;
-    s.b2 = c.take<float>(G * mp);
-    s.nl2 = c.take<float>(G * np);
+    s.b = c.take<float>(G * mp);
+    s.nl = c.take<float>(G * np);
+    s.b_step = c.take<uint16_t>(G * mp * 16);
+    s.nl_step = c.take<uint16_t>(G * np * 16);
     s.xs = c.take<uint16_t>(n * d);
     if (!grad) {
         s.rows_part = c.take<int32_t>(blocks * G);
@@ -65,7 +67,7 @@ Space layout(void* ws, int64_t n, int G, int d, int64_t m, bool grad)
         s.part = c.take<float>(std::max(2 * sweep_splits(n, G, d, m, SWEEP_LSE) * G * np, sweep_splits(n, G, d, m, SWEEP_MEAN) * G * mp));
     } else {
         s.h = c.take<float>(G * mp);
-        s.r = c.take<float>(G * np);
+        s.nr = c.take<float>(G * np);
         s.ds = c.take<float>(n * G);
         s.sum = c.take<float>(G * m * d);
         s.wsum = c.take<float>(G * m);
@@ -80,18 +82,20 @@ Space layout(void* ws, int64_t n, int G, int d, int64_t m, bool grad)
 // ---- what the passes read
 __global__ void __launch_bounds__(256) entries_kernel(const float* __restrict__ bias, const float* __restrict__ mean,
                                                       const int32_t* __restrict__ offset, float w_balance, int64_t m, int64_t mp,
-                                                      float* __restrict__ b2, float* __restrict__ h, unsigned* __restrict__ done)
+                                                      const Space s)
 {
     const int64_t j = blockIdx.x * (int64_t)256 + threadIdx.x;
     const int g = blockIdx.y;
-    if (j == 0 && done) done[g] = 0;
+    if (j == 0 && s.done) s.done[g] = 0;
     if (j >= mp) return;
-    b2[g * mp + j] = j < m ? (bias ? bias[g * m + j] * kLog2e : 0.f) : -CUDART_INF_F;
-    if (!h) return;
+    const float b = j < m ? (bias ? bias[g * m + j] : 0.f) : -CUDART_INF_F;
+    s.b[g * mp + j] = b;
+    put_step(s.b_step, g * mp + j, b);
+    if (!s.h) return;
     const float u = j < m ? mean[g * m + j] * (float)m : 0.f;
     const int32_t rows = offset[g * (m + 1) + m];
     // (an entry that no position gives any weight has p = 0 everywhere, and no gradient)
-    h[g * mp + j] = u > 0.f ? w_balance / (float)max(rows, 1) * logf(u) : 0.f;
+    s.h[g * mp + j] = u > 0.f ? w_balance / (float)max(rows, 1) * logf(u) : 0.f;
 }
 
 // Positions: x for the passes (zeros for one that takes part in no group, whose inputs may be anything); forward: the picked entry's
@@ -123,7 +127,9 @@ __global__ void __launch_bounds__(256) positions_kernel(const RouteLossArgs a, c
             any |= real;
             if (i < np) {
                 const float lse = real ? __ldg(a.lse + i * a.G + g) : -CUDART_INF_F;
-                s.nl2[g * np + i] = lse == -CUDART_INF_F ? lse : -lse * kLog2e;
+                const float nl = lse == -CUDART_INF_F ? lse : -lse;
+                s.nl[g * np + i] = nl;
+                put_step(s.nl_step, g * np + i, nl);
             }
             if (there) {
                 float v = 0.f;
@@ -191,18 +197,21 @@ __global__ void __launch_bounds__(256) lse_join_kernel(const RouteLossArgs a, co
         for (int z = 0; z < p.splits; ++z) {
             const float2 v = part[z * step];
             const float both = fmaxf(top, v.x);
-            if (both > -CUDART_INF_F) sum = sum * exp2f(top - both) + v.y * exp2f(v.x - both);
+            if (both > -CUDART_INF_F) sum = sum * expf(top - both) + v.y * expf(v.x - both);
             top = both;
         }
         if (top == -CUDART_INF_F) lse = top;  // every entry's score is -inf: no weight anywhere
         else {
-            neg = -(top + log2f(sum));
-            lse = -neg * kLn2;
+            lse = top + logf(sum);
+            neg = -lse;
         }
         const float sc = a.score[i * a.G + g];
         soft = fmaxf(-sc, 0.f) + log1pf(expf(-fabsf(sc)));  // -log sigmoid(sc)
     }
-    if (i < p.np) s.nl2[g * p.np + i] = neg;
+    if (i < p.np) {
+        s.nl[g * p.np + i] = neg;
+        put_step(s.nl_step, g * p.np + i, neg);
+    }
     if (i < a.n) a.lse[i * a.G + g] = lse;
     const int rows = __syncthreads_count(real), live = __syncthreads_count(neg != -CUDART_INF_F);
     soft = block_sum(soft);
@@ -263,7 +272,7 @@ __global__ void __launch_bounds__(256) mean_join_kernel(const RouteLossArgs a, c
     }
 }
 
-__global__ void __launch_bounds__(256) r_join_kernel(const SweepArgs p, float* __restrict__ r)
+__global__ void __launch_bounds__(256) r_join_kernel(const SweepArgs p, float* __restrict__ nr)
 {
     const int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x;
     const int g = blockIdx.y;
@@ -271,7 +280,7 @@ __global__ void __launch_bounds__(256) r_join_kernel(const SweepArgs p, float* _
     float sum = 0.f;
     if (i < p.n)
         for (int z = 0; z < p.splits; ++z) sum += p.part[((int64_t)z * p.G + g) * p.np + i];
-    r[g * p.np + i] = sum;
+    nr[g * p.np + i] = -sum;
 }
 
 // Eight elements of a row: partial sums added in their order, and rounded.
@@ -346,7 +355,7 @@ cudaError_t launch_positions(const RouteLossArgs& a, const RouteGradArgs& b, con
 
 SweepArgs pass_args(const RouteLossArgs& a, const Space& s)
 {
-    return SweepArgs{a.n, a.m, sweep_padded(a.n), sweep_padded(a.m), a.G, 1, s.xs, (const uint16_t*)a.W, s.b2, s.h, s.nl2, s.r, s.part, s.part2};
+    return SweepArgs{a.n, a.m, sweep_padded(a.n), sweep_padded(a.m), a.G, 1, s.xs, (const uint16_t*)a.W, s.b, s.h, s.nl, s.nr, s.b_step, s.nl_step, s.part, s.part2};
 }
 
 }  // namespace
@@ -366,7 +375,7 @@ cudaError_t launch_route_loss(const RouteLossArgs& a, void* ws, cudaStream_t st)
     SweepArgs p = pass_args(a, s);
     const Launch l{st, nullptr, nullptr};
     const unsigned blocks = (unsigned)((p.np + 255) / 256), G = (unsigned)a.G;
-    TRY(launch_kernel(l, entries_kernel, dim3((unsigned)((p.mp + 255) / 256), G), 256, 0, 1, a.bias, nullptr, nullptr, 0.f, a.m, p.mp, s.b2, nullptr, s.done));
+    TRY(launch_kernel(l, entries_kernel, dim3((unsigned)((p.mp + 255) / 256), G), 256, 0, 1, a.bias, nullptr, nullptr, 0.f, a.m, p.mp, s));
     if (a.n) TRY(launch_positions<false>(a, RouteGradArgs{}, s, a.n, p.np, st));
     TRY(launch_sweep(SWEEP_LSE, a.d, p, st));
     if (a.n) TRY(launch_kernel(l, lse_join_kernel, dim3(blocks, G), 256, 0, 1, a, p, s));
@@ -380,7 +389,7 @@ cudaError_t launch_route_grad(const RouteLossArgs& a, const RouteGradArgs& b, vo
     SweepArgs p = pass_args(a, s);
     const Launch l{st, nullptr, nullptr};
     const unsigned G = (unsigned)a.G;
-    TRY(launch_kernel(l, entries_kernel, dim3((unsigned)((p.mp + 255) / 256), G), 256, 0, 1, a.bias, a.mean, b.offset, b.w_balance, a.m, p.mp, s.b2, s.h, nullptr));
+    TRY(launch_kernel(l, entries_kernel, dim3((unsigned)((p.mp + 255) / 256), G), 256, 0, 1, a.bias, a.mean, b.offset, b.w_balance, a.m, p.mp, s));
     if (a.n) TRY(launch_positions<true>(a, b, s, p.np, p.np, st));
     SegmentArgs seg{};
     seg.order = b.order;
@@ -396,7 +405,7 @@ cudaError_t launch_route_grad(const RouteLossArgs& a, const RouteGradArgs& b, vo
     seg.weight_sum = s.wsum;
     TRY(launch_segment_sum(CKV_BF16, seg, s.seg, st));
     TRY(launch_sweep(SWEEP_R, a.d, p, st));
-    if (a.n) TRY(launch_kernel(l, r_join_kernel, dim3((unsigned)((p.np + 255) / 256), G), 256, 0, 1, p, s.r));
+    if (a.n) TRY(launch_kernel(l, r_join_kernel, dim3((unsigned)((p.np + 255) / 256), G), 256, 0, 1, p, s.nr));
     TRY(launch_sweep(SWEEP_DX, a.d, p, st));
     if (a.n) TRY(launch_kernel(l, dx_join_kernel, dim3((unsigned)((a.n * a.d / 8 + 255) / 256)), 256, 0, 1, a, b, p, s.ds));
     TRY(launch_sweep(SWEEP_DW, a.d, p, st));

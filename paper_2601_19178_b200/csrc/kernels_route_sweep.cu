@@ -1,8 +1,11 @@
 // The passes of the router losses over the score matrix, on the tcgen05 tensor cores (kernels_route_loss.cu has the formulas).
 //
 // One side's rows stand: 128 to a block, a thread each (TMEM lane), their inputs as an A operand in TMEM.  The other side's stream
-// through a ring of shared-memory stages, as B operand (a swizzled TMA box per 64 inputs) with up to two numbers for each
-// row beside it (bulk copies).  A tile of scores appears in TMEM, its thread reads its row of it, and:
+// through a ring of shared-memory stages, as B operand (a swizzled TMA box per 64 inputs).  What a streaming row adds to all its
+// scores (an entry's bias, a position's -lse) comes in with the product, as one more step of K = 16: ones times the number
+// cut into three bf16 parts, whose sum is the fp32 number exactly.  (Read beside the scores it cost a thread one 16-byte
+// load of shared memory per four columns, whose 512 bytes take the data path four clocks, and an addition.)  A tile of
+// scores appears in TMEM, its thread reads its row of it, and:
 //   sweep_kernel (LSE, MEAN, R)  keeps a running sum.  Three blocks per CTA, two accumulators of 64 columns each (one of 96 at d_in = 128).
 //   grad_kernel (DX, DW)         turns it into weights T (bf16, over the head of the scores they came from), which multiply the
 //                                same tile once more, now as MN-major operand:  O += T tile.  Two blocks per CTA (one at d_in =
@@ -54,6 +57,13 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile
     if (!ok) *abort_flag = 1;
     return ok;
 }
+// Named barriers of a score buffer, for the four warps whose turn it is and its block's issuing warp: "the weights of tile t stand".
+// The former arrive and run on, the latter waits; once a wait has run out, a warp takes part as the issuing warp does, tile by
+// tile, so that the others never wait for good.  Two in turn per buffer: who gives up on the buffer's next tile has arrived for
+// this one already, and on the same barrier would count for the issuing warp.  (As mbarriers they cost some 300 clocks more each turn.)
+__device__ __forceinline__ int weights_barrier(int buffer, int tile) { return 2 + 2 * buffer + ((tile >> 1) & 1); }
+__device__ __forceinline__ void weights_arrive(int buffer, int tile) { asm volatile("bar.arrive %0, 160;" ::"r"(weights_barrier(buffer, tile)) : "memory"); }
+__device__ __forceinline__ void weights_sync(int buffer, int tile) { asm volatile("bar.sync %0, 160;" ::"r"(weights_barrier(buffer, tile)) : "memory"); }
 __device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_commit_to(uint32_t bar)
@@ -80,6 +90,11 @@ __device__ __forceinline__ uint64_t tile_desc(uint32_t addr)
 {
     constexpr uint64_t layout = ROWB == 128 ? 2 : 4;  // 128-byte / 64-byte swizzle
     return (uint64_t)((addr & 0x3ffffu) >> 4) | (1ull << 16) | ((uint64_t)(ROWB * 8 >> 4) << 32) | (1ull << 46) | (layout << 61);
+}
+// That step's B operand: 16 bf16 per row, in groups of eight rows of 16 bytes, no swizzle (StepLayout of fit.h).
+__device__ __forceinline__ uint64_t step_desc(uint32_t addr)
+{
+    return (uint64_t)((addr & 0x3ffffu) >> 4) | ((uint64_t)(128 >> 4) << 16) | ((uint64_t)(256 >> 4) << 32) | (1ull << 46);
 }
 __device__ __forceinline__ void ld32(uint32_t taddr, uint32_t (&r)[32])
 {
@@ -115,6 +130,18 @@ __device__ __forceinline__ void st16(uint32_t taddr, const uint32_t* r)
         "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
         "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
         : "memory");
+}
+__device__ __forceinline__ void st8(uint32_t taddr, const uint32_t (&r)[8])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]),
+                 "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+                 : "memory");
+}
+// A operand of the step that adds a streaming row's own number: three ones for the number's three parts.
+__device__ __forceinline__ void store_ones(uint32_t taddr)
+{
+    const uint32_t ones[8] = {0x3f803f80u, 0x00003f80u, 0, 0, 0, 0, 0, 0};
+    st8(taddr, ones);
 }
 __device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void expect_bytes(uint32_t bar, uint32_t bytes)
@@ -172,6 +199,49 @@ __device__ __forceinline__ float max3f(float a, float b, float c)
 }
 __device__ __forceinline__ F2 pair(const uint32_t (&v)[32], int e) { return {__uint_as_float(v[e]), __uint_as_float(v[e + 1])}; }
 __device__ __forceinline__ F2 both(float v) { return {v, v}; }
+__device__ __forceinline__ F2 neg(F2 v) { return {-v.x, -v.y}; }
+
+// 2^x on the FMA pipe, for as many of the weights as balance it with the special-function unit: x = n + f with n the nearest whole
+// number, 2^f on [-1/2, 1/2] by the polynomial of degree DEG whose largest relative error is smallest (Remez exchange; 7.5e-5,
+// 2.6e-6, 7.5e-8 for degrees 3 to 5), 2^n by its exponent bits, which the sum that rounds x leaves in its low bits.  Arguments
+// are at most 0 but for rounding; below -127 the result is zero, and not a number stays that.
+template <int DEG>
+struct Exp2 {
+    F2 p, scale;  // 2^x = p * scale
+    __device__ __forceinline__ explicit Exp2(F2 x)
+    {
+        constexpr float kRound = 12582912.f + 127.f;  // 1.5 * 2^23 + 127
+        asm("max.NaN.f32 %0, %0, 0fC2FE0000;" : "+f"(x.x));  // -127
+        asm("max.NaN.f32 %0, %0, 0fC2FE0000;" : "+f"(x.y));
+        const F2 t = add2(x, both(kRound)), f = add2(x, neg(add2(t, both(-kRound))));
+        if (DEG == 3) p = fma2(fma2(fma2(both(0.0551716685f), f, both(0.242611125f)), f, both(0.693260968f)), f, both(0.999928057f));
+        else if (DEG == 4)
+            p = fma2(fma2(fma2(fma2(both(0.00957010221f), f, both(0.0559178591f)), f, both(0.240247443f)), f, both(0.693121791f)), f, both(0.999999285f));
+        else
+            p = fma2(fma2(fma2(fma2(fma2(both(0.00132764725f), f, both(0.00967554096f)), f, both(0.0555071309f)), f, both(0.240221202f)), f, both(0.693146944f)), f,
+                     both(1.00000012f));
+        scale = {__uint_as_float(__float_as_uint(t.x) << 23), __uint_as_float(__float_as_uint(t.y) << 23)};
+    }
+};
+
+// Pairs of sixteen whose exponentials run on the FMA pipe, spread over them.  32768 positions x 16384 entries x 4 groups, us, with 0, 3, 4, 5 and
+// 6 of them: LSE 589 521 507 509 524, MEAN 572 492 478 460 471, R 582 505 499 502 531, DX 633 599 612 628 634, DW 675 644 646 681 713.
+#ifndef FMA_LSE
+#define FMA_LSE 4
+#define FMA_MEAN 5
+#define FMA_R 4
+#define FMA_DX 3
+#define FMA_DW 3
+#endif
+constexpr int kFmaLse = FMA_LSE, kFmaMean = FMA_MEAN, kFmaR = FMA_R, kFmaDx = FMA_DX, kFmaDw = FMA_DW;
+__device__ __forceinline__ constexpr bool on_fma(int q, int of16) { return (q + 1) * of16 / 16 > q * of16 / 16; }
+template <bool DW>
+__device__ __forceinline__ F2 weight(F2 u, bool fma)
+{
+    if (!fma) return {ex2(u.x), ex2(u.y)};
+    const Exp2<DW ? 4 : 3> p(u);
+    return mul2(p.p, p.scale);
+}
 
 // A sum of many parts: what an addition loses is added with the next part.
 struct LongSum {
@@ -219,12 +289,13 @@ struct Sweep {
     static constexpr int ROWB = DIN >= 64 ? 128 : 64;
     static constexpr int BOXES = DIN == 128 ? 2 : 1;
     static constexpr int BOX = TN * ROWB, TILE = BOXES * BOX;
-    static constexpr int OFF_NUM = kStages * TILE, NUM = TN * 4, OFF_BAR = OFF_NUM + kStages * 2 * NUM;
+    static constexpr int OFF_STEP = kStages * TILE, STEP = TN * 32, OFF_NUM = OFF_STEP + kStages * STEP, NUM = TN * 4,
+                         OFF_BAR = OFF_NUM + kStages * NUM;
     enum { FULL = 0, EMPTY = kStages, AFULL = 2 * kStages, AFREE = AFULL + kBlocks * ACCS, DRAIN = AFREE + kBlocks * ACCS, COUNT };
     static constexpr int OFF_ABORT = OFF_BAR + COUNT * 8, SMEM = OFF_ABORT + 16;
     static_assert(SMEM <= 226 * 1024 && BOX % 1024 == 0, "shared memory");
-    static constexpr uint32_t COL_A = kBlocks * TN;
-    static_assert(COL_A + kBlocks * (DIN / 2) <= 512, "TMEM columns");
+    static constexpr uint32_t COL_A = kBlocks * TN, COL_ONES = COL_A + kBlocks * (DIN / 2);
+    static_assert(COL_ONES + 8 <= 512, "TMEM columns");
     static_assert(kSweepPad % TN == 0, "numbers are copied a tile at a time");
 };
 
@@ -234,7 +305,7 @@ __global__ void __launch_bounds__(kSweepThreads, 1) sweep_kernel(const __grid_co
     using L = Sweep<DIN>;
     constexpr int TN = L::TN, AN = L::AN, ACCS = L::ACCS;
     constexpr bool kEntriesStand = MODE == SWEEP_MEAN;
-    constexpr uint32_t kTileBytes = L::TILE + (MODE == SWEEP_R ? 2 : 1) * L::NUM;
+    constexpr uint32_t kTileBytes = L::TILE + L::STEP + (MODE == SWEEP_R ? L::NUM : 0);
     extern __shared__ __align__(1024) unsigned char sm[];
     __shared__ uint32_t tmem_slot;
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
@@ -255,7 +326,7 @@ __global__ void __launch_bounds__(kSweepThreads, 1) sweep_kernel(const __grid_co
     if (tid == 0) {
         for (int s = 0; s < kStages; ++s) {
             bar_init(bar(L::FULL + s), 1);
-            bar_init(bar(L::EMPTY + s), 4 * (uint32_t)n_blocks);
+            bar_init(bar(L::EMPTY + s), (MODE == SWEEP_R ? 5 : 1) * (uint32_t)n_blocks);  // the products, and who reads h
         }
         for (int i = 0; i < kBlocks * ACCS; ++i) {
             bar_init(bar(L::AFULL + i), 1);
@@ -273,8 +344,10 @@ __global__ void __launch_bounds__(kSweepThreads, 1) sweep_kernel(const __grid_co
     __syncthreads();
     tc_after();
     const uint32_t tmem = tmem_slot;
-    if (warp < 4 * n_blocks)
+    if (warp < 4 * n_blocks) {
+        if (e == 0) store_ones(tmem + lane_base + L::COL_ONES);
         load_inputs<DIN>(tmem + lane_base + L::COL_A + e * (DIN / 2), (kEntriesStand ? a.W + ((int64_t)grp * a.m + row) * DIN : a.x + row * DIN), in);
+    }
     if (warp < kLoadWarp) {  // (the loading warp is on its way)
         tc_before();
         asm volatile("bar.sync 1, %0;" ::"n"(kLoadWarp * 32) : "memory");
@@ -285,15 +358,52 @@ __global__ void __launch_bounds__(kSweepThreads, 1) sweep_kernel(const __grid_co
     float top = -CUDART_INF_F;
     if (warp < kReadWarps) {
         // ------------------------------------------------------------ thread = standing row
-        // log2 of a weight is  s log2(e) + own + number of the column
-        const float own = !in || MODE == SWEEP_LSE ? 0.f : kEntriesStand ? a.b2[grp * a.mp + row] : a.nl2[grp * a.np + row];
+        // log2 of a weight is  s log2(e) + own
+        float own = !in || MODE == SWEEP_LSE ? 0.f : (kEntriesStand ? a.b[grp * a.mp + row] : a.nl[grp * a.np + row]) * kLog2e;
         const uint32_t tacc = tmem + lane_base + (uint32_t)(TN * e);
+        auto look = [&](uint32_t (&x)[32], const float4* num) {
+            F2 u[16];
+            if (MODE == SWEEP_LSE) {
+                float m0 = __uint_as_float(x[0]), m1 = __uint_as_float(x[1]);
+#pragma unroll
+                for (int q = 2; q < 30; q += 4) {
+                    m0 = max3f(m0, __uint_as_float(x[q]), __uint_as_float(x[q + 1]));
+                    m1 = max3f(m1, __uint_as_float(x[q + 2]), __uint_as_float(x[q + 3]));
+                }
+                m0 = max3f(fmaxf(m0, m1), __uint_as_float(x[30]), __uint_as_float(x[31]));
+                if (m0 > top) {
+                    const float f = ex2((top - m0) * kLog2e);
+                    sum.s *= f;
+                    sum.lost *= f;
+                    top = m0;
+                    own = -m0 * kLog2e;
+                }
+            }
+#pragma unroll
+            for (int q = 0; q < 16; ++q) u[q] = fma2(pair(x, 2 * q), both(kLog2e), both(own));
+            F2 part{0.f, 0.f};
+#pragma unroll
+            for (int q = 0; q < 16; ++q) {
+                F2 w{};
+                if (MODE == SWEEP_R) {
+                    const float4 k = num[q / 2];
+                    w = q % 2 ? F2{k.z, k.w} : F2{k.x, k.y};
+                }
+                if (on_fma(q, MODE == SWEEP_R ? kFmaR : MODE == SWEEP_LSE ? kFmaLse : kFmaMean)) {
+                    const Exp2<MODE == SWEEP_R ? 4 : 5> p(u[q]);
+                    part = MODE == SWEEP_R ? fma2(mul2(p.p, p.scale), w, part) : fma2(p.p, p.scale, part);
+                } else {
+                    const F2 p{ex2(u[q].x), ex2(u[q].y)};
+                    part = MODE == SWEEP_R ? fma2(p, w, part) : add2(part, p);
+                }
+            }
+            sum.add(part.x + part.y);
+        };
         int s = 0;
-        uint32_t par = 0;
         for (int t = 0; e < n_blocks && t < n_tiles; ++t) {
-            if (!bar_wait(bar(L::FULL + s), par, abort_flag)) break;  // (the numbers; the products wait for the tile themselves)
-            const float* num = reinterpret_cast<const float*>(sm + L::OFF_NUM + s * 2 * L::NUM);
             bool ok = true;
+            if (MODE == SWEEP_R) ok = bar_wait(bar(L::FULL + s), (t / kStages) & 1, abort_flag);  // (h is to be seen; the products wait themselves)
+            const float* num = reinterpret_cast<const float*>(sm + L::OFF_NUM + s * L::NUM);
 #pragma unroll
             for (int h = 0; h < ACCS; ++h) {
                 const int acc = ACCS * e + h;
@@ -309,59 +419,13 @@ __global__ void __launch_bounds__(kSweepThreads, 1) sweep_kernel(const __grid_co
                 __syncwarp();
                 if (lane == 0) bar_arrive(bar(L::AFREE + acc));
 #pragma unroll
-                for (int c = 0; c < AN / 32; ++c) {
-                    const float4* n0 = reinterpret_cast<const float4*>(num + AN * h + 32 * c);
-                    const float4* n1 = n0 + TN / 4;
-                    F2 u[16];
-#pragma unroll
-                    for (int q = 0; q < 8; ++q) {
-                        const float4 k = n0[q];
-                        F2 k0{k.x, k.y}, k1{k.z, k.w};
-                        if (MODE != SWEEP_LSE) {
-                            k0 = add2(k0, both(own));
-                            k1 = add2(k1, both(own));
-                        }
-                        u[2 * q] = fma2(pair(v[c], 4 * q), both(kLog2e), k0);
-                        u[2 * q + 1] = fma2(pair(v[c], 4 * q + 2), both(kLog2e), k1);
-                    }
-                    if (MODE == SWEEP_LSE) {
-                        float m0 = u[0].x, m1 = u[0].y;
-#pragma unroll
-                        for (int q = 1; q < 15; q += 2) {
-                            m0 = max3f(m0, u[q].x, u[q].y);
-                            m1 = max3f(m1, u[q + 1].x, u[q + 1].y);
-                        }
-                        m0 = max3f(fmaxf(m0, m1), u[15].x, u[15].y);
-                        if (m0 > top) {
-                            const float f = ex2(top - m0);
-                            sum.s *= f;
-                            sum.lost *= f;
-                            top = m0;
-                        }
-                        const float off = top == -CUDART_INF_F ? 0.f : -top;
-#pragma unroll
-                        for (int q = 0; q < 16; ++q) u[q] = add2(u[q], both(off));
-                    }
-                    F2 part{0.f, 0.f};
-#pragma unroll
-                    for (int q = 0; q < 16; ++q) {
-                        const F2 p{ex2(u[q].x), ex2(u[q].y)};
-                        if (MODE == SWEEP_R) {
-                            const F2 w = reinterpret_cast<const F2*>(n1)[q];
-                            part = fma2(p, w, part);
-                        } else {
-                            part = add2(part, p);
-                        }
-                    }
-                    sum.add(part.x + part.y);
-                }
+                for (int c = 0; c < AN / 32; ++c) look(v[c], reinterpret_cast<const float4*>(num + AN * h + 32 * c));
             }
             if (!ok) break;
-            __syncwarp();
-            if (lane == 0) bar_arrive(bar(L::EMPTY + s));
-            if (++s == kStages) {
-                s = 0;
-                par ^= 1;
+            if (MODE == SWEEP_R) {
+                __syncwarp();
+                if (lane == 0) bar_arrive(bar(L::EMPTY + s));
+                if (++s == kStages) s = 0;
             }
         }
     } else if (warp < kIssueWarp + kBlocks) {
@@ -383,7 +447,9 @@ __global__ void __launch_bounds__(kSweepThreads, 1) sweep_kernel(const __grid_co
 #pragma unroll
                     for (int ks = 0; ks < DIN / 16; ++ks)
                         mma_ts(d + AN * h, at + 8 * ks, w + (uint64_t)(((ks & 3) * 32 + (ks >> 2) * L::BOX) >> 4), idesc, ks > 0);
+                    mma_ts(d + AN * h, tmem + L::COL_ONES, step_desc(sb + L::OFF_STEP + s * L::STEP + AN * h * 32), idesc, 1u);
                     tc_commit_to(bar(L::AFULL + ACCS * blk + h));
+                    if (h == ACCS - 1) tc_commit_to(bar(L::EMPTY + s));
                 }
                 __syncwarp();
             }
@@ -411,9 +477,8 @@ __global__ void __launch_bounds__(kSweepThreads, 1) sweep_kernel(const __grid_co
 #pragma unroll
                 for (int i = 0; i < L::BOXES; ++i)
                     load_box(sb + s * L::TILE + i * L::BOX, &map, 64 * i, (int)c0, kEntriesStand ? 0 : grp, bar(L::FULL + s));
-                const uint32_t num = sb + L::OFF_NUM + s * 2 * L::NUM;
-                load_bytes(num, kEntriesStand ? a.nl2 + grp * a.np + c0 : a.b2 + grp * a.mp + c0, L::NUM, bar(L::FULL + s));
-                if (MODE == SWEEP_R) load_bytes(num + L::NUM, a.h + grp * a.mp + c0, L::NUM, bar(L::FULL + s));
+                load_bytes(sb + L::OFF_STEP + s * L::STEP, kEntriesStand ? a.nl_step + (grp * a.np + c0) * 16 : a.b_step + (grp * a.mp + c0) * 16, L::STEP, bar(L::FULL + s));
+                if (MODE == SWEEP_R) load_bytes(sb + L::OFF_NUM + s * L::NUM, a.h + grp * a.mp + c0, L::NUM, bar(L::FULL + s));
             }
             __syncwarp();
             ++issued;
@@ -447,12 +512,14 @@ struct Grad {
     static constexpr int BOXES = DIN == 128 ? 2 : 1;
     static constexpr int BOX = TN * ROWB, TILE = BOXES * BOX, STAGES = 8;
     static constexpr int ON = DIN < 64 ? DIN : 64;     // columns of O that one product covers: a box
-    static constexpr int OFF_NUM = STAGES * TILE, NUM = TN * 4, OFF_SUM = OFF_NUM + STAGES * 2 * NUM, OFF_BAR = OFF_SUM + BLOCKS * 128 * 4;
-    enum { FULL = 0, EMPTY = STAGES, SFULL = 2 * STAGES, TREADY = SFULL + 2 * BLOCKS, OFULL = TREADY + 2 * BLOCKS, COUNT = OFULL + BLOCKS };
+    static constexpr int OFF_STEP = STAGES * TILE, STEP = TN * 32, OFF_NUM = OFF_STEP + STAGES * STEP, NUM = TN * 4, OFF_SUM = OFF_NUM + STAGES * NUM,
+                         OFF_BAR = OFF_SUM + BLOCKS * 128 * 4;
+    enum { FULL = 0, EMPTY = STAGES, SFULL = 2 * STAGES, OFULL = SFULL + 2 * BLOCKS, COUNT = OFULL + BLOCKS };
     static constexpr int OFF_ABORT = OFF_BAR + COUNT * 8, SMEM = OFF_ABORT + 16;
     static_assert(SMEM <= 226 * 1024 && BOX % 1024 == 0, "shared memory");
-    static constexpr uint32_t COL_O = 2 * TN, COL_A = COL_O + DIN, COL_BLOCK = COL_A + DIN / 2;  // a block's: two buffers, O, inputs
-    static_assert(BLOCKS * COL_BLOCK <= 512, "TMEM columns");
+    static constexpr uint32_t COL_O = 2 * TN, COL_A = COL_O + DIN, COL_BLOCK = COL_A + DIN / 2,  // a block's: two buffers, O, inputs
+                              COL_ONES = BLOCKS * COL_BLOCK;
+    static_assert(COL_ONES + 8 <= 512, "TMEM columns");
     static_assert(kSweepPad % TN == 0, "numbers are copied a tile at a time");
 };
 
@@ -489,10 +556,7 @@ __global__ void __launch_bounds__(Grad<DIN>::THREADS, 1) grad_kernel(const __gri
             bar_init(bar(L::FULL + s), 1);
             bar_init(bar(L::EMPTY + s), (uint32_t)n_blocks);
         }
-        for (int i = 0; i < 2 * L::BLOCKS; ++i) {
-            bar_init(bar(L::SFULL + i), 1);
-            bar_init(bar(L::TREADY + i), 4);
-        }
+        for (int i = 0; i < 2 * L::BLOCKS; ++i) bar_init(bar(L::SFULL + i), 1);
         for (int i = 0; i < L::BLOCKS; ++i) bar_init(bar(L::OFULL + i), 1);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -505,6 +569,7 @@ __global__ void __launch_bounds__(Grad<DIN>::THREADS, 1) grad_kernel(const __gri
     __syncthreads();
     tc_after();
     const uint32_t tmem = tmem_slot, tblock = tmem + (uint32_t)e * L::COL_BLOCK;
+    if (warp < 4) store_ones(tmem + lane_base + L::COL_ONES);
     if (warp < 8 * n_blocks && buf == 0)
         load_inputs<DIN>(tblock + lane_base + L::COL_A, (kEntriesStand ? a.W + ((int64_t)blockIdx.y * a.m + row) * DIN : a.x + row * DIN), in);
     if (warp < L::LOAD_WARP) {  // (the loading warp is on its way)
@@ -517,8 +582,8 @@ __global__ void __launch_bounds__(Grad<DIN>::THREADS, 1) grad_kernel(const __gri
     if (warp < L::READ_WARPS) {
         // ------------------------------------------------------------ weights, thread = standing row, every second tile
         int g = first_group, in_group = first_tile;
-        auto own0 = [&] { return !in ? -CUDART_INF_F : kEntriesStand ? a.b2[g * a.mp + row] : a.nl2[g * a.np + row]; };
-        auto own1 = [&] { return !in ? 0.f : kEntriesStand ? a.h[g * a.mp + row] : -a.r[g * a.np + row]; };
+        auto own0 = [&] { return !in ? -CUDART_INF_F : (kEntriesStand ? a.b[g * a.mp + row] : a.nl[g * a.np + row]) * kLog2e; };
+        auto own1 = [&] { return !in ? 0.f : kEntriesStand ? a.h[g * a.mp + row] : a.nr[g * a.np + row]; };
         float log_own = 0.f, h_own = 0.f;
         if (n_tiles > 0) {
             log_own = own0();
@@ -526,6 +591,7 @@ __global__ void __launch_bounds__(Grad<DIN>::THREADS, 1) grad_kernel(const __gri
         }
         const uint32_t ts = tblock + lane_base + (uint32_t)(TN * buf);
         if (buf == 1) ++in_group;
+        bool ok = true;
         for (int t = buf; e < n_blocks && t < n_tiles; t += 2, in_group += 2) {
             if (!kEntriesStand && in_group >= per_group) {
                 do {
@@ -536,26 +602,29 @@ __global__ void __launch_bounds__(Grad<DIN>::THREADS, 1) grad_kernel(const __gri
                 h_own = own1();
             }
             const int s = t % L::STAGES;
-            if (!bar_wait(bar(L::SFULL + 2 * e + buf), (t >> 1) & 1, abort_flag)) break;
-            if (!bar_wait(bar(L::FULL + s), (t / L::STAGES) & 1, abort_flag)) break;  // (long complete: the numbers are to be seen)
+            ok = ok && bar_wait(bar(L::SFULL + 2 * e + buf), (t >> 1) & 1, abort_flag);
+            ok = ok && bar_wait(bar(L::FULL + s), (t / L::STAGES) & 1, abort_flag);  // (long complete: the numbers are to be seen)
+            if (!ok) {
+                weights_sync(2 * e + buf, t);
+                continue;
+            }
             tc_after();
-            const float* num = reinterpret_cast<const float*>(sm + L::OFF_NUM + s * 2 * L::NUM);
+            const float* num = reinterpret_cast<const float*>(sm + L::OFF_NUM + s * L::NUM);
 #pragma unroll
             for (int c = 0; c < TN / 32; ++c) {
                 uint32_t v[32], w[16];
                 ld32(ts + 32 * c, v);
                 wait_ld32(v);
-                const float4 *n0 = reinterpret_cast<const float4*>(num + 32 * c), *n1 = n0 + TN / 4;
+                const float4* n1 = reinterpret_cast<const float4*>(num + 32 * c);
                 F2 part{0.f, 0.f};
 #pragma unroll
                 for (int q = 0; q < 8; ++q) {
-                    const float4 k = n0[q], hk = n1[q];
-                    const F2 u0 = fma2(pair(v, 4 * q), both(kLog2e), add2({k.x, k.y}, both(log_own)));
-                    const F2 u1 = fma2(pair(v, 4 * q + 2), both(kLog2e), add2({k.z, k.w}, both(log_own)));
-                    // DX: p (h_j - r_i), own is -r_i;  DW: p (h_j - r_i), own is h_j and the column's number r_i
-                    const F2 d0 = kEntriesStand ? fma2({hk.x, hk.y}, both(-1.f), both(h_own)) : add2({hk.x, hk.y}, both(h_own));
-                    const F2 d1 = kEntriesStand ? fma2({hk.z, hk.w}, both(-1.f), both(h_own)) : add2({hk.z, hk.w}, both(h_own));
-                    const F2 w0 = mul2({ex2(u0.x), ex2(u0.y)}, d0), w1 = mul2({ex2(u1.x), ex2(u1.y)}, d1);
+                    const float4 hk = n1[q];
+                    const F2 u0 = fma2(pair(v, 4 * q), both(kLog2e), both(log_own)), u1 = fma2(pair(v, 4 * q + 2), both(kLog2e), both(log_own));
+                    // h_j - r_i, of which one is the thread's own and the other one the column's
+                    const F2 d0 = add2({hk.x, hk.y}, both(h_own)), d1 = add2({hk.z, hk.w}, both(h_own));
+                    const F2 w0 = mul2(weight<kEntriesStand>(u0, on_fma(2 * q, kEntriesStand ? kFmaDw : kFmaDx)), d0);
+                    const F2 w1 = mul2(weight<kEntriesStand>(u1, on_fma(2 * q + 1, kEntriesStand ? kFmaDw : kFmaDx)), d1);
                     if (kEntriesStand) part = add2(part, add2(w0, w1));
                     w[2 * q] = pack_bf16(w0.x, w0.y);
                     w[2 * q + 1] = pack_bf16(w1.x, w1.y);
@@ -565,8 +634,7 @@ __global__ void __launch_bounds__(Grad<DIN>::THREADS, 1) grad_kernel(const __gri
             }
             wait_st();
             tc_before();
-            __syncwarp();
-            if (lane == 0) bar_arrive(bar(L::TREADY + 2 * e + buf));
+            weights_arrive(2 * e + buf, t);
         }
     } else if (warp < L::LOAD_WARP) {
         // ------------------------------------------------------------ products, one warp per block
@@ -574,11 +642,11 @@ __global__ void __launch_bounds__(Grad<DIN>::THREADS, 1) grad_kernel(const __gri
         constexpr uint32_t idesc_s = idesc_bf16(128, TN, false), idesc_o = idesc_bf16(128, L::ON, true);
         const int blk = warp - L::ISSUE_WARP;
         const uint32_t tb = tmem + (uint32_t)blk * L::COL_BLOCK;
-        bool ok = blk < n_blocks;
-        for (int t = -2; ok && t < n_tiles; ++t) {
+        bool ok = true;
+        for (int t = -2; blk < n_blocks && t < n_tiles; ++t) {
             const int nxt = t + 2;
             if (t >= 0) {
-                ok = bar_wait(bar(L::TREADY + 2 * blk + (t & 1)), (t >> 1) & 1, abort_flag);
+                weights_sync(2 * blk + (t & 1), t);
                 if (ok && elect_one()) {
                     tc_after();
                     const uint32_t tile = sb + (t % L::STAGES) * L::TILE, tw = tb + (uint32_t)(TN * (t & 1));
@@ -599,6 +667,7 @@ __global__ void __launch_bounds__(Grad<DIN>::THREADS, 1) grad_kernel(const __gri
 #pragma unroll
                 for (int ks = 0; ks < DIN / 16; ++ks)
                     mma_ts(tb + (uint32_t)(TN * (nxt & 1)), tb + L::COL_A + 8 * ks, w + (uint64_t)(((ks & 3) * 32 + (ks >> 2) * L::BOX) >> 4), idesc_s, ks > 0);
+                mma_ts(tb + (uint32_t)(TN * (nxt & 1)), tmem + L::COL_ONES, step_desc(sb + L::OFF_STEP + (nxt % L::STAGES) * L::STEP), idesc_s, 1u);
                 tc_commit_to(bar(L::SFULL + 2 * blk + (nxt & 1)));
             }
             __syncwarp();
@@ -622,13 +691,12 @@ __global__ void __launch_bounds__(Grad<DIN>::THREADS, 1) grad_kernel(const __gri
             if (!ok) break;
             if (lane == 0) {
                 const int64_t c0 = (int64_t)in_group * TN;
-                expect_bytes(bar(L::FULL + s), L::TILE + 2 * L::NUM);
+                expect_bytes(bar(L::FULL + s), L::TILE + L::STEP + L::NUM);
 #pragma unroll
                 for (int i = 0; i < L::BOXES; ++i)
                     load_box(sb + s * L::TILE + i * L::BOX, &map, 64 * i, (int)c0, kEntriesStand ? 0 : g, bar(L::FULL + s));
-                const uint32_t num = sb + L::OFF_NUM + s * 2 * L::NUM;
-                load_bytes(num, kEntriesStand ? a.nl2 + g * a.np + c0 : a.b2 + g * a.mp + c0, L::NUM, bar(L::FULL + s));
-                load_bytes(num + L::NUM, kEntriesStand ? a.r + g * a.np + c0 : a.h + g * a.mp + c0, L::NUM, bar(L::FULL + s));
+                load_bytes(sb + L::OFF_STEP + s * L::STEP, kEntriesStand ? a.nl_step + (g * a.np + c0) * 16 : a.b_step + (g * a.mp + c0) * 16, L::STEP, bar(L::FULL + s));
+                load_bytes(sb + L::OFF_NUM + s * L::NUM, kEntriesStand ? a.nr + g * a.np + c0 : a.h + g * a.mp + c0, L::NUM, bar(L::FULL + s));
             }
             __syncwarp();
             ++issued;
