@@ -100,10 +100,11 @@ try:
     from . import _pycall
 except ImportError as e:
     raise ImportError(f"{e}: build it with `python paper_2601_19178_b200/build.py`") from e
-_ATTEND, _ATTEND_VISIBLE, _ATTEND_STATIC, _APPEND, _PUT, _ROUTE, _PROJECT = (
+(_ATTEND, _ATTEND_VISIBLE, _ATTEND_STATIC, _APPEND, _PUT, _ROUTE, _PROJECT, _SORT, _LOSS, _LOSS_GRAD, _GATHER, _GATHER_GRAD) = (
     ctypes.cast(f, ctypes.c_void_p).value
     for f in (lib.ckv_attend, lib.ckv_attend_visible, lib.ckv_attend_static, lib.ckv_cache_append, lib.ckv_cache_put_batch,
-              lib.ckv_route, lib.ckv_project))
+              lib.ckv_route, lib.ckv_project, lib.ckv_sort_indices, lib.ckv_route_loss, lib.ckv_route_loss_grad, lib.ckv_gather,
+              lib.ckv_gather_grad))
 
 
 def _ptr(x) -> Optional[int]:
@@ -365,6 +366,10 @@ def ckv_sort_indices_bytes(n: int, n_groups: int, n_entries: int) -> int:
 def ckv_sort_indices(device: int, n: int, n_groups: int, n_entries: int, idx, order, offset, workspace, workspace_bytes: int,
                      stream=None) -> None:
     """Positions by the entry they picked: idx [n][G] -> order [G][n], offset [G][n_entries + 1] (int32, device)."""
+    stream = _stream(stream)
+    st = _pycall.sort(_SORT, device, n, n_groups, n_entries, idx, order, offset, workspace, workspace_bytes, stream or 0)
+    if st is not None:
+        return _check(None, st, "ckv_sort_indices") if st else None
     _check(None, lib.ckv_sort_indices(device, n, n_groups, n_entries, _ptr(idx), _ptr(order), _ptr(offset), _ptr(workspace),
                                       int(workspace_bytes), _stream(stream)), "ckv_sort_indices")
 
@@ -379,6 +384,10 @@ def ckv_route_loss_bytes(n: int, n_groups: int, d_in: int, n_entries: int):
 def ckv_route_loss(device: int, n: int, n_groups: int, d_in: int, n_entries: int, x, W, bias, idx, loss, lse, score, mean,
                    workspace, workspace_bytes: int, stream=None) -> None:
     """Router losses [G][2] (balance, peak), with lse and score [n][G] and mean [G][n_entries] for the gradient."""
+    stream = _stream(stream)
+    st = _pycall.loss(_LOSS, device, n, n_groups, d_in, n_entries, x, W, bias, idx, loss, lse, score, mean, workspace, workspace_bytes, stream or 0)
+    if st is not None:
+        return _check(None, st, "ckv_route_loss") if st else None
     _check(None, lib.ckv_route_loss(device, n, n_groups, d_in, n_entries, _ptr(x), _ptr(W), _ptr(bias), _ptr(idx), _ptr(loss),
                                     _ptr(lse), _ptr(score), _ptr(mean), _ptr(workspace), int(workspace_bytes), _stream(stream)),
            "ckv_route_loss")
@@ -388,6 +397,11 @@ def ckv_route_loss_grad(device: int, n: int, n_groups: int, d_in: int, n_entries
                         score, mean, balance_weight: float, peak_weight: float, d_score, dx, dW, dbias, workspace,
                         workspace_bytes: int, stream=None) -> None:
     """Gradient of the router losses, and of what else depends on the picked scores (d_score), by x, W and bias."""
+    stream = _stream(stream)
+    st = _pycall.loss_grad(_LOSS_GRAD, device, n, n_groups, d_in, n_entries, x, W, bias, idx, order, offset, lse, score, mean,
+                           balance_weight, peak_weight, d_score, dx, dW, dbias, workspace, workspace_bytes, stream or 0)
+    if st is not None:
+        return _check(None, st, "ckv_route_loss_grad") if st else None
     _check(None, lib.ckv_route_loss_grad(device, n, n_groups, d_in, n_entries, _ptr(x), _ptr(W), _ptr(bias), _ptr(idx),
                                          _ptr(order), _ptr(offset), _ptr(lse), _ptr(score), _ptr(mean), balance_weight,
                                          peak_weight, _ptr(d_score), _ptr(dx), _ptr(dW), _ptr(dbias), _ptr(workspace),
@@ -397,6 +411,10 @@ def ckv_route_loss_grad(device: int, n: int, n_groups: int, d_in: int, n_entries
 def ckv_gather(device: int, dtype: int, n: int, n_groups: int, head_dim: int, d_shared: int, n_entries: int, pool, idx, user,
                score, out, stream=None) -> None:
     """out [n][G][head_dim] = (user part | sigmoid(score) * picked pool row); score None: without the gate."""
+    stream = _stream(stream)
+    st = _pycall.gather(_GATHER, device, dtype, n, n_groups, head_dim, d_shared, n_entries, pool, idx, user, score, out, stream or 0)
+    if st is not None:
+        return _check(None, st, "ckv_gather") if st else None
     _check(None, lib.ckv_gather(device, dtype, n, n_groups, head_dim, d_shared, n_entries, _ptr(pool), _ptr(idx), _ptr(user),
                                 _ptr(score), _ptr(out), _stream(stream)), "ckv_gather")
 
@@ -410,6 +428,11 @@ def ckv_gather_grad_bytes(n: int, n_groups: int, head_dim: int) -> int:
 def ckv_gather_grad(device: int, dtype: int, n: int, n_groups: int, head_dim: int, d_shared: int, n_entries: int, pool, order,
                     offset, score, d_out, d_pool, d_user, d_score, workspace, workspace_bytes: int, stream=None) -> None:
     """Gradients of ckv_gather by the pool (fp32), the user parts and the scores."""
+    stream = _stream(stream)
+    st = _pycall.gather_grad(_GATHER_GRAD, device, dtype, n, n_groups, head_dim, d_shared, n_entries, pool, order, offset, score, d_out,
+                             d_pool, d_user, d_score, workspace, workspace_bytes, stream or 0)
+    if st is not None:
+        return _check(None, st, "ckv_gather_grad") if st else None
     _check(None, lib.ckv_gather_grad(device, dtype, n, n_groups, head_dim, d_shared, n_entries, _ptr(pool), _ptr(order),
                                      _ptr(offset), _ptr(score), _ptr(d_out), _ptr(d_pool), _ptr(d_user), _ptr(d_score),
                                      _ptr(workspace), int(workspace_bytes), _stream(stream)), "ckv_gather_grad")

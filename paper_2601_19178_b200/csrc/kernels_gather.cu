@@ -22,30 +22,45 @@ __device__ __forceinline__ float widen<uint16_t>(uint16_t v) { return __uint_as_
 
 __device__ __forceinline__ float sigmoid(float x) { return 1.f / (1.f + expf(-x)); }
 
-// One element as a word's low bits, and back, and times a gate (the product rounded once).
-__device__ __forceinline__ uint32_t bits_of(float v) { return __float_as_uint(v); }
-__device__ __forceinline__ uint32_t bits_of(uint16_t v) { return v; }
+// A word (two bf16 or one fp32) times a gate, each product rounded once.
 template <typename E>
 __device__ __forceinline__ uint32_t scaled(uint32_t word, float f)
 {
     if (sizeof(E) == 4) return __float_as_uint(__uint_as_float(word) * f);
     return pack_bf16(__uint_as_float(word << 16) * f, __uint_as_float(word & 0xffff0000u) * f);
 }
+// 16 bytes by loads of LOAD bytes, which is what the address lies on.
+template <int LOAD>
+__device__ __forceinline__ void load16(uint32_t (&w)[4], const void* p)
+{
+    if (LOAD == 16) {
+        const uint4 v = __ldg(reinterpret_cast<const uint4*>(p));
+        w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+    } else if (LOAD == 4) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) w[q] = __ldg(reinterpret_cast<const uint32_t*>(p) + q);
+    } else {
+        const uint16_t* h = reinterpret_cast<const uint16_t*>(p);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) w[q] = __ldg(h + 2 * q) | (uint32_t)__ldg(h + 2 * q + 1) << 16;
+    }
+}
 
-// Lookup.  A warp takes 32 rows at a time: a lane fetches one row's index and score and works out where its pool row lies and the
-// gate; then the lanes run over the rows' 4-byte words side by side, so that loads and stores move whole lines whatever the
-// widths (a pool row of 60 or 62 bytes lies on no wider boundary).  log_words: words of a row, a power of two.
-// WORDS: no word holds elements of both parts, and the arrays lie on words; else element by element.
-template <typename E, bool WORDS>
-__global__ void __launch_bounds__(256) gather_kernel(int64_t rows, int G, int log_words, int skip, int ds, int64_t m, bool store_words,
+// Lookup.  A warp takes up to 32 rows at a time: a lane fetches one row's index and score and works out where its pool row lies and
+// the gate; then the lanes run over the rows' 16-byte pieces side by side.  A pool row of 60 or 62 bytes lies on no wider
+// boundary than a word or an element: LOAD is what all pieces lie on.  log_pieces: of a row; log_rows: rows of a warp, fewer
+// where there are few, so that a warp's chain of loads is short.
+template <typename E, int LOAD>
+__global__ void __launch_bounds__(256) gather_kernel(int64_t rows, int G, int log_pieces, int log_rows, int skip, int ds, int64_t m, int store,
                                                      const E* __restrict__ pool, const int32_t* __restrict__ idx,
                                                      const E* __restrict__ user, const float* __restrict__ score, E* __restrict__ out)
 {
-    constexpr int PER = 4 / (int)sizeof(E);  // elements of a word
-    const int lane = threadIdx.x & 31;
-    const int64_t warps = (int64_t)gridDim.x * 8;
-    for (int64_t r0 = (blockIdx.x * (int64_t)8 + (threadIdx.x >> 5)) * 32; r0 < rows; r0 += warps * 32) {
-        const int n_rows = (int)min(rows - r0, (int64_t)32);
+    constexpr int N = 16 / (int)sizeof(E), PER = 4 / (int)sizeof(E);  // elements of a piece, of a word
+    const int lane = threadIdx.x & 31, bytes = (skip + ds) * (int)sizeof(E);
+    const int64_t step = (int64_t)gridDim.x * 8 << log_rows;
+    grid_dependency_wait();
+    for (int64_t r0 = (blockIdx.x * (int64_t)8 + (threadIdx.x >> 5)) << log_rows; r0 < rows; r0 += step) {
+        const int n_rows = (int)min(rows - r0, (int64_t)1 << log_rows);
         int64_t from = -1;
         float gate = 1.f;
         if (lane < n_rows) {
@@ -53,38 +68,46 @@ __global__ void __launch_bounds__(256) gather_kernel(int64_t rows, int G, int lo
             if (j >= 0 && j < m) from = ((r0 + lane) % G * m + j) * ds;
             if (score) gate = sigmoid(__ldg(score + r0 + lane));
         }
+        char* const to = reinterpret_cast<char*>(out) + r0 * bytes;
 #pragma unroll 4
-        for (int i = 0; i < 1 << log_words; ++i) {
-            const int w = 32 * i + lane, k = w >> log_words, c = (w - (k << log_words)) * PER;
+        for (int i = 0; i < 1 << (log_pieces + log_rows - 5); ++i) {
+            const int w = 32 * i + lane, k = w >> log_pieces, c = (w - (k << log_pieces)) * N;
             const int64_t at = __shfl_sync(0xffffffffu, from, k);
             const float f = __shfl_sync(0xffffffffu, gate, k);
             if (k >= n_rows) continue;
-            const E *u = user + (r0 + k) * skip + c, *p = pool + at + (c - skip);
-            uint32_t v = 0;
-            if (WORDS) {
-                if (c < skip) v = __ldg(reinterpret_cast<const uint32_t*>(u));
-                else if (at >= 0) {
-                    v = __ldg(reinterpret_cast<const uint32_t*>(p));
-                    if (score) v = scaled<E>(v, f);
+            uint32_t v[4] = {};
+            if (at >= 0) {
+                if (c >= skip) load16<LOAD>(v, pool + at + (c - skip));
+                else {  // a piece with elements of both parts, or of the user's alone
+#pragma unroll
+                    for (int q = 0; q < N; ++q)
+                        if (c + q >= skip) {
+                            const E x = __ldg(pool + at + (c + q - skip));
+                            v[q / PER] |= sizeof(E) == 2 ? (uint32_t)(uint16_t)x << (16 * (q % PER)) : __float_as_uint((float)x);
+                        }
                 }
+                if (score)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) v[q] = scaled<E>(v[q], f);
+            }
+            if (c < skip) {
+                const E* u = user + (r0 + k) * skip + c;
+#pragma unroll
+                for (int q = 0; q < N; ++q)
+                    if (c + q < skip) {
+                        const E x = __ldg(u + q);
+                        if (sizeof(E) == 4) v[q / PER] = __float_as_uint((float)x);
+                        else v[q / PER] = (v[q / PER] & (q % PER ? 0xffffu : 0xffff0000u)) | (uint32_t)(uint16_t)x << (16 * (q % PER));
+                    }
+            }
+            char* const o = to + w * 16;
+            if (store == 16) *reinterpret_cast<uint4*>(o) = make_uint4(v[0], v[1], v[2], v[3]);
+            else if (store == 4) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) reinterpret_cast<uint32_t*>(o)[q] = v[q];
             } else {
 #pragma unroll
-                for (int q = 0; q < PER; ++q) {
-                    uint32_t x = 0;
-                    if (c + q < skip) x = bits_of(u[q]);
-                    else if (at >= 0) {
-                        x = bits_of(p[q]);
-                        if (score) x = scaled<E>(x, f);
-                    }
-                    v |= PER == 2 ? (x & 0xffffu) << (16 * q) : x;
-                }
-            }
-            E* o = out + ((r0 << log_words) + w) * PER;
-            if (store_words) *reinterpret_cast<uint32_t*>(o) = v;
-            else {
-                const uint16_t half[2] = {(uint16_t)v, (uint16_t)(v >> 16)};
-#pragma unroll
-                for (int q = 0; q < 2; ++q) reinterpret_cast<uint16_t*>(o)[q] = half[q];
+                for (int q = 0; q < 8; ++q) reinterpret_cast<uint16_t*>(o)[q] = (uint16_t)(v[q / 2] >> (16 * (q % 2)));
             }
         }
     }
@@ -92,65 +115,111 @@ __global__ void __launch_bounds__(256) gather_kernel(int64_t rows, int G, int lo
 
 // ---- sums over runs of equal entries ---------------------------------------------------------------------------
 // The sorted positions of a group are cut into chunks of equal length, whatever the entries.  LANES lanes walk a chunk, 16 bytes of
-// a row each; rows of several chunks travel at a time, kAhead of each.  Runs that lie inside the chunk are written; the one that
-// began before it and the one that goes on behind it leave a partial sum (head, tail), which join_kernel adds up in the
-// order of the chunks.  Nothing depends on the order in which warps run.
-constexpr int kAhead = 4, kSegThreads = 128;
+// a row each.  A run that lies inside the chunk is written; the one that began before it and the one that goes on behind it leave a
+// partial sum (head, tail), which the block joins in the order of its chunks, and of the blocks join_kernel.  Nothing
+// depends on the order in which warps run.
+constexpr int kSegThreads = 128;
 
-template <typename E>
-struct Row16 {  // 16 bytes of a row
-    static constexpr int N = 16 / (int)sizeof(E);
-    E v[N];
-};
-
-template <typename E, int LANES>
-__global__ void __launch_bounds__(kSegThreads) segment_kernel(const SegmentArgs a, float* __restrict__ part, float* __restrict__ wpart,
-                                                              int32_t* __restrict__ goes_on, int chunks, int chunk, int wide)
+// sigmoid(x) and 1 - sigmoid(x)
+__device__ __forceinline__ float2 sigmoids(float x)
 {
-    constexpr int N = Row16<E>::N, PER_BLOCK = kSegThreads / LANES;
-    const int sub = threadIdx.x % LANES, g = blockIdx.y, col0 = sub * N, ds = a.width - a.skip;
-    const int c = blockIdx.x * PER_BLOCK + threadIdx.x / LANES;
-    const bool live = c < chunks;
-    const int32_t *order = a.order + (int64_t)g * a.n, *offset = a.offset + (int64_t)g * (a.m + 1);
-    const int64_t begin = live ? (int64_t)c * chunk : a.n, end = min(begin + chunk, a.n);
-    // the entry of the first position: the last j with offset[j] <= begin (m: no entry)
-    int64_t lo = 0, hi = live ? a.m : 0;
+    const float e = expf(-fabsf(x)), big = 1.f / (1.f + e), small = e * big;
+    return x >= 0.f ? make_float2(big, small) : make_float2(small, big);
+}
+
+// The last j in [lo, hi] with offset[j] <= pos; offset[lo] <= pos.
+__device__ __forceinline__ int64_t entry_of(const int32_t* __restrict__ offset, int64_t pos, int64_t lo, int64_t hi)
+{
     while (lo < hi) {
         const int64_t mid = (lo + hi + 1) / 2;
-        if (__ldg(offset + mid) <= begin) lo = mid;
+        if (__ldg(offset + mid) <= pos) lo = mid;
         else hi = mid - 1;
     }
-    int64_t j = lo, run_end = !live ? a.n : j < a.m ? offset[j + 1] : a.n;
+    return lo;
+}
+// The same by LANES lanes that look at as many places at a time (all lanes of the warp take part).
+template <int LANES>
+__device__ __forceinline__ int64_t entry_of_group(const int32_t* __restrict__ offset, int64_t pos, int64_t hi)
+{
+    const int lane = threadIdx.x & 31, sub = lane % LANES;
+    const unsigned mine = (LANES == 32 ? 0xffffffffu : (1u << LANES % 32) - 1) << (lane - sub);
+    int64_t lo = 0;
+    while (__any_sync(0xffffffffu, lo < hi)) {
+        const int64_t at = lo + ((hi - lo) * (sub + 1) + LANES) / (LANES + 1);  // lo < at <= hi, rising with sub
+        const bool below = lo < hi && __ldg(offset + at) <= pos;
+        const int n = __popc(__ballot_sync(0xffffffffu, below) & mine);         // places at or before the entry
+        const int64_t next = n < LANES ? lo + ((hi - lo) * (n + 1) + LANES) / (LANES + 1) - 1 : hi;
+        if (lo < hi) {
+            if (n > 0) lo = lo + ((hi - lo) * n + LANES) / (LANES + 1);
+            hi = next;
+        }
+    }
+    return lo;
+}
+
+// What a chunk leaves for its block.
+struct Ends {
+    int32_t head, tail;  // entries of the run that began before the chunk, and of the one that began in it and goes on; -1: none
+    bool open;           // the head run goes on behind the chunk
+};
+
+// GATED: pool is given, so that the weight is a sigmoid and d_score is wanted.
+template <typename E, int LANES, bool GATED>
+__global__ void __launch_bounds__(kSegThreads, GATED ? 5 : 6) segment_kernel(const SegmentArgs a, float* __restrict__ part, float* __restrict__ wpart,
+                                                                              int32_t* __restrict__ goes_on, int chunk, int wide)
+{
+    constexpr int N = 16 / (int)sizeof(E), GROUPS = kSegThreads / LANES;  // elements of a lane, chunks of a block
+    constexpr int AHEAD = LANES < 8 ? 4 : 8, PER = AHEAD > LANES ? AHEAD / LANES : 1;  // rows on their way, looked up by a lane
+    constexpr int WIDTH = LANES * N;
+    __shared__ __align__(16) float ends[GROUPS][2][WIDTH];
+    __shared__ float wends[GROUPS][2];
+    __shared__ Ends info[GROUPS];
+    const int lane = threadIdx.x & 31, sub = lane % LANES, grp = threadIdx.x / LANES, g = blockIdx.y, col0 = sub * N, ds = WIDTH - a.skip;
+    const unsigned mine = (LANES == 32 ? 0xffffffffu : (1u << LANES % 32) - 1) << (lane - sub);
+    const int32_t *order = a.order + (int64_t)g * a.n, *offset = a.offset + (int64_t)g * (a.m + 1);
+    const int64_t begin = min(((int64_t)blockIdx.x * GROUPS + grp) * chunk, a.n), end = min(begin + chunk, a.n);
+    const bool live = begin < end;
+    grid_dependency_wait();
+    // the entries of the first and the last position (m: no entry)
+    int64_t j = entry_of_group<LANES>(offset, begin, live ? a.m : 0);
+    const int64_t j_last = entry_of_group<LANES>(offset, end - 1, live ? a.m : 0);
+    int64_t run_end = live && j < a.m ? offset[j + 1] : a.n;
     bool head = live && offset[j] < begin;
+    if (sub == 0) info[grp] = Ends{-1, -1, false};
     float acc[N] = {}, own[N] = {}, wsum = 0.f;
-    const int64_t at = ((int64_t)g * chunks + c) * 2;
     auto fetch_pool = [&] {
-        if (!a.pool) return;
+        if (!GATED) return;
         const E* p = (const E*)a.pool + ((int64_t)g * a.m + j) * ds + col0 - a.skip;
 #pragma unroll
         for (int q = 0; q < N; ++q) own[q] = j < a.m && col0 + q >= a.skip ? widen(__ldg(p + q)) : 0.f;
     };
     auto flush = [&](bool tail) {
         if (j < a.m) {
-            const bool partial = head || tail;
-            float* to = partial ? part + (at + (head ? 0 : 1)) * a.width + col0 : a.sum + ((int64_t)g * a.m + j) * ds + col0 - a.skip;
-            if (partial || wide == 4) {  // whole 16-byte pieces
-                if (partial || col0 >= a.skip) {
-#pragma unroll
-                    for (int q = 0; q < N; q += 4) *reinterpret_cast<float4*>(to + q) = make_float4(acc[q], acc[q + 1], acc[q + 2], acc[q + 3]);
+            if (head || tail) {
+                if (sub == 0) {
+                    if (head) info[grp].head = (int32_t)j, info[grp].open = tail;
+                    else info[grp].tail = (int32_t)j;
+                    wends[grp][head ? 0 : 1] = wsum;
                 }
-            } else if (wide == 2) {
+                float* to = &ends[grp][head ? 0 : 1][col0];
 #pragma unroll
-                for (int q = 0; q < N; q += 2)
-                    if (col0 + q >= a.skip) *reinterpret_cast<float2*>(to + q) = make_float2(acc[q], acc[q + 1]);
+                for (int q = 0; q < N; q += 4) *reinterpret_cast<float4*>(to + q) = make_float4(acc[q], acc[q + 1], acc[q + 2], acc[q + 3]);
             } else {
+                float* to = a.sum + ((int64_t)g * a.m + j) * ds + col0 - a.skip;
+                if (wide == 4) {
+                    if (col0 >= a.skip)
 #pragma unroll
-                for (int q = 0; q < N; ++q)
-                    if (col0 + q >= a.skip) to[q] = acc[q];
-            }
-            if (a.weight_sum && sub == 0) {
-                if (partial) wpart[at + (head ? 0 : 1)] = wsum;
-                else a.weight_sum[(int64_t)g * a.m + j] = wsum;
+                        for (int q = 0; q < N; q += 4) *reinterpret_cast<float4*>(to + q) = make_float4(acc[q], acc[q + 1], acc[q + 2], acc[q + 3]);
+                } else if (wide == 2) {
+#pragma unroll
+                    for (int q = 0; q < N; q += 2)
+                        if (col0 + q >= a.skip) *reinterpret_cast<float2*>(to + q) = make_float2(acc[q], acc[q + 1]);
+                } else {
+#pragma unroll
+                    for (int q = 0; q < N; ++q)
+                        if (col0 + q >= a.skip) to[q] = acc[q];
+                }
+                if (a.weight_sum && sub == 0) a.weight_sum[(int64_t)g * a.m + j] = wsum;
             }
         }
 #pragma unroll
@@ -159,66 +228,123 @@ __global__ void __launch_bounds__(kSegThreads) segment_kernel(const SegmentArgs 
         head = false;
     };
     if (live) fetch_pool();
-    const int64_t last = begin + chunk;  // (chunks of a warp take as many steps each: the lanes stay together)
-    for (int64_t t0 = begin; t0 < last; t0 += kAhead) {
-        int32_t pos[kAhead];
-        uint4 raw[kAhead];
-        float sc[kAhead];
+    // a lane's share of the next rows: position of row `sub` (and `sub` + LANES)
+    int32_t ahead[PER];
+    auto look_ahead = [&](int64_t t0) {
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            pos[k] = t0 + k < end ? __ldg(order + t0 + k) : -1;
-            if (pos[k] >= a.n) pos[k] = -1;  // not an order
+        for (int i = 0; i < PER; ++i) {
+            const int64_t t = t0 + sub + i * LANES;
+            ahead[i] = sub + i * LANES < AHEAD && t < end ? __ldg(order + t) : -1;
         }
+    };
+    look_ahead(begin);
+    for (int64_t t0 = begin; t0 < begin + chunk; t0 += AHEAD) {  // (as many turns for every chunk: a warp's stay together)
+        int32_t pos[PER];
+        float2 gate[PER];  // weight of the row; GATED: and one less it
+        int32_t key[PER];
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            const bool real = pos[k] >= 0;
-            raw[k] = real ? __ldg(reinterpret_cast<const uint4*>((const E*)a.rows + pos[k] * a.stride + g * a.group_stride + col0)) : make_uint4(0, 0, 0, 0);
-            sc[k] = real && a.score ? __ldg(a.score + (int64_t)pos[k] * a.G + g) : 0.f;
+        for (int i = 0; i < PER; ++i) {
+            pos[i] = ahead[i] < a.n ? ahead[i] : -1;  // (not an order)
+            const float sc = pos[i] >= 0 && a.score ? __ldg(a.score + (int64_t)pos[i] * a.G + g) : 0.f;
+            gate[i] = pos[i] < 0 ? make_float2(0.f, 0.f) : !a.score ? make_float2(1.f, 0.f) : GATED ? sigmoids(sc) : make_float2(sc, 0.f);
+            key[i] = (int32_t)j;
         }
+        uint4 raw[AHEAD];
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            const int64_t t = t0 + k;
-            if (t >= run_end && t < end) {
-                flush(false);
-                do {
-                    ++j;
+        for (int k = 0; k < AHEAD; ++k) {
+            const int32_t p = __shfl_sync(0xffffffffu, pos[k / LANES], k % LANES, LANES);
+            raw[k] = p >= 0 ? __ldg(reinterpret_cast<const uint4*>((const E*)a.rows + p * a.stride + g * a.group_stride + col0)) : make_uint4(0, 0, 0, 0);
+        }
+        look_ahead(t0 + AHEAD);
+        const bool mixed = t0 + AHEAD > run_end && j != j_last;
+        if (mixed)
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const int64_t t = t0 + sub + i * LANES;
+                key[i] = (int32_t)entry_of(offset, min(t, end - 1), j, j_last);
+            }
+        const bool any_mixed = __any_sync(0xffffffffu, mixed);
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const int32_t p = __shfl_sync(0xffffffffu, pos[k / LANES], k % LANES, LANES);
+            const float w = __shfl_sync(0xffffffffu, gate[k / LANES].x, k % LANES, LANES);
+            if (any_mixed) {
+                const int32_t here = __shfl_sync(0xffffffffu, key[k / LANES], k % LANES, LANES);
+                if (here != (int32_t)j) {
+                    flush(false);
+                    j = here;
                     run_end = j < a.m ? __ldg(offset + j + 1) : a.n;
-                } while (t >= run_end);
-                fetch_pool();
+                    fetch_pool();
+                }
             }
             const E* v = reinterpret_cast<const E*>(&raw[k]);
-            const bool real = pos[k] >= 0;
-            const float w = !real ? 0.f : !a.score ? 1.f : a.pool ? sigmoid(sc[k]) : sc[k];
             float dot = 0.f;
 #pragma unroll
             for (int q = 0; q < N; ++q) {
                 const float x = widen(v[q]);
-                if (real) acc[q] = fmaf(w, x, acc[q]);
-                dot = fmaf(own[q], x, dot);
+                if (p >= 0) acc[q] = fmaf(w, x, acc[q]);
+                if (GATED) dot = fmaf(own[q], x, dot);
             }
             wsum += w;
-            const int64_t o = (int64_t)pos[k] * a.G + g;
-            if (a.d_user && real && col0 < a.skip) {
+            if (a.d_user && p >= 0 && col0 < a.skip) {
+                E* to = (E*)a.d_user + ((int64_t)p * a.G + g) * a.skip + col0;
 #pragma unroll
                 for (int q = 0; q < N; ++q)
-                    if (col0 + q < a.skip) ((E*)a.d_user)[o * a.skip + col0 + q] = v[q];
+                    if (col0 + q < a.skip) to[q] = v[q];
             }
-            if (a.d_score) {
+            if (GATED && a.d_score) {
+                const float less = __shfl_sync(0xffffffffu, gate[k / LANES].y, k % LANES, LANES);
 #pragma unroll
                 for (int d = LANES / 2; d > 0; d /= 2) dot += __shfl_xor_sync(0xffffffffu, dot, d);
-                if (sub == 0 && real) a.d_score[o] = j < a.m ? dot * w * sigmoid(-sc[k]) : 0.f;
+                if (sub == 0 && p >= 0) a.d_score[(int64_t)p * a.G + g] = j < a.m ? dot * w * less : 0.f;
             }
         }
     }
-    if (!live) return;
-    const bool tail = run_end > end;
-    if (sub == 0) goes_on[(int64_t)g * chunks + c] = tail && !head && j < a.m ? (int32_t)j : -1;  // began here, ends in a later chunk
-    flush(tail);
+    __syncwarp(mine);
+    if (live) flush(j < a.m && offset[j + 1] > end);
+    __syncthreads();
+    // the block's chunks in their order, a thread per column (and one for the weights)
+    const int col = threadIdx.x;
+    const int64_t block = (int64_t)g * gridDim.x + blockIdx.x;
+    const bool weights = col == WIDTH % kSegThreads && a.weight_sum;  // (rows of 128 columns have no thread left: their first one does both)
+    for (int pass = 0; pass < 2; ++pass) {
+        if (pass == 0 ? col >= WIDTH : !weights) continue;
+        float sum = 0.f;
+        int32_t open = -1;
+        bool before = false;  // the open run began before the block
+        auto close = [&](int32_t e, int which) {
+            if (which < 0) {
+                if (pass) a.weight_sum[(int64_t)g * a.m + e] = sum;
+                else if (col >= a.skip) a.sum[((int64_t)g * a.m + e) * ds + col - a.skip] = sum;
+            } else if (pass) wpart[block * 2 + which] = sum;
+            else part[(block * 2 + which) * WIDTH + col] = sum;
+        };
+        for (int c = 0; c < GROUPS; ++c) {
+            const Ends e = info[c];
+            if (e.head >= 0) {
+                if (open < 0) before = true, sum = 0.f;
+                sum += pass ? wends[c][0] : ends[c][0][col];
+                open = e.head;
+                if (!e.open) {
+                    close(open, before ? 0 : -1);
+                    open = -1;
+                }
+            }
+            if (e.tail >= 0) {
+                open = e.tail;
+                before = false;
+                sum = pass ? wends[c][1] : ends[c][1][col];
+            }
+        }
+        if (open >= 0) close(open, before ? 0 : 1);
+        if (pass == 0 && col == 0) goes_on[block] = open >= 0 && !before ? open : -1;  // began in this block, ends in a later one
+    }
 }
 
-// Blocks of the first kind: the runs that began in chunk c and go on behind it, a warp per chunk; runs of many chunks by the whole block,
-// an eighth of the chunks per warp.  Blocks of the second kind: entries without a position.
-constexpr int kJoinWarps = 8, kLongRun = 16;
+// `chunks` of `chunk` positions are the blocks of segment_kernel here.  Blocks of the first kind: the runs that began in chunk c and go on
+// behind it, a warp per chunk; runs of many chunks by the whole block, an eighth of the chunks per warp.  Blocks of the second
+// kind: entries without a position.
+constexpr int kJoinWarps = 8, kLongRun = 8;
 __global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const SegmentArgs a, const float* __restrict__ part, const float* __restrict__ wpart,
                                                                const int32_t* __restrict__ goes_on, int chunks, int chunk, int join_blocks)
 {
@@ -226,6 +352,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const SegmentArgs
     __shared__ int32_t entry[kJoinWarps], upto[kJoinWarps];
     const int g = blockIdx.y, ds = a.width - a.skip, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int32_t* offset = a.offset + (int64_t)g * (a.m + 1);
+    grid_dependency_wait();
     if ((int)blockIdx.x >= join_blocks) {
         const int64_t j0 = ((int64_t)((int)blockIdx.x - join_blocks) * kJoinWarps + warp) * 32, j = j0 + lane;
         unsigned empty = __ballot_sync(0xffffffffu, j < a.m && __ldg(offset + min(j, a.m)) == __ldg(offset + min(j + 1, a.m)));
@@ -236,7 +363,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const SegmentArgs
     }
     // columns lane, lane + 32, ... of the head parts of chunks [from, to), and (column `width`) of the weights
     auto add_heads = [&](int from, int to, float (&sum)[5]) {
-#pragma unroll 4
+#pragma unroll 8
         for (int k = from; k < to; ++k) {
             const float* p = part + ((int64_t)g * chunks + k) * 2 * a.width;
 #pragma unroll
@@ -304,37 +431,40 @@ int chunk_of(int64_t n, int G)
     while (c < 128 && n * G / c > 16384) c *= 2;
     return c;
 }
+// of a block: kSegThreads / lanes chunks
+int64_t block_of(int64_t n, int G, int width, int elem) { return (int64_t)chunk_of(n, G) * kSegThreads * 16 / (width * elem); }
 
 struct SegmentSpace {
     float *part, *wpart;
     int32_t* goes_on;
     int64_t bytes;
-    SegmentSpace(void* ws, int64_t n, int G, int width)
+    SegmentSpace(void* ws, int64_t n, int G, int width, int elem)
     {
         Carve c(ws);
-        const int64_t chunk = chunk_of(n, G), chunks = (n + chunk - 1) / chunk;
-        part = c.take<float>(chunks * G * 2 * width);
-        wpart = c.take<float>(chunks * G * 2);
-        goes_on = c.take<int32_t>(chunks * G);
+        const int64_t block = block_of(n, G, width, elem), blocks = (n + block - 1) / block;
+        part = c.take<float>(blocks * G * 2 * width);
+        wpart = c.take<float>(blocks * G * 2);
+        goes_on = c.take<int32_t>(blocks * G);
         bytes = c.used;
     }
 };
 
 template <typename E>
-cudaError_t launch_segments(const SegmentArgs& a, const SegmentSpace& sp, int chunks, int chunk, int wide, cudaStream_t s)
+cudaError_t launch_segments(const SegmentArgs& a, const SegmentSpace& sp, int blocks, int wide, cudaStream_t s)
 {
-    const Launch l{s, nullptr, nullptr};
-    auto go = [&](auto kernel, int lanes) {
-        const int per_block = kSegThreads / lanes;
-        return launch_kernel(l, kernel, dim3((unsigned)((chunks + per_block - 1) / per_block), (unsigned)a.G), kSegThreads, 0, 1, a, sp.part, sp.wpart,
-                             sp.goes_on, chunks, chunk, wide);
+    auto go = [&](auto gated, auto plain) {
+        return launch_kernel(Launch{s, nullptr, nullptr, true}, a.pool ? gated : plain, dim3((unsigned)blocks, (unsigned)a.G), kSegThreads, 0, 1, a, sp.part,
+                             sp.wpart, sp.goes_on, chunk_of(a.n, a.G), wide);
     };
     switch (a.width * (int)sizeof(E)) {
-        case 32: return go(segment_kernel<E, 2>, 2);
-        case 64: return go(segment_kernel<E, 4>, 4);
-        case 128: return go(segment_kernel<E, 8>, 8);
-        case 256: return go(segment_kernel<E, 16>, 16);
-        default: return go(segment_kernel<E, 32>, 32);
+        case 32:
+            if constexpr (sizeof(E) == 2) return go(segment_kernel<E, 2, true>, segment_kernel<E, 2, false>);
+        case 64: return go(segment_kernel<E, 4, true>, segment_kernel<E, 4, false>);
+        case 128: return go(segment_kernel<E, 8, true>, segment_kernel<E, 8, false>);
+        case 256: return go(segment_kernel<E, 16, true>, segment_kernel<E, 16, false>);
+        default:
+            if constexpr (sizeof(E) == 4) return go(segment_kernel<E, 32, true>, segment_kernel<E, 32, false>);
+            return cudaErrorInvalidValue;
     }
 }
 
@@ -342,13 +472,21 @@ template <typename E>
 cudaError_t launch_gather_t(int64_t n, int G, int D, int ds, int64_t m, const void* pool, const int32_t* idx, const void* user,
                             const float* score, void* out, cudaStream_t s)
 {
-    const int skip = D - ds, per = 4 / (int)sizeof(E);
-    const bool words = skip % per == 0 && (((uintptr_t)pool | (uintptr_t)user) & 3) == 0;
-    int log_words = 0;
-    while (per << log_words < D) ++log_words;
-    const int64_t blocks = std::min<int64_t>((n * G + 255) / 256, 148 * 8);
-    return launch_kernel(Launch{s, nullptr, nullptr}, words ? gather_kernel<E, true> : gather_kernel<E, false>, dim3((unsigned)blocks), 256, 0, 1, n * G, G,
-                         log_words, skip, ds, m, ((uintptr_t)out & 3) == 0, (const E*)pool, idx, (const E*)user, score, (E*)out);
+    constexpr int e = (int)sizeof(E);
+    const int skip = D - ds;
+    auto lies_on = [](const void* p, int step) { return ((uintptr_t)p | (uintptr_t)step) % 16 == 0 ? 16 : ((uintptr_t)p | (uintptr_t)step) % 4 == 0 ? 4 : 2; };
+    const int load = std::min(lies_on(pool, ds * e), lies_on(nullptr, skip * e)), store = lies_on(out, 16);
+    int log_pieces = 0, log_rows = 5;
+    while (16 << log_pieces < D * e) ++log_pieces;
+    while (log_pieces + log_rows > 5 && log_rows > 0 && (n * G >> log_rows) < 148 * 32) --log_rows;
+    const int64_t per_block = (int64_t)8 << log_rows, blocks = std::min<int64_t>((n * G + per_block - 1) / per_block, 148 * 8);
+    auto go = [&](auto kernel) {
+        return launch_kernel(Launch{s, nullptr, nullptr, true}, kernel, dim3((unsigned)blocks), 256, 0, 1, n * G, G, log_pieces, log_rows, skip, ds, m, store,
+                             (const E*)pool, idx, (const E*)user, score, (E*)out);
+    };
+    if constexpr (e == 2)
+        if (load == 2) return go(gather_kernel<E, 2>);
+    return load == 16 ? go(gather_kernel<E, 16>) : go(gather_kernel<E, 4>);
 }
 
 }  // namespace
@@ -360,21 +498,26 @@ cudaError_t launch_gather(int dtype, int64_t n, int G, int D, int ds, int64_t m,
                             : launch_gather_t<uint16_t>(n, G, D, ds, m, pool, idx, user, score, out, s);
 }
 
-int64_t segment_workspace(int64_t n, int G, int width) { return SegmentSpace(nullptr, n, G, width).bytes; }
+int64_t segment_workspace(int64_t n, int G, int width)  // of either type: the longer blocks are those of 16-bit elements
+{
+    return std::max(SegmentSpace(nullptr, n, G, width, 2).bytes, SegmentSpace(nullptr, n, G, width, 4).bytes);
+}
 
 cudaError_t launch_segment_sum(int dtype, const SegmentArgs& a, void* ws, cudaStream_t s)
 {
-    const SegmentSpace sp(ws, a.n, a.G, a.width);
-    const int chunk = chunk_of(a.n, a.G), chunks = (int)((a.n + chunk - 1) / chunk), ds = a.width - a.skip;
+    const int elem = dtype == CKV_F32 ? 4 : 2, ds = a.width - a.skip;
+    const SegmentSpace sp(ws, a.n, a.G, a.width, elem);
+    const int64_t block = block_of(a.n, a.G, a.width, elem);
+    const int blocks = (int)((a.n + block - 1) / block);
     // floats of a sum's row that can be stored at a time
-    const int wide = ((uintptr_t)a.sum & 15) == 0 && ds % 4 == 0 && a.skip % (dtype == CKV_F32 ? 4 : 8) == 0 ? 4
+    const int wide = ((uintptr_t)a.sum & 15) == 0 && ds % 4 == 0 && a.skip % (16 / elem) == 0 ? 4
                      : ((uintptr_t)a.sum & 7) == 0 && ds % 2 == 0 && a.skip % 2 == 0 ? 2 : 1;
     cudaError_t e = cudaSuccess;
-    if (chunks > 0) e = dtype == CKV_F32 ? launch_segments<float>(a, sp, chunks, chunk, wide, s) : launch_segments<uint16_t>(a, sp, chunks, chunk, wide, s);
-    const int join_blocks = (chunks + kJoinWarps - 1) / kJoinWarps, empty_blocks = (int)((a.m + 32 * kJoinWarps - 1) / (32 * kJoinWarps));
+    if (blocks > 0) e = dtype == CKV_F32 ? launch_segments<float>(a, sp, blocks, wide, s) : launch_segments<uint16_t>(a, sp, blocks, wide, s);
+    const int join_blocks = (blocks + kJoinWarps - 1) / kJoinWarps, empty_blocks = (int)((a.m + 32 * kJoinWarps - 1) / (32 * kJoinWarps));
     if (e == cudaSuccess)
-        e = launch_kernel(Launch{s, nullptr, nullptr}, join_kernel, dim3((unsigned)(join_blocks + empty_blocks), (unsigned)a.G), 32 * kJoinWarps, 0, 1, a, sp.part,
-                          sp.wpart, sp.goes_on, chunks, chunk, join_blocks);
+        e = launch_kernel(Launch{s, nullptr, nullptr, true}, join_kernel, dim3((unsigned)(join_blocks + empty_blocks), (unsigned)a.G), 32 * kJoinWarps, 0, 1, a,
+                          sp.part, sp.wpart, sp.goes_on, blocks, (int)block, join_blocks);
     return e;
 }
 

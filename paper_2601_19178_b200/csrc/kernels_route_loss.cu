@@ -80,31 +80,35 @@ Space layout(void* ws, int64_t n, int G, int d, int64_t m, bool grad)
 }
 
 // ---- what the passes read
-__global__ void __launch_bounds__(256) entries_kernel(const float* __restrict__ bias, const float* __restrict__ mean,
-                                                      const int32_t* __restrict__ offset, float w_balance, int64_t m, int64_t mp,
-                                                      const Space s)
+__device__ __forceinline__ void prepare_entry(const RouteLossArgs& a, const RouteGradArgs& b, const Space& s, int64_t mp, int g, int64_t j)
 {
-    const int64_t j = blockIdx.x * (int64_t)256 + threadIdx.x;
-    const int g = blockIdx.y;
     if (j == 0 && s.done) s.done[g] = 0;
     if (j >= mp) return;
-    const float b = j < m ? (bias ? bias[g * m + j] : 0.f) : -CUDART_INF_F;
-    s.b[g * mp + j] = b;
-    put_step(s.b_step, g * mp + j, b);
+    const float bias = j < a.m ? (a.bias ? a.bias[g * a.m + j] : 0.f) : -CUDART_INF_F;
+    s.b[g * mp + j] = bias;
+    put_step(s.b_step, g * mp + j, bias);
     if (!s.h) return;
-    const float u = j < m ? mean[g * m + j] * (float)m : 0.f;
-    const int32_t rows = offset[g * (m + 1) + m];
+    const float u = j < a.m ? a.mean[g * a.m + j] * (float)a.m : 0.f;
+    const int32_t rows = b.offset[g * (a.m + 1) + a.m];
     // (an entry that no position gives any weight has p = 0 everywhere, and no gradient)
-    s.h[g * mp + j] = u > 0.f ? w_balance / (float)max(rows, 1) * logf(u) : 0.f;
+    s.h[g * mp + j] = u > 0.f ? b.w_balance / (float)max(rows, 1) * logf(u) : 0.f;
 }
 
 // Positions: x for the passes (zeros for one that takes part in no group, whose inputs may be anything); forward: the picked entry's
-// score; gradient: -lse and the picked entry's coefficient.  A position to D / 8 lanes, 16 bytes of it to each.
+// score; gradient: -lse and the picked entry's coefficient.  A position to D / 8 lanes, 16 bytes of it to each.  The first
+// `entry_blocks` blocks, as many for each group, prepare the entries instead.
 template <int D, bool GRAD>
-__global__ void __launch_bounds__(256) positions_kernel(const RouteLossArgs a, const RouteGradArgs b, const Space s, int64_t np, bool whole)
+__global__ void __launch_bounds__(256) prepare_kernel(const RouteLossArgs a, const RouteGradArgs b, const Space s, int64_t np, int64_t mp,
+                                                      int entry_blocks, bool whole)
 {
     constexpr int LANES = D / 8;
-    const int64_t i = blockIdx.x * (int64_t)(256 / LANES) + threadIdx.x / LANES;
+    grid_dependency_wait();
+    if ((int)blockIdx.x < entry_blocks) {
+        const int per_group = entry_blocks / a.G;
+        prepare_entry(a, b, s, mp, (int)blockIdx.x / per_group, (int64_t)((int)blockIdx.x % per_group) * 256 + threadIdx.x);
+        return;
+    }
+    const int64_t i = (int64_t)((int)blockIdx.x - entry_blocks) * (256 / LANES) + threadIdx.x / LANES;
     const int sub = threadIdx.x % LANES;
     const bool there = i < a.n;
     uint4 raw = make_uint4(0, 0, 0, 0);
@@ -168,24 +172,32 @@ __global__ void __launch_bounds__(256) positions_kernel(const RouteLossArgs a, c
 }
 
 // ---- joins
-__device__ double block_sum(double v)
+// Sums over the 256 threads of a block, in a fixed order.
+template <int N>
+__device__ __forceinline__ void block_sum(double (&v)[N])
 {
-    __shared__ double part[8];
+    __shared__ double part[N][8];
     __syncthreads();
 #pragma unroll
-    for (int d = 16; d > 0; d /= 2) v += __shfl_xor_sync(0xffffffffu, v, d);
-    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
-    __syncthreads();
-    double t = 0;
+    for (int k = 0; k < N; ++k) {
 #pragma unroll
-    for (int w = 0; w < 8; ++w) t += part[w];
-    return t;
+        for (int d = 16; d > 0; d /= 2) v[k] += __shfl_xor_sync(0xffffffffu, v[k], d);
+        if ((threadIdx.x & 31) == 0) part[k][threadIdx.x >> 5] = v[k];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        v[k] = 0;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) v[k] += part[k][w];
+    }
 }
 
 __global__ void __launch_bounds__(256) lse_join_kernel(const RouteLossArgs a, const SweepArgs p, const Space s)
 {
     const int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x;
     const int g = blockIdx.y;
+    grid_dependency_wait();
     const int32_t k = i < a.n ? __ldg(a.idx + i * a.G + g) : -1;
     const bool real = k >= 0 && k < a.m;
     float lse = 0.f, neg = -CUDART_INF_F;
@@ -214,12 +226,13 @@ __global__ void __launch_bounds__(256) lse_join_kernel(const RouteLossArgs a, co
     }
     if (i < a.n) a.lse[i * a.G + g] = lse;
     const int rows = __syncthreads_count(real), live = __syncthreads_count(neg != -CUDART_INF_F);
-    soft = block_sum(soft);
+    double sum1[1] = {soft};
+    block_sum(sum1);
     if (threadIdx.x == 0) {
         const int64_t at = (int64_t)g * gridDim.x + blockIdx.x;
         s.rows_part[at] = rows;
         s.live_part[at] = live;
-        s.peak_part[at] = soft;
+        s.peak_part[at] = sum1[0];
     }
 }
 
@@ -231,44 +244,53 @@ __global__ void __launch_bounds__(256) mean_join_kernel(const RouteLossArgs a, c
 {
     __shared__ bool last;
     const int g = blockIdx.y;
-    double rows = 0;
-    for (int b = threadIdx.x; b < blocks; b += 256) rows += s.rows_part[(int64_t)g * blocks + b];
-    rows = block_sum(rows);
+    grid_dependency_wait();
+    // what the last block wants is asked for at once by all
+    double of_rows[3] = {};  // positions that take part, those with a weight, peak losses
+    for (int b = threadIdx.x; b < blocks; b += 256) {
+        of_rows[0] += s.rows_part[(int64_t)g * blocks + b];
+        of_rows[1] += s.live_part[(int64_t)g * blocks + b];
+        of_rows[2] += s.peak_part[(int64_t)g * blocks + b];
+    }
+    float sum[kMeanEntries / 256];
+#pragma unroll
+    for (int q = 0; q < kMeanEntries / 256; ++q) {
+        const int64_t j = blockIdx.x * (int64_t)kMeanEntries + q * 256 + threadIdx.x;
+        sum[q] = 0.f;
+        if (j < a.m)
+#pragma unroll 4
+            for (int z = 0; z < p.splits; ++z) sum[q] += p.part[((int64_t)z * a.G + g) * p.mp + j];
+    }
+    block_sum(of_rows);
+    const double rows = of_rows[0];
     const float inv = rows > 0 ? (float)(1.0 / rows) : 0.f;
-    double balance = 0;
+    double balance[1] = {};
 #pragma unroll
     for (int q = 0; q < kMeanEntries / 256; ++q) {
         const int64_t j = blockIdx.x * (int64_t)kMeanEntries + q * 256 + threadIdx.x;
         if (j >= a.m) continue;
-        float sum = 0.f;
-        for (int z = 0; z < p.splits; ++z) sum += p.part[((int64_t)z * a.G + g) * p.mp + j];
-        const float mean = sum * inv;
+        const float mean = sum[q] * inv;
         a.mean[(int64_t)g * a.m + j] = mean;
         const double u = (double)mean * (double)a.m;
-        balance += (u > 0 ? u * log(u) : u * 0) - u + 1;
+        balance[0] += (u > 0 ? u * log(u) : u * 0) - u + 1;
     }
-    balance = block_sum(balance);
+    block_sum(balance);
     if (threadIdx.x == 0) {
-        s.balance_part[(int64_t)g * gridDim.x + blockIdx.x] = balance;
+        s.balance_part[(int64_t)g * gridDim.x + blockIdx.x] = balance[0];
         __threadfence();
         last = atomicAdd(s.done + g, 1u) + 1 == gridDim.x;
         __threadfence();
     }
     __syncthreads();
     if (!last) return;
-    double peak = 0, live = 0;
-    for (int b = threadIdx.x; b < blocks; b += 256) {
-        live += s.live_part[(int64_t)g * blocks + b];
-        peak += s.peak_part[(int64_t)g * blocks + b];
+    if (gridDim.x > 1) {
+        balance[0] = 0;
+        for (int b = threadIdx.x; b < (int)gridDim.x; b += 256) balance[0] += *(volatile double*)(s.balance_part + (int64_t)g * gridDim.x + b);
+        block_sum(balance);
     }
-    balance = 0;
-    for (int b = threadIdx.x; b < (int)gridDim.x; b += 256) balance += *(volatile double*)(s.balance_part + (int64_t)g * gridDim.x + b);
-    live = block_sum(live);
-    peak = block_sum(peak);
-    balance = block_sum(balance);
     if (threadIdx.x == 0) {
-        a.loss[2 * g] = rows > 0 ? (float)(balance / (double)a.m + (live - rows) / rows) : 0.f;
-        a.loss[2 * g + 1] = rows > 0 ? (float)(peak / rows) : 0.f;
+        a.loss[2 * g] = rows > 0 ? (float)(balance[0] / (double)a.m + (of_rows[1] - rows) / rows) : 0.f;
+        a.loss[2 * g + 1] = rows > 0 ? (float)(of_rows[2] / rows) : 0.f;
     }
 }
 
@@ -276,9 +298,11 @@ __global__ void __launch_bounds__(256) r_join_kernel(const SweepArgs p, float* _
 {
     const int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x;
     const int g = blockIdx.y;
+    grid_dependency_wait();
     if (i >= p.np) return;
     float sum = 0.f;
     if (i < p.n)
+#pragma unroll 4
         for (int z = 0; z < p.splits; ++z) sum += p.part[((int64_t)z * p.G + g) * p.np + i];
     nr[g * p.np + i] = -sum;
 }
@@ -304,6 +328,7 @@ __device__ __forceinline__ void put8(uint16_t* out, const float (&v)[8], bool wh
 __global__ void __launch_bounds__(256) dx_join_kernel(const RouteLossArgs a, const RouteGradArgs b, const SweepArgs p, const float* __restrict__ ds)
 {
     const int64_t e = (blockIdx.x * (int64_t)256 + threadIdx.x) * 8, total = a.n * a.d;
+    grid_dependency_wait();
     if (e >= total) return;
     const int64_t i = e / a.d;
     const int c = (int)(e - i * a.d);
@@ -330,6 +355,7 @@ __global__ void __launch_bounds__(256) dx_join_kernel(const RouteLossArgs a, con
 __global__ void __launch_bounds__(256) dw_join_kernel(const RouteLossArgs a, const RouteGradArgs b, const SweepArgs p, const Space s)
 {
     const int64_t e = (blockIdx.x * (int64_t)256 + threadIdx.x) * 8, total = a.G * a.m * a.d;
+    grid_dependency_wait();
     if (e >= total) return;
     float v[8] = {};
     add8(v, s.sum + e);
@@ -345,12 +371,13 @@ __global__ void __launch_bounds__(256) dw_join_kernel(const RouteLossArgs a, con
 }
 
 template <bool GRAD>
-cudaError_t launch_positions(const RouteLossArgs& a, const RouteGradArgs& b, const Space& s, int64_t rows, int64_t np, cudaStream_t st)
+cudaError_t launch_prepare(const RouteLossArgs& a, const RouteGradArgs& b, const Space& s, int64_t rows, int64_t np, int64_t mp, cudaStream_t st)
 {
     const bool whole = ((uintptr_t)a.x & 15) == 0;
-    return launch_kernel(Launch{st, nullptr, nullptr},
-                         a.d == 32 ? positions_kernel<32, GRAD> : a.d == 64 ? positions_kernel<64, GRAD> : positions_kernel<128, GRAD>,
-                         dim3((unsigned)((rows * (a.d / 8) + 255) / 256)), 256, 0, 1, a, b, s, np, whole);
+    const int entry_blocks = (int)((mp + 255) / 256) * a.G;
+    return launch_kernel(Launch{st, nullptr, nullptr, true},
+                         a.d == 32 ? prepare_kernel<32, GRAD> : a.d == 64 ? prepare_kernel<64, GRAD> : prepare_kernel<128, GRAD>,
+                         dim3((unsigned)(entry_blocks + (rows * (a.d / 8) + 255) / 256)), 256, 0, 1, a, b, s, np, mp, entry_blocks, whole);
 }
 
 SweepArgs pass_args(const RouteLossArgs& a, const Space& s)
@@ -373,10 +400,9 @@ cudaError_t launch_route_loss(const RouteLossArgs& a, void* ws, cudaStream_t st)
 {
     const Space s = layout(ws, a.n, a.G, a.d, a.m, false);
     SweepArgs p = pass_args(a, s);
-    const Launch l{st, nullptr, nullptr};
+    const Launch l{st, nullptr, nullptr, true};
     const unsigned blocks = (unsigned)((p.np + 255) / 256), G = (unsigned)a.G;
-    TRY(launch_kernel(l, entries_kernel, dim3((unsigned)((p.mp + 255) / 256), G), 256, 0, 1, a.bias, nullptr, nullptr, 0.f, a.m, p.mp, s));
-    if (a.n) TRY(launch_positions<false>(a, RouteGradArgs{}, s, a.n, p.np, st));
+    TRY(launch_prepare<false>(a, RouteGradArgs{}, s, a.n, p.np, p.mp, st));
     TRY(launch_sweep(SWEEP_LSE, a.d, p, st));
     if (a.n) TRY(launch_kernel(l, lse_join_kernel, dim3(blocks, G), 256, 0, 1, a, p, s));
     TRY(launch_sweep(SWEEP_MEAN, a.d, p, st));
@@ -387,10 +413,9 @@ cudaError_t launch_route_grad(const RouteLossArgs& a, const RouteGradArgs& b, vo
 {
     const Space s = layout(ws, a.n, a.G, a.d, a.m, true);
     SweepArgs p = pass_args(a, s);
-    const Launch l{st, nullptr, nullptr};
+    const Launch l{st, nullptr, nullptr, true};
     const unsigned G = (unsigned)a.G;
-    TRY(launch_kernel(l, entries_kernel, dim3((unsigned)((p.mp + 255) / 256), G), 256, 0, 1, a.bias, a.mean, b.offset, b.w_balance, a.m, p.mp, s));
-    if (a.n) TRY(launch_positions<true>(a, b, s, p.np, p.np, st));
+    TRY(launch_prepare<true>(a, b, s, a.n ? p.np : 0, p.np, p.mp, st));
     SegmentArgs seg{};
     seg.order = b.order;
     seg.offset = b.offset;

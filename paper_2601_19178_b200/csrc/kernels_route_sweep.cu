@@ -343,6 +343,7 @@ __global__ void __launch_bounds__(kSweepThreads, 1) sweep_kernel(const __grid_co
     tc_before();
     __syncthreads();
     tc_after();
+    grid_dependency_wait();
     const uint32_t tmem = tmem_slot;
     if (warp < 4 * n_blocks) {
         if (e == 0) store_ones(tmem + lane_base + L::COL_ONES);
@@ -568,6 +569,7 @@ __global__ void __launch_bounds__(Grad<DIN>::THREADS, 1) grad_kernel(const __gri
     tc_before();
     __syncthreads();
     tc_after();
+    grid_dependency_wait();
     const uint32_t tmem = tmem_slot, tblock = tmem + (uint32_t)e * L::COL_BLOCK;
     if (warp < 4) store_ones(tmem + lane_base + L::COL_ONES);
     if (warp < 8 * n_blocks && buf == 0)
@@ -740,18 +742,18 @@ __global__ void __launch_bounds__(Grad<DIN>::THREADS, 1) grad_kernel(const __gri
 
 struct Shape {
     int rows, tile;     // standing rows of a CTA, streaming rows of a tile
-    int64_t start;      // what a CTA costs besides its tiles, in tiles
+    double start, join; // what a CTA costs besides its tiles, and what a further split costs, in tiles
 };
 Shape shape_of(int d, int mode)
 {
-    if (mode == SWEEP_DX || mode == SWEEP_DW) return Shape{d == 128 ? 128 : 256, 64, 8};
-    return Shape{kRows, d == 128 ? 96 : 128, 4};
+    if (mode == SWEEP_DX || mode == SWEEP_DW) return Shape{d == 128 ? 128 : 256, 64, 8, 0.5};
+    return Shape{kRows, d == 128 ? 96 : 128, 4, 0.25};
 }
 
 template <int DIN>
 cudaError_t launch_t(int mode, const SweepArgs& a, const CUtensorMap& map, dim3 grid, cudaStream_t s)
 {
-    const Launch l{s, nullptr, nullptr};
+    const Launch l{s, nullptr, nullptr, true};
     switch (mode) {
         case SWEEP_LSE: return launch_kernel(l, sweep_kernel<DIN, SWEEP_LSE>, grid, kSweepThreads, Sweep<DIN>::SMEM, 1, map, a);
         case SWEEP_MEAN: return launch_kernel(l, sweep_kernel<DIN, SWEEP_MEAN>, grid, kSweepThreads, Sweep<DIN>::SMEM, 1, map, a);
@@ -772,9 +774,10 @@ int sweep_splits(int64_t n, int G, int d, int64_t m, int mode)
     const int64_t blocks = ((entries ? m : n) + sh.rows - 1) / sh.rows * (mode == SWEEP_DX ? 1 : G);
     const int64_t tiles = ((entries ? n : m) + sh.tile - 1) / sh.tile * groups;
     int best = 1;
-    int64_t best_cost = INT64_MAX;
+    double best_cost = 1e300;
     for (int sp = 1; sp <= kSweepMaxSplits && sp <= std::max<int64_t>(tiles, 1); ++sp) {
-        const int64_t rounds = (blocks * sp + 147) / 148, cost = rounds * ((tiles + sp - 1) / sp + sh.start);
+        const int64_t rounds = (blocks * sp + 147) / 148;
+        const double cost = rounds * ((double)((tiles + sp - 1) / sp) + sh.start) + sh.join * sp;
         if (cost < best_cost) {
             best_cost = cost;
             best = sp;

@@ -37,6 +37,7 @@ __global__ void __launch_bounds__(256) count_kernel(const Pass p, int32_t* __res
     extern __shared__ int32_t bins[];
     const int g = blockIdx.y;
     for (int j = threadIdx.x; j < p.stride; j += 256) bins[j] = 0;
+    grid_dependency_wait();
     __syncthreads();
     const int64_t begin = blockIdx.x * p.chunk, end = min(begin + p.chunk, p.n);
     uint32_t* keys = p.key + (int64_t)g * p.n;
@@ -58,6 +59,7 @@ __device__ __forceinline__ int4 operator+(int4 a, int4 b) { return make_int4(a.x
 __global__ void __launch_bounds__(64) chunk_scan_kernel(int32_t* __restrict__ table, int32_t* __restrict__ total, int chunks, int stride)
 {
     const int j = (blockIdx.x * 64 + threadIdx.x) * 4, g = blockIdx.y;
+    grid_dependency_wait();
     if (j >= stride) return;
     int32_t* t = table + (int64_t)g * chunks * stride + j;
     int4 sum = make_int4(0, 0, 0, 0);
@@ -106,6 +108,7 @@ __global__ void __launch_bounds__(1024) bin_scan_kernel(int32_t* __restrict__ to
     const int g = blockIdx.x;
     int32_t* t = total + (int64_t)g * stride;
     int32_t carry = 0;
+    grid_dependency_wait();
     for (int j0 = 0; j0 < bins; j0 += 4096) {
         const int j = j0 + threadIdx.x * 4;
         const int4 v = j < stride ? *reinterpret_cast<int4*>(t + j) : make_int4(0, 0, 0, 0);
@@ -121,22 +124,24 @@ __global__ void __launch_bounds__(1024) bin_scan_kernel(int32_t* __restrict__ to
     }
 }
 
-// One warp's turn with 32 positions: the place of each, next[] moved on.  Lanes with equal keys stay in order; the additions of successive
-// turns are made in order as well, so that a turn need not wait for the one before.
-__device__ __forceinline__ int32_t take_places(int32_t* next, int d)  // d < 0: none
+// One warp's turn with 32 positions: the place of each, next[] moved on.  Lanes with equal keys (`same`) stay in order.  The warp has
+// next[] to itself: a read, and a write by one lane of each key (with shared-memory additions instead, of which the results
+// were awaited at the end, a turn took 600 clocks).
+__device__ __forceinline__ int32_t take_places(volatile int32_t* next, int d, unsigned same)  // d < 0: none
 {
     const int lane = threadIdx.x & 31;
-    const unsigned same = __match_any_sync(0xffffffffu, d);
-    const int leader = __ffs(same) - 1;
     int32_t at = 0;
-    if (d >= 0 && lane == leader) at = atomicAdd(next + d, __popc(same));
-    return __shfl_sync(0xffffffffu, at, leader) + __popc(same & ((1u << lane) - 1));
+    if (d >= 0) at = next[d];
+    if (d >= 0 && lane == __ffs(same) - 1) next[d] = at + __popc(same);
+    __syncwarp();
+    return at + __popc(same & ((1u << lane) - 1));
 }
 
 __global__ void __launch_bounds__(128) place_kernel(const Pass p, const int32_t* __restrict__ table, const int32_t* __restrict__ base)
 {
-    extern __shared__ int32_t next[];
+    extern __shared__ __align__(16) int32_t next[];
     const int g = blockIdx.y, lane = threadIdx.x & 31;
+    grid_dependency_wait();
     const int32_t *t = table + ((int64_t)g * p.chunks + blockIdx.x) * p.stride, *b = base + (int64_t)g * p.stride;
 #pragma unroll 4
     for (int j = threadIdx.x * 4; j < p.stride; j += 512)
@@ -157,7 +162,8 @@ __global__ void __launch_bounds__(128) place_kernel(const Pass p, const int32_t*
     fetch(begin);
     for (int64_t i0 = begin; i0 < end; i0 += 32 * kAhead) {
         uint32_t k_now[kAhead];
-        int32_t v_now[kAhead], at[kAhead];
+        int32_t v_now[kAhead], at[kAhead], d[kAhead];
+        unsigned same[kAhead];
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
             k_now[k] = key[k];
@@ -165,7 +171,12 @@ __global__ void __launch_bounds__(128) place_kernel(const Pass p, const int32_t*
         }
         fetch(i0 + 32 * kAhead);
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) at[k] = take_places(next, i0 + 32 * k + lane < end ? digit_of(k_now[k], p.shift) : -1);
+        for (int k = 0; k < kAhead; ++k) {
+            d[k] = i0 + 32 * k + lane < end ? digit_of(k_now[k], p.shift) : -1;
+            same[k] = __match_any_sync(0xffffffffu, d[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) at[k] = take_places(next, d[k], same[k]);
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
             if (i0 + 32 * k + lane >= end) continue;
@@ -179,10 +190,11 @@ __global__ void __launch_bounds__(128) place_kernel(const Pass p, const int32_t*
 __global__ void __launch_bounds__(kBlockThreads) block_sort_kernel(int n, int G, int64_t m, const int32_t* __restrict__ idx,
                                                                    int32_t* __restrict__ order, int32_t* __restrict__ offset)
 {
-    extern __shared__ int32_t next[];
+    extern __shared__ __align__(16) int32_t next[];
     const int g = blockIdx.x, tid = threadIdx.x, lane = tid & 31, bins = (int)m + 1;
     uint16_t* keys = reinterpret_cast<uint16_t*>(next + ((bins + 3) & ~3));
     for (int j = tid; j < bins; j += kBlockThreads) next[j] = 0;
+    grid_dependency_wait();
     __syncthreads();
 #pragma unroll 4
     for (int i = tid; i < n; i += kBlockThreads) {
@@ -207,7 +219,8 @@ __global__ void __launch_bounds__(kBlockThreads) block_sort_kernel(int n, int G,
 #pragma unroll 4
     for (int i0 = 0; i0 < n; i0 += 32) {
         const int i = i0 + lane;
-        const int32_t at = take_places(next, i < n ? keys[i] : -1);
+        const int d = i < n ? keys[i] : -1;
+        const int32_t at = take_places(next, d, __match_any_sync(0xffffffffu, d));
         if (i < n) order[(int64_t)g * n + at] = i;
     }
 }
@@ -216,6 +229,7 @@ __global__ void __launch_bounds__(kBlockThreads) block_sort_kernel(int n, int G,
 __global__ void __launch_bounds__(256) bounds_kernel(const uint32_t* __restrict__ key, int32_t* __restrict__ offset, int64_t n, int64_t m)
 {
     const int64_t j = blockIdx.x * (int64_t)256 + threadIdx.x;
+    grid_dependency_wait();
     if (j > m) return;
     const uint32_t* k = key + (int64_t)blockIdx.y * n;
     int64_t lo = 0, hi = n;
@@ -272,7 +286,7 @@ int64_t sort_workspace(int64_t n, int G, int64_t m) { return SortSpace(nullptr, 
 cudaError_t launch_sort_indices(int64_t n, int G, int64_t m, const int32_t* idx, int32_t* order, int32_t* offset, void* ws,
                                 cudaStream_t s)
 {
-    const Launch l{s, nullptr, nullptr};
+    const Launch l{s, nullptr, nullptr, true};
     if (by_block(n, m))
         return launch_kernel(l, block_sort_kernel, dim3((unsigned)G), kBlockThreads, stride_of(m) * 4 + (n + 1) / 2 * 4, 1, (int)n, G, m, idx, order, offset);
     const SortSpace sp(ws, n, G, m);

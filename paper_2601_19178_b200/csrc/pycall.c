@@ -200,10 +200,105 @@ static PyObject* put(PyObject* self, PyObject* const* args, Py_ssize_t n_args)
     return PyLong_FromLong(status);
 }
 
+static int addresses(PyObject* const* args, int n, void** p)
+{
+    for (int i = 0; i < n; ++i)
+        if (!optional_address(args[i], &p[i])) return 0;
+    return 1;
+}
+
+typedef int32_t (*sort_fn)(int32_t, int32_t, int32_t, int32_t, const void*, void*, void*, void*, int64_t, void*);
+typedef int32_t (*loss_fn)(int32_t, int32_t, int32_t, int32_t, int32_t, const void*, const void*, const void*, const void*, void*, void*,
+                           void*, void*, void*, int64_t, void*);
+typedef int32_t (*loss_grad_fn)(int32_t, int32_t, int32_t, int32_t, int32_t, const void*, const void*, const void*, const void*,
+                                const void*, const void*, const void*, const void*, const void*, float, float, const void*, void*,
+                                void*, void*, void*, int64_t, void*);
+typedef int32_t (*gather_fn)(int32_t, int32_t, int32_t, int32_t, int32_t, int32_t, int32_t, const void*, const void*, const void*,
+                             const void*, void*, void*);
+typedef int32_t (*gather_grad_fn)(int32_t, int32_t, int32_t, int32_t, int32_t, int32_t, int32_t, const void*, const void*, const void*,
+                                  const void*, const void*, void*, void*, void*, void*, int64_t, void*);
+
+/* The calls that fit the router and the pool, their arguments behind the function address in the C ABI's order (every array a
+ * contiguous tensor or None): the status of the call, or None as above. */
+static PyObject* fit(PyObject* const* args, Py_ssize_t n_args, int want, int n_whole, int n_first, int n_second, int floats, int workspace,
+                     int which)
+{
+    if (n_args != want) {
+        PyErr_Format(PyExc_TypeError, "the call takes %d arguments", want);
+        return NULL;
+    }
+    void* fn = PyLong_AsVoidPtr(args[0]);
+    void* stream = PyLong_AsVoidPtr(args[n_args - 1]);
+    if (PyErr_Occurred()) return NULL;
+    int32_t v[7], status = 0;
+    void* p[14];
+    float f[2] = {0, 0};
+    int64_t bytes = 0;
+    PyObject* const* a = args + 1;
+    int plain = whole_numbers(a, n_whole, v);
+    a += n_whole;
+    plain = plain && addresses(a, n_first, p);
+    a += n_first;
+    for (int i = 0; plain && i < floats; ++i) f[i] = (float)PyFloat_AsDouble(a[i]);
+    a += floats;
+    plain = plain && !PyErr_Occurred() && addresses(a, n_second, p + n_first);
+    a += n_second;
+    if (plain && workspace) bytes = PyLong_AsLongLong(*a);
+    if (PyErr_Occurred()) return NULL;
+    if (!plain) Py_RETURN_NONE;
+    Py_BEGIN_ALLOW_THREADS;
+    switch (which) {
+        case 0: status = ((sort_fn)fn)(v[0], v[1], v[2], v[3], p[0], p[1], p[2], p[3], bytes, stream); break;
+        case 1:
+            status = ((loss_fn)fn)(v[0], v[1], v[2], v[3], v[4], p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], p[8], bytes, stream);
+            break;
+        case 2:
+            status = ((loss_grad_fn)fn)(v[0], v[1], v[2], v[3], v[4], p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], p[8], f[0], f[1],
+                                        p[9], p[10], p[11], p[12], p[13], bytes, stream);
+            break;
+        case 3: status = ((gather_fn)fn)(v[0], v[1], v[2], v[3], v[4], v[5], v[6], p[0], p[1], p[2], p[3], p[4], stream); break;
+        default:
+            status = ((gather_grad_fn)fn)(v[0], v[1], v[2], v[3], v[4], v[5], v[6], p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], p[8],
+                                          bytes, stream);
+    }
+    Py_END_ALLOW_THREADS;
+    return PyLong_FromLong(status);
+}
+static PyObject* sort(PyObject* self, PyObject* const* args, Py_ssize_t n)
+{
+    (void)self;
+    return fit(args, n, 11, 4, 4, 0, 0, 1, 0);
+}
+static PyObject* loss(PyObject* self, PyObject* const* args, Py_ssize_t n)
+{
+    (void)self;
+    return fit(args, n, 17, 5, 9, 0, 0, 1, 1);
+}
+static PyObject* loss_grad(PyObject* self, PyObject* const* args, Py_ssize_t n)
+{
+    (void)self;
+    return fit(args, n, 24, 5, 9, 5, 2, 1, 2);
+}
+static PyObject* gather(PyObject* self, PyObject* const* args, Py_ssize_t n)
+{
+    (void)self;
+    return fit(args, n, 14, 7, 5, 0, 0, 0, 3);
+}
+static PyObject* gather_grad(PyObject* self, PyObject* const* args, Py_ssize_t n)
+{
+    (void)self;
+    return fit(args, n, 19, 7, 9, 0, 0, 1, 4);
+}
+
 static PyMethodDef methods[] = {{"attend", (PyCFunction)(void (*)(void))attend, METH_FASTCALL, "one decode call"},
                                 {"append", (PyCFunction)(void (*)(void))append, METH_FASTCALL, "one append"},
                                 {"put", (PyCFunction)(void (*)(void))put, METH_FASTCALL, "one put of several users"},
                                 {"prefill", (PyCFunction)(void (*)(void))prefill, METH_FASTCALL, "one router or projection call"},
+                                {"sort", (PyCFunction)(void (*)(void))sort, METH_FASTCALL, "one sort of indices"},
+                                {"loss", (PyCFunction)(void (*)(void))loss, METH_FASTCALL, "one call of the router losses"},
+                                {"loss_grad", (PyCFunction)(void (*)(void))loss_grad, METH_FASTCALL, "one call of their gradient"},
+                                {"gather", (PyCFunction)(void (*)(void))gather, METH_FASTCALL, "one lookup"},
+                                {"gather_grad", (PyCFunction)(void (*)(void))gather_grad, METH_FASTCALL, "one call of its gradient"},
                                 {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pycall", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
