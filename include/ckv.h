@@ -297,7 +297,7 @@ CKV_API ckv_status ckv_project(int32_t device, int32_t n, int32_t n_groups, int3
  * position without an entry (padding): it takes no part in the losses and gradients of its group, whatever its inputs hold.
  * Results are the same bits from call to call.  Array arguments are device memory of `device` (or managed), aligned to
  * their elements, W and d_out to 16 bytes.  `workspace` is device memory on a 256-byte boundary of at least the size that the _bytes
- * function of the call gives, of any contents; calls that may overlap on the GPU, captured graphs among them, need one each.
+ * function of the call gives (NULL where that is 0), of any contents; calls that may overlap on the GPU, captured graphs among them, need one each.
  * Errors of all of them: INVALID_ARG (sizes, null, host or misaligned pointers, workspace too small), UNSUPPORTED (d_in,
  * head_dim, more than 65535 groups), SHAPE (d_shared outside [1, head_dim]), CUDA.
  */
@@ -350,9 +350,11 @@ CKV_API ckv_status ckv_route_loss_grad(int32_t device, int32_t n, int32_t n_grou
  * [n][n_groups][head_dim], all of `dtype`; a position without an entry gets zeros behind its user part.  The product is
  * rounded once.
  */
+CKV_API ckv_status ckv_gather_bytes(int32_t dtype, int32_t n, int32_t n_groups, int32_t head_dim, int32_t d_shared,
+                                    int32_t n_entries, int64_t* bytes);
 CKV_API ckv_status ckv_gather(int32_t device, int32_t dtype, int32_t n, int32_t n_groups, int32_t head_dim, int32_t d_shared,
                               int32_t n_entries, const void* pool, const int32_t* idx, const void* user, const float* score,
-                              void* out, void* stream);
+                              void* out, void* workspace, int64_t workspace_bytes, void* stream);
 
 /*
  * Gradients of ckv_gather, d_out [n][n_groups][head_dim] of `dtype`, order and offset of ckv_sort_indices:

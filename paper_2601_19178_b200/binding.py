@@ -28,7 +28,7 @@ EXPORTS = (
     "ckv_cache_bytes", "ckv_set_option", "ckv_get_option", "ckv_last_stat", "ckv_strerror",
     "ckv_last_cuda_error", "ckv_version", "ckv_route", "ckv_project", "ckv_pool_load_sides", "ckv_attend_visible",
     "ckv_sort_indices_bytes", "ckv_sort_indices", "ckv_route_loss_bytes", "ckv_route_loss", "ckv_route_loss_grad",
-    "ckv_gather", "ckv_gather_grad_bytes", "ckv_gather_grad",
+    "ckv_gather_bytes", "ckv_gather", "ckv_gather_grad_bytes", "ckv_gather_grad",
 )
 
 
@@ -85,7 +85,8 @@ def _load() -> ctypes.CDLL:
         "ckv_route_loss_bytes": (i32, [i32, i32, i32, i32, p64, p64]),
         "ckv_route_loss": (i32, [i32] * 5 + [vp] * 9 + [i64, vp]),
         "ckv_route_loss_grad": (i32, [i32] * 5 + [vp] * 9 + [ctypes.c_float] * 2 + [vp] * 5 + [i64, vp]),
-        "ckv_gather": (i32, [i32] * 7 + [vp] * 6),
+        "ckv_gather_bytes": (i32, [i32] * 6 + [p64]),
+        "ckv_gather": (i32, [i32] * 7 + [vp] * 6 + [i64, vp]),
         "ckv_gather_grad_bytes": (i32, [i32, i32, i32, p64]),
         "ckv_gather_grad": (i32, [i32] * 7 + [vp] * 9 + [i64, vp]),
     }
@@ -408,15 +409,22 @@ def ckv_route_loss_grad(device: int, n: int, n_groups: int, d_in: int, n_entries
                                          int(workspace_bytes), _stream(stream)), "ckv_route_loss_grad")
 
 
+def ckv_gather_bytes(dtype: int, n: int, n_groups: int, head_dim: int, d_shared: int, n_entries: int) -> int:
+    v = ctypes.c_int64()
+    _check(None, lib.ckv_gather_bytes(dtype, n, n_groups, head_dim, d_shared, n_entries, ctypes.byref(v)), "ckv_gather_bytes")
+    return v.value
+
+
 def ckv_gather(device: int, dtype: int, n: int, n_groups: int, head_dim: int, d_shared: int, n_entries: int, pool, idx, user,
-               score, out, stream=None) -> None:
+               score, out, workspace, workspace_bytes: int, stream=None) -> None:
     """out [n][G][head_dim] = (user part | sigmoid(score) * picked pool row); score None: without the gate."""
     stream = _stream(stream)
-    st = _pycall.gather(_GATHER, device, dtype, n, n_groups, head_dim, d_shared, n_entries, pool, idx, user, score, out, stream or 0)
+    st = _pycall.gather(_GATHER, device, dtype, n, n_groups, head_dim, d_shared, n_entries, pool, idx, user, score, out, workspace,
+                        workspace_bytes, stream or 0)
     if st is not None:
         return _check(None, st, "ckv_gather") if st else None
     _check(None, lib.ckv_gather(device, dtype, n, n_groups, head_dim, d_shared, n_entries, _ptr(pool), _ptr(idx), _ptr(user),
-                                _ptr(score), _ptr(out), _stream(stream)), "ckv_gather")
+                                _ptr(score), _ptr(out), _ptr(workspace), int(workspace_bytes), _stream(stream)), "ckv_gather")
 
 
 def ckv_gather_grad_bytes(n: int, n_groups: int, head_dim: int) -> int:

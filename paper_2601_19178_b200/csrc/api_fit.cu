@@ -136,17 +136,29 @@ ckv_status ckv_route_loss_grad(int32_t device, int32_t n, int32_t n_groups, int3
     return status_of(launch_route_grad(a, b, workspace, (cudaStream_t)stream));
 }
 
-ckv_status ckv_gather(int32_t device, int32_t dtype, int32_t n, int32_t n_groups, int32_t head_dim, int32_t d_shared, int32_t n_entries,
-                      const void* pool, const int32_t* idx, const void* user, const float* score, void* out, void* stream)
+ckv_status ckv_gather_bytes(int32_t dtype, int32_t n, int32_t n_groups, int32_t head_dim, int32_t d_shared, int32_t n_entries,
+                            int64_t* bytes)
 {
-    const ckv_status st = check_gather(device, dtype, n, n_groups, head_dim, d_shared, n_entries);
+    if (!bytes) return CKV_ERR_INVALID_ARG;
+    const ckv_status st = check_gather(0, dtype, n, n_groups, head_dim, d_shared, n_entries);
+    if (st == CKV_OK) *bytes = gather_workspace(dtype, n, n_groups, head_dim, d_shared, n_entries);
+    return st;
+}
+
+ckv_status ckv_gather(int32_t device, int32_t dtype, int32_t n, int32_t n_groups, int32_t head_dim, int32_t d_shared, int32_t n_entries,
+                      const void* pool, const int32_t* idx, const void* user, const float* score, void* out, void* workspace,
+                      int64_t workspace_bytes, void* stream)
+{
+    ckv_status st = check_gather(device, dtype, n, n_groups, head_dim, d_shared, n_entries);
     if (st != CKV_OK) return st;
     if (n == 0) return CKV_OK;
     DeviceGuard dg(device);
     if (!dg.ok) return CKV_ERR_CUDA;
     const int e = dtype == CKV_F32 ? 4 : 2;
     if (!on_device(Arg{pool, e}, Arg{idx, 4}, Arg{user, e, d_shared == head_dim}, Arg{score, 4, true}, Arg{out, e})) return CKV_ERR_INVALID_ARG;
-    return status_of(launch_gather(dtype, n, n_groups, head_dim, d_shared, n_entries, pool, idx, user, score, out, (cudaStream_t)stream));
+    st = check_workspace(workspace, workspace_bytes, gather_workspace(dtype, n, n_groups, head_dim, d_shared, n_entries));
+    if (st != CKV_OK) return st;
+    return status_of(launch_gather(dtype, n, n_groups, head_dim, d_shared, n_entries, pool, idx, user, score, out, workspace, (cudaStream_t)stream));
 }
 
 ckv_status ckv_gather_grad_bytes(int32_t n, int32_t n_groups, int32_t head_dim, int64_t* bytes)

@@ -29,8 +29,9 @@ cudaError_t launch_sort_indices(int64_t n, int G, int64_t m, const int32_t* idx,
 
 // ---- kernels_gather.cu
 // out[i][g] = (user[i][g] | gate * pool[g][idx[i][g]]), gate = sigmoid(score[i][g]) or 1, rows of D elements, D - ds of them the user's
+int64_t gather_workspace(int dtype, int64_t n, int G, int D, int ds, int64_t m);
 cudaError_t launch_gather(int dtype, int64_t n, int G, int D, int ds, int64_t m, const void* pool, const int32_t* idx,
-                          const void* user, const float* score, void* out, cudaStream_t s);
+                          const void* user, const float* score, void* out, void* ws, cudaStream_t s);
 
 // Sums of rows over the runs of equal entries in a sorted order, and what falls off on the way.
 struct SegmentArgs {

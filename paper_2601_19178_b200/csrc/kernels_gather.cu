@@ -49,14 +49,15 @@ __device__ __forceinline__ void load16(uint32_t (&w)[4], const void* p)
 // Lookup.  A warp takes up to 32 rows at a time: a lane fetches one row's index and score and works out where its pool row lies and
 // the gate; then the lanes run over the rows' 16-byte pieces side by side.  A pool row of 60 or 62 bytes lies on no wider
 // boundary than a word or an element: LOAD is what all pieces lie on.  log_pieces: of a row; log_rows: rows of a warp, fewer
-// where there are few, so that a warp's chain of loads is short.
+// where there are few, so that a warp's chain of loads is short.  skip: elements of a row in front of the pool's, the user's or
+// (widened pool) none.
 template <typename E, int LOAD>
-__global__ void __launch_bounds__(256) gather_kernel(int64_t rows, int G, int log_pieces, int log_rows, int skip, int ds, int64_t m, int store,
+__global__ void __launch_bounds__(256) gather_kernel(int64_t rows, int G, int log_pieces, int log_rows, int skip, int user_width, int user_bytes, int ds, int64_t m, int store,
                                                      const E* __restrict__ pool, const int32_t* __restrict__ idx,
                                                      const E* __restrict__ user, const float* __restrict__ score, E* __restrict__ out)
 {
     constexpr int N = 16 / (int)sizeof(E), PER = 4 / (int)sizeof(E);  // elements of a piece, of a word
-    const int lane = threadIdx.x & 31, bytes = (skip + ds) * (int)sizeof(E);
+    const int lane = threadIdx.x & 31, bytes = (skip + ds) * (int)sizeof(E);  // skip + ds: a row of `out`
     const int64_t step = (int64_t)gridDim.x * 8 << log_rows;
     grid_dependency_wait();
     for (int64_t r0 = (blockIdx.x * (int64_t)8 + (threadIdx.x >> 5)) << log_rows; r0 < rows; r0 += step) {
@@ -90,11 +91,17 @@ __global__ void __launch_bounds__(256) gather_kernel(int64_t rows, int G, int lo
 #pragma unroll
                     for (int q = 0; q < 4; ++q) v[q] = scaled<E>(v[q], f);
             }
-            if (c < skip) {
-                const E* u = user + (r0 + k) * skip + c;
+            if (c < user_width) {
+                const E* u = user + (r0 + k) * user_width + c;
+                if (user_bytes == 4) v[0] = __ldg(reinterpret_cast<const uint32_t*>(u));
+                else if (user_bytes == 8) {
+                    const uint2 x = __ldg(reinterpret_cast<const uint2*>(u));
+                    v[0] = x.x, v[1] = x.y;
+                } else if (user_bytes == 2) v[0] = (v[0] & 0xffff0000u) | __ldg(reinterpret_cast<const uint16_t*>(u));
+                else
 #pragma unroll
                 for (int q = 0; q < N; ++q)
-                    if (c + q < skip) {
+                    if (c + q < user_width) {
                         const E x = __ldg(u + q);
                         if (sizeof(E) == 4) v[q / PER] = __float_as_uint((float)x);
                         else v[q / PER] = (v[q / PER] & (q % PER ? 0xffffu : 0xffff0000u)) | (uint32_t)(uint16_t)x << (16 * (q % PER));
@@ -155,6 +162,35 @@ __device__ __forceinline__ int64_t entry_of_group(const int32_t* __restrict__ of
         }
     }
     return lo;
+}
+
+// Each of LANES lanes has its share of AHEAD rows' sums: added up so that row sub + i LANES ends in dot[i] of lane `sub`.  With every step a
+// lane gives away the rows that are not its own.
+template <int LANES, int AHEAD>
+__device__ __forceinline__ void share_out(float (&dot)[AHEAD], int sub)
+{
+    if constexpr (LANES >= AHEAD) {
+#pragma unroll
+        for (int d = LANES / 2; d >= AHEAD; d /= 2)
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) dot[k] += __shfl_xor_sync(0xffffffffu, dot[k], d);
+#pragma unroll
+        for (int half = AHEAD / 2; half > 0; half /= 2)
+#pragma unroll
+            for (int k = 0; k < half; ++k) {
+                const bool up = sub & half;
+                const float give = up ? dot[k] : dot[k + half], keep = up ? dot[k + half] : dot[k];
+                dot[k] = keep + __shfl_xor_sync(0xffffffffu, give, half);
+            }
+    } else {
+        static_assert(LANES == 2, "a lane keeps every second row");
+#pragma unroll
+        for (int i = 0; i < AHEAD / 2; ++i) {
+            const bool up = sub & 1;
+            const float give = up ? dot[2 * i] : dot[2 * i + 1], keep = up ? dot[2 * i + 1] : dot[2 * i];
+            dot[i] = keep + __shfl_xor_sync(0xffffffffu, give, 1);
+        }
+    }
 }
 
 // What a chunk leaves for its block.
@@ -238,10 +274,11 @@ __global__ void __launch_bounds__(kSegThreads, GATED ? 5 : 6) segment_kernel(con
         }
     };
     look_ahead(begin);
+    const E* const rows = (const E*)a.rows + g * a.group_stride + col0;
+    const int user_bytes = a.skip <= N && ((uintptr_t)a.d_user & (a.skip * sizeof(E) - 1)) == 0 ? a.skip * (int)sizeof(E) : 0;
     for (int64_t t0 = begin; t0 < begin + chunk; t0 += AHEAD) {  // (as many turns for every chunk: a warp's stay together)
-        int32_t pos[PER];
+        int32_t pos[PER], key[PER];
         float2 gate[PER];  // weight of the row; GATED: and one less it
-        int32_t key[PER];
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             pos[i] = ahead[i] < a.n ? ahead[i] : -1;  // (not an order)
@@ -253,7 +290,7 @@ __global__ void __launch_bounds__(kSegThreads, GATED ? 5 : 6) segment_kernel(con
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) {
             const int32_t p = __shfl_sync(0xffffffffu, pos[k / LANES], k % LANES, LANES);
-            raw[k] = p >= 0 ? __ldg(reinterpret_cast<const uint4*>((const E*)a.rows + p * a.stride + g * a.group_stride + col0)) : make_uint4(0, 0, 0, 0);
+            raw[k] = p >= 0 ? __ldcs(reinterpret_cast<const uint4*>(rows + p * a.stride)) : make_uint4(0, 0, 0, 0);
         }
         look_ahead(t0 + AHEAD);
         const bool mixed = t0 + AHEAD > run_end && j != j_last;
@@ -263,41 +300,70 @@ __global__ void __launch_bounds__(kSegThreads, GATED ? 5 : 6) segment_kernel(con
                 const int64_t t = t0 + sub + i * LANES;
                 key[i] = (int32_t)entry_of(offset, min(t, end - 1), j, j_last);
             }
-        const bool any_mixed = __any_sync(0xffffffffu, mixed);
+        // Run by run: all rows of the entry at hand, then the next entry's, until no chunk of the warp has more.  (A flush between any two
+        // rows made code that did not fit the instruction cache.)
+        float dot[AHEAD] = {};
+        bool more, fresh = true;  // fresh: the chunk's run has not been added
+        do {
+            unsigned here[PER];  // rows of this run, bit k % LANES of word k / LANES
+            int32_t next = INT32_MAX;
 #pragma unroll
-        for (int k = 0; k < AHEAD; ++k) {
-            const int32_t p = __shfl_sync(0xffffffffu, pos[k / LANES], k % LANES, LANES);
-            const float w = __shfl_sync(0xffffffffu, gate[k / LANES].x, k % LANES, LANES);
-            if (any_mixed) {
-                const int32_t here = __shfl_sync(0xffffffffu, key[k / LANES], k % LANES, LANES);
-                if (here != (int32_t)j) {
-                    flush(false);
-                    j = here;
-                    run_end = j < a.m ? __ldg(offset + j + 1) : a.n;
-                    fetch_pool();
+            for (int i = 0; i < PER; ++i) {
+                here[i] = (__ballot_sync(0xffffffffu, fresh && pos[i] >= 0 && key[i] == (int32_t)j) & mine) >> (lane - sub);
+                if (pos[i] >= 0 && key[i] > (int32_t)j) next = min(next, key[i]);
+            }
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                const float w = __shfl_sync(0xffffffffu, gate[k / LANES].x, k % LANES, LANES);
+                if (here[k / LANES] >> (k % LANES) & 1) {
+                    const E* v = reinterpret_cast<const E*>(&raw[k]);
+                    float sum = 0.f;
+#pragma unroll
+                    for (int q = 0; q < N; ++q) {
+                        const float x = widen(v[q]);
+                        acc[q] = fmaf(w, x, acc[q]);
+                        if (GATED) sum = fmaf(own[q], x, sum);
+                    }
+                    if (GATED) dot[k] = sum;
+                    else wsum += w;
                 }
             }
-            const E* v = reinterpret_cast<const E*>(&raw[k]);
-            float dot = 0.f;
+            more = __any_sync(0xffffffffu, mixed);
+            if (!more) break;
 #pragma unroll
-            for (int q = 0; q < N; ++q) {
-                const float x = widen(v[q]);
-                if (p >= 0) acc[q] = fmaf(w, x, acc[q]);
-                if (GATED) dot = fmaf(own[q], x, dot);
+            for (int d = LANES / 2; d > 0; d /= 2) next = min(next, __shfl_xor_sync(0xffffffffu, next, d));
+            fresh = next != INT32_MAX;
+            more = __any_sync(0xffffffffu, fresh);
+            if (fresh) {
+                flush(false);
+                j = next;
+                run_end = j < a.m ? __ldg(offset + j + 1) : a.n;
+                fetch_pool();
             }
-            wsum += w;
-            if (a.d_user && p >= 0 && col0 < a.skip) {
+        } while (more);
+        if (a.d_user) {
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                const int32_t p = __shfl_sync(0xffffffffu, pos[k / LANES], k % LANES, LANES);
+                if (p < 0 || col0 >= a.skip) continue;
                 E* to = (E*)a.d_user + ((int64_t)p * a.G + g) * a.skip + col0;
+                switch (user_bytes) {  // one store for a row's whole part
+                    case 2: *reinterpret_cast<uint16_t*>(to) = (uint16_t)raw[k].x; break;
+                    case 4: *reinterpret_cast<uint32_t*>(to) = raw[k].x; break;
+                    case 8: *reinterpret_cast<uint2*>(to) = make_uint2(raw[k].x, raw[k].y); break;
+                    case 16: *reinterpret_cast<uint4*>(to) = raw[k]; break;
+                    default:
 #pragma unroll
-                for (int q = 0; q < N; ++q)
-                    if (col0 + q < a.skip) to[q] = v[q];
+                        for (int q = 0; q < N; ++q)
+                            if (col0 + q < a.skip) to[q] = reinterpret_cast<const E*>(&raw[k])[q];
+                }
             }
-            if (GATED && a.d_score) {
-                const float less = __shfl_sync(0xffffffffu, gate[k / LANES].y, k % LANES, LANES);
+        }
+        if (GATED && a.d_score) {
+            share_out<LANES, AHEAD>(dot, sub);
 #pragma unroll
-                for (int d = LANES / 2; d > 0; d /= 2) dot += __shfl_xor_sync(0xffffffffu, dot, d);
-                if (sub == 0 && p >= 0) a.d_score[(int64_t)p * a.G + g] = j < a.m ? dot * w * less : 0.f;
-            }
+            for (int i = 0; i < PER; ++i)
+                if (pos[i] >= 0) a.d_score[(int64_t)pos[i] * a.G + g] = key[i] < a.m ? dot[i] * gate[i].x * gate[i].y : 0.f;
         }
     }
     __syncwarp(mine);
@@ -468,20 +534,51 @@ cudaError_t launch_segments(const SegmentArgs& a, const SegmentSpace& sp, int bl
     }
 }
 
+// Pool rows behind `skip` zeros, D elements each: every piece of a row then is 16 bytes on a 16-byte boundary.
+template <typename E>
+__global__ void __launch_bounds__(256) widen_pool_kernel(int64_t pieces, int log_pieces, int skip, int ds, const E* __restrict__ pool, uint4* __restrict__ wide)
+{
+    constexpr int N = 16 / (int)sizeof(E);
+    const int64_t t = blockIdx.x * (int64_t)256 + threadIdx.x;
+    grid_dependency_wait();
+    if (t >= pieces) return;
+    const int64_t r = t >> log_pieces;
+    const int c = (int)(t - (r << log_pieces)) * N;
+    __align__(16) E v[N];
+#pragma unroll
+    for (int q = 0; q < N; ++q) v[q] = c + q >= skip ? __ldg(pool + r * ds + (c + q - skip)) : (E)0;
+    wide[t] = *reinterpret_cast<const uint4*>(v);
+}
+
+// Whether a lookup copies the pool first.  Four loads of a piece's words (eight of its elements) keep the L1 busy for longer than the row
+// takes to store (1048576 x 8 rows of 64 bytes 261 us, WIDE us behind the copy), which pays once there are some rows per entry.
+bool widens(int64_t n, int D, int ds, int64_t m, int elem) { return n >= 2 * m && (ds * elem % 16 != 0 || (D - ds) * elem % 16 != 0); }
+
 template <typename E>
 cudaError_t launch_gather_t(int64_t n, int G, int D, int ds, int64_t m, const void* pool, const int32_t* idx, const void* user,
-                            const float* score, void* out, cudaStream_t s)
+                            const float* score, void* out, void* ws, cudaStream_t s)
 {
     constexpr int e = (int)sizeof(E);
-    const int skip = D - ds;
-    auto lies_on = [](const void* p, int step) { return ((uintptr_t)p | (uintptr_t)step) % 16 == 0 ? 16 : ((uintptr_t)p | (uintptr_t)step) % 4 == 0 ? 4 : 2; };
-    const int load = std::min(lies_on(pool, ds * e), lies_on(nullptr, skip * e)), store = lies_on(out, 16);
+    int skip = D - ds, user_width = skip;
     int log_pieces = 0, log_rows = 5;
     while (16 << log_pieces < D * e) ++log_pieces;
+    if (widens(n, D, ds, m, e)) {
+        const int64_t pieces = G * m << log_pieces;
+        const cudaError_t er = launch_kernel(Launch{s, nullptr, nullptr, true}, widen_pool_kernel<E>, dim3((unsigned)((pieces + 255) / 256)), 256, 0, 1, pieces,
+                                             log_pieces, skip, ds, (const E*)pool, (uint4*)ws);
+        if (er != cudaSuccess) return er;
+        pool = ws;
+        skip = 0;
+        ds = D;
+    }
+    auto lies_on = [](const void* p, int step) { return ((uintptr_t)p | (uintptr_t)step) % 16 == 0 ? 16 : ((uintptr_t)p | (uintptr_t)step) % 4 == 0 ? 4 : 2; };
+    // a user part that one load takes
+    const int ub = user_width * e, user_bytes = (ub == 2 || ub == 4 || ub == 8) && (uintptr_t)user % ub == 0 ? ub : 0;
+    const int load = std::min(lies_on(pool, ds * e), lies_on(nullptr, skip * e)), store = lies_on(out, 16);
     while (log_pieces + log_rows > 5 && log_rows > 0 && (n * G >> log_rows) < 148 * 32) --log_rows;
     const int64_t per_block = (int64_t)8 << log_rows, blocks = std::min<int64_t>((n * G + per_block - 1) / per_block, 148 * 8);
     auto go = [&](auto kernel) {
-        return launch_kernel(Launch{s, nullptr, nullptr, true}, kernel, dim3((unsigned)blocks), 256, 0, 1, n * G, G, log_pieces, log_rows, skip, ds, m, store,
+        return launch_kernel(Launch{s, nullptr, nullptr, true}, kernel, dim3((unsigned)blocks), 256, 0, 1, n * G, G, log_pieces, log_rows, skip, user_width, user_bytes, ds, m, store,
                              (const E*)pool, idx, (const E*)user, score, (E*)out);
     };
     if constexpr (e == 2)
@@ -491,11 +588,17 @@ cudaError_t launch_gather_t(int64_t n, int G, int D, int ds, int64_t m, const vo
 
 }  // namespace
 
-cudaError_t launch_gather(int dtype, int64_t n, int G, int D, int ds, int64_t m, const void* pool, const int32_t* idx,
-                          const void* user, const float* score, void* out, cudaStream_t s)
+int64_t gather_workspace(int dtype, int64_t n, int G, int D, int ds, int64_t m)
 {
-    return dtype == CKV_F32 ? launch_gather_t<float>(n, G, D, ds, m, pool, idx, user, score, out, s)
-                            : launch_gather_t<uint16_t>(n, G, D, ds, m, pool, idx, user, score, out, s);
+    const int elem = dtype == CKV_F32 ? 4 : 2;
+    return widens(n, D, ds, m, elem) ? G * m * D * elem : 0;
+}
+
+cudaError_t launch_gather(int dtype, int64_t n, int G, int D, int ds, int64_t m, const void* pool, const int32_t* idx,
+                          const void* user, const float* score, void* out, void* ws, cudaStream_t s)
+{
+    return dtype == CKV_F32 ? launch_gather_t<float>(n, G, D, ds, m, pool, idx, user, score, out, ws, s)
+                            : launch_gather_t<uint16_t>(n, G, D, ds, m, pool, idx, user, score, out, ws, s);
 }
 
 int64_t segment_workspace(int64_t n, int G, int width)  // of either type: the longer blocks are those of 16-bit elements

@@ -214,14 +214,13 @@ typedef int32_t (*loss_grad_fn)(int32_t, int32_t, int32_t, int32_t, int32_t, con
                                 const void*, const void*, const void*, const void*, const void*, float, float, const void*, void*,
                                 void*, void*, void*, int64_t, void*);
 typedef int32_t (*gather_fn)(int32_t, int32_t, int32_t, int32_t, int32_t, int32_t, int32_t, const void*, const void*, const void*,
-                             const void*, void*, void*);
+                             const void*, void*, void*, int64_t, void*);
 typedef int32_t (*gather_grad_fn)(int32_t, int32_t, int32_t, int32_t, int32_t, int32_t, int32_t, const void*, const void*, const void*,
                                   const void*, const void*, void*, void*, void*, void*, int64_t, void*);
 
 /* The calls that fit the router and the pool, their arguments behind the function address in the C ABI's order (every array a
  * contiguous tensor or None): the status of the call, or None as above. */
-static PyObject* fit(PyObject* const* args, Py_ssize_t n_args, int want, int n_whole, int n_first, int n_second, int floats, int workspace,
-                     int which)
+static PyObject* fit(PyObject* const* args, Py_ssize_t n_args, int want, int n_whole, int n_first, int n_second, int floats, int which)
 {
     if (n_args != want) {
         PyErr_Format(PyExc_TypeError, "the call takes %d arguments", want);
@@ -243,7 +242,7 @@ static PyObject* fit(PyObject* const* args, Py_ssize_t n_args, int want, int n_w
     a += floats;
     plain = plain && !PyErr_Occurred() && addresses(a, n_second, p + n_first);
     a += n_second;
-    if (plain && workspace) bytes = PyLong_AsLongLong(*a);
+    if (plain) bytes = PyLong_AsLongLong(*a);
     if (PyErr_Occurred()) return NULL;
     if (!plain) Py_RETURN_NONE;
     Py_BEGIN_ALLOW_THREADS;
@@ -256,7 +255,7 @@ static PyObject* fit(PyObject* const* args, Py_ssize_t n_args, int want, int n_w
             status = ((loss_grad_fn)fn)(v[0], v[1], v[2], v[3], v[4], p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], p[8], f[0], f[1],
                                         p[9], p[10], p[11], p[12], p[13], bytes, stream);
             break;
-        case 3: status = ((gather_fn)fn)(v[0], v[1], v[2], v[3], v[4], v[5], v[6], p[0], p[1], p[2], p[3], p[4], stream); break;
+        case 3: status = ((gather_fn)fn)(v[0], v[1], v[2], v[3], v[4], v[5], v[6], p[0], p[1], p[2], p[3], p[4], p[5], bytes, stream); break;
         default:
             status = ((gather_grad_fn)fn)(v[0], v[1], v[2], v[3], v[4], v[5], v[6], p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], p[8],
                                           bytes, stream);
@@ -267,27 +266,27 @@ static PyObject* fit(PyObject* const* args, Py_ssize_t n_args, int want, int n_w
 static PyObject* sort(PyObject* self, PyObject* const* args, Py_ssize_t n)
 {
     (void)self;
-    return fit(args, n, 11, 4, 4, 0, 0, 1, 0);
+    return fit(args, n, 11, 4, 4, 0, 0, 0);
 }
 static PyObject* loss(PyObject* self, PyObject* const* args, Py_ssize_t n)
 {
     (void)self;
-    return fit(args, n, 17, 5, 9, 0, 0, 1, 1);
+    return fit(args, n, 17, 5, 9, 0, 0, 1);
 }
 static PyObject* loss_grad(PyObject* self, PyObject* const* args, Py_ssize_t n)
 {
     (void)self;
-    return fit(args, n, 24, 5, 9, 5, 2, 1, 2);
+    return fit(args, n, 24, 5, 9, 5, 2, 2);
 }
 static PyObject* gather(PyObject* self, PyObject* const* args, Py_ssize_t n)
 {
     (void)self;
-    return fit(args, n, 14, 7, 5, 0, 0, 0, 3);
+    return fit(args, n, 16, 7, 6, 0, 0, 3);
 }
 static PyObject* gather_grad(PyObject* self, PyObject* const* args, Py_ssize_t n)
 {
     (void)self;
-    return fit(args, n, 19, 7, 9, 0, 0, 1, 4);
+    return fit(args, n, 19, 7, 9, 0, 0, 4);
 }
 
 static PyMethodDef methods[] = {{"attend", (PyCFunction)(void (*)(void))attend, METH_FASTCALL, "one decode call"},

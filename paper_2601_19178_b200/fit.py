@@ -22,6 +22,7 @@ from .session import _DT
 # what the workspaces take: functions of the sizes alone
 _sort_bytes = functools.lru_cache(maxsize=512)(B.ckv_sort_indices_bytes)
 _loss_bytes = functools.lru_cache(maxsize=512)(B.ckv_route_loss_bytes)
+_gather_bytes = functools.lru_cache(maxsize=512)(B.ckv_gather_bytes)
 _gather_grad_bytes = functools.lru_cache(maxsize=512)(B.ckv_gather_grad_bytes)
 
 
@@ -124,7 +125,9 @@ def gather(pool: torch.Tensor, idx: torch.Tensor, user: Optional[torch.Tensor], 
     _check("user", user, (n, G, du), pool.dtype, dev)
     _check("score", score, (n, G), torch.float32, dev)
     out = pool.new_empty((n, G, du + ds))
-    B.ckv_gather(dev, dt, n, G, du + ds, ds, m, pool, idx, user if du else None, score, out, stream)
+    nbytes = _gather_bytes(dt, n, G, du + ds, ds, m)
+    ws = pool.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
+    B.ckv_gather(dev, dt, n, G, du + ds, ds, m, pool, idx, user if du else None, score, out, ws, nbytes, stream)
     return out
 
 

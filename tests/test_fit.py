@@ -107,16 +107,17 @@ def test_sizes_are_refused_without_a_gpu():
             assert L.ckv_sort_indices(0, n, G, m, None, None, None, None, 0, None) == want
             assert L.ckv_route_loss(0, n, G, 64, m, *[None] * 9, 0, None) == want
             assert L.ckv_route_loss_grad(0, n, G, 64, m, *[None] * 9, 0.0, 0.0, *[None] * 5, 0, None) == want
-            assert L.ckv_gather(0, 1, n, G, 32, 30, m, *[None] * 6) == want
+            assert L.ckv_gather(0, 1, n, G, 32, 30, m, *[None] * 6, 0, None) == want
+            assert L.ckv_gather_bytes(1, n, G, 32, 30, m, ctypes.byref(v)) == want
             assert L.ckv_gather_grad(0, 1, n, G, 32, 30, m, *[None] * 9, 0, None) == want
     assert L.ckv_sort_indices_bytes(1, 1, 1, None) == bad
     for d in (0, 16, 48, 256):
         assert L.ckv_route_loss_bytes(1, 1, d, 1, ctypes.byref(v), ctypes.byref(w)) == no
         assert L.ckv_route_loss(0, 1, 1, d, 1, *[None] * 9, 0, None) == no
-    assert L.ckv_gather(0, 1, 1, 1, 48, 30, 4, *[None] * 6) == no
-    assert L.ckv_gather(0, 2, 1, 1, 32, 30, 4, *[None] * 6) == bad
+    assert L.ckv_gather(0, 1, 1, 1, 48, 30, 4, *[None] * 6, 0, None) == no
+    assert L.ckv_gather(0, 2, 1, 1, 32, 30, 4, *[None] * 6, 0, None) == bad
     for ds in (0, 33, -1):
-        assert L.ckv_gather(0, 1, 1, 1, 32, ds, 4, *[None] * 6) == ckv.CKV_ERR_SHAPE
+        assert L.ckv_gather(0, 1, 1, 1, 32, ds, 4, *[None] * 6, 0, None) == ckv.CKV_ERR_SHAPE
         assert L.ckv_gather_grad(0, 1, 1, 1, 32, ds, 4, *[None] * 9, 0, None) == ckv.CKV_ERR_SHAPE
 
 
@@ -306,7 +307,8 @@ def test_gpu_gather_off_the_word_boundary():
     for p, u in ((moved(pool), user), (pool, moved(user)), (moved(pool), moved(user))):
         assert torch.equal(ckv.gather(p, idx, u, score), want)
         out = moved(torch.zeros_like(want))
-        ckv.ckv_gather(0, ckv.CKV_BF16, 333, 2, 32, 30, 40, p, idx, u, score, out)
+        need = ckv.ckv_gather_bytes(ckv.CKV_BF16, 333, 2, 32, 30, 40)
+        ckv.ckv_gather(0, ckv.CKV_BF16, 333, 2, 32, 30, 40, p, idx, u, score, out, torch.empty(need, dtype=torch.uint8, device="cuda"), need)
         assert torch.equal(out, want)
     order = ckv.sort_indices(idx, 40)
     want = ckv.gather_grad(pool, order, score, d_out)
@@ -356,7 +358,7 @@ def _gather_case(seed, dtype, n, G, m, D, du, gated, pad=0.2):
 
 GATHERS = [("bf16", 1, 1, 1, 16, 0), ("bf16", 200, 2, 1024, 32, 4), ("f32", 200, 2, 1024, 32, 4), ("bf16", 1000, 3, 77, 64, 1),
            ("bf16", 3001, 1, 5000, 64, 4), ("bf16", 777, 2, 3, 128, 8), ("f32", 999, 4, 50, 16, 3), ("f32", 300, 1, 9, 128, 127),
-           ("bf16", 129, 5, 130, 32, 31), ("bf16", 65, 8, 64, 128, 0), ("f32", 5000, 1, 1, 64, 2), ("bf16", 40000, 2, 300, 32, 2)]
+           ("bf16", 129, 5, 130, 32, 31), ("bf16", 50, 3, 900, 32, 1), ("bf16", 700, 2, 3000, 128, 2), ("bf16", 65, 8, 64, 128, 0), ("f32", 5000, 1, 1, 64, 2), ("bf16", 40000, 2, 300, 32, 2)]
 
 
 @pytest.mark.gpu
