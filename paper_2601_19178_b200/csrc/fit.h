@@ -8,6 +8,16 @@
 
 namespace ckv {
 
+#ifdef __CUDACC__
+// A plain load.  (Kernels that are launched early wait for the ones before them, grid_dependency_wait; loads that promise that their
+// memory does not change during the kernel, __ldg and those of const __restrict__ pointers, need not stay behind that wait.)
+template <typename T>
+__device__ __forceinline__ T ld(const T* p)
+{
+    return *p;
+}
+#endif
+
 // Pieces of a caller's workspace, each on a 256-byte boundary.  A null base only adds up the size.
 struct Carve {
     char* base;
@@ -58,14 +68,29 @@ constexpr int kSweepMaxSplits = 64;
 inline int64_t sweep_padded(int64_t n) { return (n + kSweepPad - 1) / kSweepPad * kSweepPad; }
 struct SweepArgs {
     int64_t n, m, np, mp;           // positions, entries; both padded
-    int G, splits;
+    int G, splits, splits_dw;       // splits_dw: DW's, next to DX's
+    bool join_here;                 // the last of a standing block's blocks joins their results
     const uint16_t *x, *W;          // [n][d], [G][m][d]
     const float *b, *h;             // [G][mp] bias (-inf behind the last entry); h
-    const float *nl, *nr;           // [G][np] -lse (-inf: no weight); -r
-    const uint16_t *b_step, *nl_step;  // b and nl as operands of a product, see put_step
-    float* part;    // LSE: float2 (maximum, sum) [splits][G][np]; MEAN [splits][G][mp]; R [splits][G][np]; DX [splits][n][d]; DW [splits][G][m][d]
-    float* part2;   // DW: sums of T [splits][G][mp]
+    float *nl, *nr;                 // [G][np] -lse (-inf: no weight), which LSE leaves; -r, which R leaves
+    const uint16_t* b_step;         // b and nl as operands of a product, see put_step
+    uint16_t* nl_step;
+    float* part;    // LSE: float2 (maximum, sum) [splits][G][np]; MEAN [splits][G][mp]; R [splits][G][np]; DX [splits][n][d]
+    float *part_dw, *part2;  // DW [splits_dw][G][m][d], and the sums of T [splits_dw][G][mp]
+    unsigned* ticket;   // LSE, MEAN, R: zero; blocks that are done, of each standing block (and group); MEAN: and of each group
+    // LSE, MEAN: indices, scores, results; per block of kSweepPad positions and group the positions that take part, those of them that have
+    // a weight (scores that are not all -inf) and the sum of -log sigmoid(score); per block of as many entries the balance loss's part
+    const int32_t* idx;
+    const float* score;
+    float *lse, *mean, *loss;
+    int32_t *rows_part, *live_part;
+    double *peak_part, *balance_part;
+    // what is joined to DX and DW: the picked entry's coefficient [n][G], and the sums over an entry's positions of what it multiplies and of itself
+    const float *ds, *sum, *wsum;
 };
+inline int64_t sweep_blocks(int64_t rows) { return sweep_padded(rows) / kSweepPad; }
+// tickets of a pass
+int64_t sweep_tickets(int64_t n, int G, int d, int64_t m, int mode);
 #ifdef __CUDACC__
 // A number as three bf16 parts whose sum it is (16 elements per row: 8 rows of 16 bytes, of which the first six hold the parts, then
 // the rows' zero halves), as a K-major operand without swizzle wants it.
@@ -80,7 +105,8 @@ __device__ __forceinline__ void put_step(uint16_t* step, int64_t row, float v)
 }
 #endif
 int sweep_splits(int64_t n, int G, int d, int64_t m, int mode);
-cudaError_t launch_sweep(int mode, int d, SweepArgs& a, cudaStream_t s);  // sets a.splits
+cudaError_t launch_sweep(int mode, int d, SweepArgs& a, cudaStream_t s);  // LSE, MEAN, R, and what joins their partial results
+cudaError_t launch_sweep_grad(int d, SweepArgs& a, cudaStream_t s);       // DX and DW; sets a.splits and a.splits_dw
 
 // ---- kernels_route_loss.cu
 struct RouteLossArgs {

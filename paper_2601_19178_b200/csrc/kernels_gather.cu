@@ -34,15 +34,15 @@ template <int LOAD>
 __device__ __forceinline__ void load16(uint32_t (&w)[4], const void* p)
 {
     if (LOAD == 16) {
-        const uint4 v = __ldg(reinterpret_cast<const uint4*>(p));
+        const uint4 v = ld(reinterpret_cast<const uint4*>(p));
         w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
     } else if (LOAD == 4) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) w[q] = __ldg(reinterpret_cast<const uint32_t*>(p) + q);
+        for (int q = 0; q < 4; ++q) w[q] = ld(reinterpret_cast<const uint32_t*>(p) + q);
     } else {
         const uint16_t* h = reinterpret_cast<const uint16_t*>(p);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) w[q] = __ldg(h + 2 * q) | (uint32_t)__ldg(h + 2 * q + 1) << 16;
+        for (int q = 0; q < 4; ++q) w[q] = ld(h + 2 * q) | (uint32_t)ld(h + 2 * q + 1) << 16;
     }
 }
 
@@ -53,8 +53,8 @@ __device__ __forceinline__ void load16(uint32_t (&w)[4], const void* p)
 // (widened pool) none.
 template <typename E, int LOAD>
 __global__ void __launch_bounds__(256) gather_kernel(int64_t rows, int G, int log_pieces, int log_rows, int skip, int user_width, int user_bytes, int ds, int64_t m, int store,
-                                                     const E* __restrict__ pool, const int32_t* __restrict__ idx,
-                                                     const E* __restrict__ user, const float* __restrict__ score, E* __restrict__ out)
+                                                     const E* pool, const int32_t* idx,
+                                                     const E* user, const float* score, E* out)
 {
     constexpr int N = 16 / (int)sizeof(E), PER = 4 / (int)sizeof(E);  // elements of a piece, of a word
     const int lane = threadIdx.x & 31, bytes = (skip + ds) * (int)sizeof(E);  // skip + ds: a row of `out`
@@ -65,9 +65,9 @@ __global__ void __launch_bounds__(256) gather_kernel(int64_t rows, int G, int lo
         int64_t from = -1;
         float gate = 1.f;
         if (lane < n_rows) {
-            const int32_t j = __ldg(idx + r0 + lane);
+            const int32_t j = ld(idx + r0 + lane);
             if (j >= 0 && j < m) from = ((r0 + lane) % G * m + j) * ds;
-            if (score) gate = sigmoid(__ldg(score + r0 + lane));
+            if (score) gate = sigmoid(ld(score + r0 + lane));
         }
         char* const to = reinterpret_cast<char*>(out) + r0 * bytes;
 #pragma unroll 4
@@ -83,7 +83,7 @@ __global__ void __launch_bounds__(256) gather_kernel(int64_t rows, int G, int lo
 #pragma unroll
                     for (int q = 0; q < N; ++q)
                         if (c + q >= skip) {
-                            const E x = __ldg(pool + at + (c + q - skip));
+                            const E x = ld(pool + at + (c + q - skip));
                             v[q / PER] |= sizeof(E) == 2 ? (uint32_t)(uint16_t)x << (16 * (q % PER)) : __float_as_uint((float)x);
                         }
                 }
@@ -93,16 +93,16 @@ __global__ void __launch_bounds__(256) gather_kernel(int64_t rows, int G, int lo
             }
             if (c < user_width) {
                 const E* u = user + (r0 + k) * user_width + c;
-                if (user_bytes == 4) v[0] = __ldg(reinterpret_cast<const uint32_t*>(u));
+                if (user_bytes == 4) v[0] = ld(reinterpret_cast<const uint32_t*>(u));
                 else if (user_bytes == 8) {
-                    const uint2 x = __ldg(reinterpret_cast<const uint2*>(u));
+                    const uint2 x = ld(reinterpret_cast<const uint2*>(u));
                     v[0] = x.x, v[1] = x.y;
-                } else if (user_bytes == 2) v[0] = (v[0] & 0xffff0000u) | __ldg(reinterpret_cast<const uint16_t*>(u));
+                } else if (user_bytes == 2) v[0] = (v[0] & 0xffff0000u) | ld(reinterpret_cast<const uint16_t*>(u));
                 else
 #pragma unroll
                 for (int q = 0; q < N; ++q)
                     if (c + q < user_width) {
-                        const E x = __ldg(u + q);
+                        const E x = ld(u + q);
                         if (sizeof(E) == 4) v[q / PER] = __float_as_uint((float)x);
                         else v[q / PER] = (v[q / PER] & (q % PER ? 0xffffu : 0xffff0000u)) | (uint32_t)(uint16_t)x << (16 * (q % PER));
                     }
@@ -135,33 +135,39 @@ __device__ __forceinline__ float2 sigmoids(float x)
 }
 
 // The last j in [lo, hi] with offset[j] <= pos; offset[lo] <= pos.
-__device__ __forceinline__ int64_t entry_of(const int32_t* __restrict__ offset, int64_t pos, int64_t lo, int64_t hi)
+__device__ __forceinline__ int64_t entry_of(const int32_t* offset, int64_t pos, int64_t lo, int64_t hi)
 {
     while (lo < hi) {
         const int64_t mid = (lo + hi + 1) / 2;
-        if (__ldg(offset + mid) <= pos) lo = mid;
+        if (ld(offset + mid) <= pos) lo = mid;
         else hi = mid - 1;
     }
     return lo;
 }
-// The same by LANES lanes that look at as many places at a time (all lanes of the warp take part).
+// The same for two positions, by LANES lanes that look at as many places at a time (all lanes of the warp take part).
 template <int LANES>
-__device__ __forceinline__ int64_t entry_of_group(const int32_t* __restrict__ offset, int64_t pos, int64_t hi)
+__device__ __forceinline__ void entries_of_group(const int32_t* offset, const int64_t (&pos)[2], int64_t top, int64_t (&lo)[2])
 {
     const int lane = threadIdx.x & 31, sub = lane % LANES;
     const unsigned mine = (LANES == 32 ? 0xffffffffu : (1u << LANES % 32) - 1) << (lane - sub);
-    int64_t lo = 0;
-    while (__any_sync(0xffffffffu, lo < hi)) {
-        const int64_t at = lo + ((hi - lo) * (sub + 1) + LANES) / (LANES + 1);  // lo < at <= hi, rising with sub
-        const bool below = lo < hi && __ldg(offset + at) <= pos;
-        const int n = __popc(__ballot_sync(0xffffffffu, below) & mine);         // places at or before the entry
-        const int64_t next = n < LANES ? lo + ((hi - lo) * (n + 1) + LANES) / (LANES + 1) - 1 : hi;
-        if (lo < hi) {
-            if (n > 0) lo = lo + ((hi - lo) * n + LANES) / (LANES + 1);
-            hi = next;
+    int64_t hi[2] = {top, top};
+    lo[0] = lo[1] = 0;
+    while (__any_sync(0xffffffffu, lo[0] < hi[0] || lo[1] < hi[1])) {
+        bool below[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int64_t at = lo[k] + ((hi[k] - lo[k]) * (sub + 1) + LANES) / (LANES + 1);  // lo < at <= hi, rising with sub
+            below[k] = lo[k] < hi[k] && ld(offset + at) <= pos[k];
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int n = __popc(__ballot_sync(0xffffffffu, below[k]) & mine);  // places at or before the entry
+            if (lo[k] >= hi[k]) continue;
+            const int64_t wide = hi[k] - lo[k], from = lo[k];
+            if (n > 0) lo[k] = from + (wide * n + LANES) / (LANES + 1);
+            if (n < LANES) hi[k] = from + (wide * (n + 1) + LANES) / (LANES + 1) - 1;
         }
     }
-    return lo;
 }
 
 // Each of LANES lanes has its share of AHEAD rows' sums: added up so that row sub + i LANES ends in dot[i] of lane `sub`.  With every step a
@@ -201,8 +207,8 @@ struct Ends {
 
 // GATED: pool is given, so that the weight is a sigmoid and d_score is wanted.
 template <typename E, int LANES, bool GATED>
-__global__ void __launch_bounds__(kSegThreads, GATED ? 5 : 6) segment_kernel(const SegmentArgs a, float* __restrict__ part, float* __restrict__ wpart,
-                                                                              int32_t* __restrict__ goes_on, int chunk, int wide)
+__global__ void __launch_bounds__(kSegThreads, GATED ? 5 : 6) segment_kernel(const SegmentArgs a, float* part, float* wpart,
+                                                                              int32_t* goes_on, int chunk, int wide)
 {
     constexpr int N = 16 / (int)sizeof(E), GROUPS = kSegThreads / LANES;  // elements of a lane, chunks of a block
     constexpr int AHEAD = LANES < 8 ? 4 : 8, PER = AHEAD > LANES ? AHEAD / LANES : 1;  // rows on their way, looked up by a lane
@@ -217,8 +223,10 @@ __global__ void __launch_bounds__(kSegThreads, GATED ? 5 : 6) segment_kernel(con
     const bool live = begin < end;
     grid_dependency_wait();
     // the entries of the first and the last position (m: no entry)
-    int64_t j = entry_of_group<LANES>(offset, begin, live ? a.m : 0);
-    const int64_t j_last = entry_of_group<LANES>(offset, end - 1, live ? a.m : 0);
+    int64_t ends_at[2];
+    entries_of_group<LANES>(offset, {begin, end - 1}, live ? a.m : 0, ends_at);
+    int64_t j = ends_at[0];
+    const int64_t j_last = ends_at[1];
     int64_t run_end = live && j < a.m ? offset[j + 1] : a.n;
     bool head = live && offset[j] < begin;
     if (sub == 0) info[grp] = Ends{-1, -1, false};
@@ -227,7 +235,7 @@ __global__ void __launch_bounds__(kSegThreads, GATED ? 5 : 6) segment_kernel(con
         if (!GATED) return;
         const E* p = (const E*)a.pool + ((int64_t)g * a.m + j) * ds + col0 - a.skip;
 #pragma unroll
-        for (int q = 0; q < N; ++q) own[q] = j < a.m && col0 + q >= a.skip ? widen(__ldg(p + q)) : 0.f;
+        for (int q = 0; q < N; ++q) own[q] = j < a.m && col0 + q >= a.skip ? widen(ld(p + q)) : 0.f;
     };
     auto flush = [&](bool tail) {
         if (j < a.m) {
@@ -270,7 +278,7 @@ __global__ void __launch_bounds__(kSegThreads, GATED ? 5 : 6) segment_kernel(con
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int64_t t = t0 + sub + i * LANES;
-            ahead[i] = sub + i * LANES < AHEAD && t < end ? __ldg(order + t) : -1;
+            ahead[i] = sub + i * LANES < AHEAD && t < end ? ld(order + t) : -1;
         }
     };
     look_ahead(begin);
@@ -282,7 +290,7 @@ __global__ void __launch_bounds__(kSegThreads, GATED ? 5 : 6) segment_kernel(con
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             pos[i] = ahead[i] < a.n ? ahead[i] : -1;  // (not an order)
-            const float sc = pos[i] >= 0 && a.score ? __ldg(a.score + (int64_t)pos[i] * a.G + g) : 0.f;
+            const float sc = pos[i] >= 0 && a.score ? ld(a.score + (int64_t)pos[i] * a.G + g) : 0.f;
             gate[i] = pos[i] < 0 ? make_float2(0.f, 0.f) : !a.score ? make_float2(1.f, 0.f) : GATED ? sigmoids(sc) : make_float2(sc, 0.f);
             key[i] = (int32_t)j;
         }
@@ -337,10 +345,10 @@ __global__ void __launch_bounds__(kSegThreads, GATED ? 5 : 6) segment_kernel(con
             if (fresh) {
                 flush(false);
                 j = next;
-                run_end = j < a.m ? __ldg(offset + j + 1) : a.n;
                 fetch_pool();
             }
         } while (more);
+        if (mixed) run_end = j < a.m ? ld(offset + j + 1) : a.n;
         if (a.d_user) {
 #pragma unroll
             for (int k = 0; k < AHEAD; ++k) {
@@ -367,7 +375,7 @@ __global__ void __launch_bounds__(kSegThreads, GATED ? 5 : 6) segment_kernel(con
         }
     }
     __syncwarp(mine);
-    if (live) flush(j < a.m && offset[j + 1] > end);
+    if (live) flush(j < a.m && run_end > end);
     __syncthreads();
     // the block's chunks in their order, a thread per column (and one for the weights)
     const int col = threadIdx.x;
@@ -411,8 +419,8 @@ __global__ void __launch_bounds__(kSegThreads, GATED ? 5 : 6) segment_kernel(con
 // behind it, a warp per chunk; runs of many chunks by the whole block, an eighth of the chunks per warp.  Blocks of the second
 // kind: entries without a position.
 constexpr int kJoinWarps = 8, kLongRun = 8;
-__global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const SegmentArgs a, const float* __restrict__ part, const float* __restrict__ wpart,
-                                                               const int32_t* __restrict__ goes_on, int chunks, int chunk, int join_blocks)
+__global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const SegmentArgs a, const float* part, const float* wpart,
+                                                               const int32_t* goes_on, int chunks, int chunk, int join_blocks)
 {
     __shared__ float eighth[kJoinWarps][132];
     __shared__ int32_t entry[kJoinWarps], upto[kJoinWarps];
@@ -421,7 +429,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const SegmentArgs
     grid_dependency_wait();
     if ((int)blockIdx.x >= join_blocks) {
         const int64_t j0 = ((int64_t)((int)blockIdx.x - join_blocks) * kJoinWarps + warp) * 32, j = j0 + lane;
-        unsigned empty = __ballot_sync(0xffffffffu, j < a.m && __ldg(offset + min(j, a.m)) == __ldg(offset + min(j + 1, a.m)));
+        unsigned empty = __ballot_sync(0xffffffffu, j < a.m && ld(offset + min(j, a.m)) == ld(offset + min(j + 1, a.m)));
         if (a.weight_sum && (empty >> lane & 1)) a.weight_sum[(int64_t)g * a.m + j] = 0.f;
         for (; empty; empty &= empty - 1)
             for (int c = lane; c < ds; c += 32) a.sum[((int64_t)g * a.m + j0 + __ffs(empty) - 1) * ds + c] = 0.f;
@@ -434,8 +442,8 @@ __global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const SegmentArgs
             const float* p = part + ((int64_t)g * chunks + k) * 2 * a.width;
 #pragma unroll
             for (int q = 0; q < 4; ++q)
-                if (lane + 32 * q < a.width) sum[q] += __ldg(p + lane + 32 * q);
-            if (a.weight_sum) sum[4] += __ldg(wpart + ((int64_t)g * chunks + k) * 2);
+                if (lane + 32 * q < a.width) sum[q] += ld(p + lane + 32 * q);
+            if (a.weight_sum) sum[4] += ld(wpart + ((int64_t)g * chunks + k) * 2);
         }
     };
     auto put = [&](int64_t j, const float (&sum)[5]) {
@@ -449,13 +457,13 @@ __global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const SegmentArgs
     auto tail_of = [&](int c, float (&sum)[5]) {
         const int64_t at = ((int64_t)g * chunks + c) * 2 + 1;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) sum[q] = lane + 32 * q < a.width ? __ldg(part + at * a.width + lane + 32 * q) : 0.f;
-        sum[4] = a.weight_sum ? __ldg(wpart + at) : 0.f;
+        for (int q = 0; q < 4; ++q) sum[q] = lane + 32 * q < a.width ? ld(part + at * a.width + lane + 32 * q) : 0.f;
+        sum[4] = a.weight_sum ? ld(wpart + at) : 0.f;
     };
     const int c = blockIdx.x * kJoinWarps + warp;
-    const int32_t j = c < chunks ? __ldg(goes_on + (int64_t)g * chunks + c) : -1;
+    const int32_t j = c < chunks ? ld(goes_on + (int64_t)g * chunks + c) : -1;
     int to = 0;
-    if (j >= 0) to = min((__ldg(offset + j + 1) - 1) / chunk + 1, chunks);  // behind the last chunk that holds some of it
+    if (j >= 0) to = min((ld(offset + j + 1) - 1) / chunk + 1, chunks);  // behind the last chunk that holds some of it
     const bool is_long = j >= 0 && to - c > kLongRun;
     if (lane == 0) {
         entry[warp] = is_long ? j : -1;
@@ -536,7 +544,7 @@ cudaError_t launch_segments(const SegmentArgs& a, const SegmentSpace& sp, int bl
 
 // Pool rows behind `skip` zeros, D elements each: every piece of a row then is 16 bytes on a 16-byte boundary.
 template <typename E>
-__global__ void __launch_bounds__(256) widen_pool_kernel(int64_t pieces, int log_pieces, int skip, int ds, const E* __restrict__ pool, uint4* __restrict__ wide)
+__global__ void __launch_bounds__(256) widen_pool_kernel(int64_t pieces, int log_pieces, int skip, int ds, const E* pool, uint4* wide)
 {
     constexpr int N = 16 / (int)sizeof(E);
     const int64_t t = blockIdx.x * (int64_t)256 + threadIdx.x;
@@ -546,7 +554,7 @@ __global__ void __launch_bounds__(256) widen_pool_kernel(int64_t pieces, int log
     const int c = (int)(t - (r << log_pieces)) * N;
     __align__(16) E v[N];
 #pragma unroll
-    for (int q = 0; q < N; ++q) v[q] = c + q >= skip ? __ldg(pool + r * ds + (c + q - skip)) : (E)0;
+    for (int q = 0; q < N; ++q) v[q] = c + q >= skip ? ld(pool + r * ds + (c + q - skip)) : (E)0;
     wide[t] = *reinterpret_cast<const uint4*>(v);
 }
 

@@ -13,7 +13,8 @@
 //   R     positions stand, entries stream:  sum_j p_ij h_j
 //   DX    positions stand, entries of all groups stream:  sum_j T_ij W_j
 //   DW    entries stand, positions stream:  sum_i T_ij x_i, sum_i T_ij
-// and what streams is shared out among `splits` blocks, whose partial results are joined in their order.
+// and what streams is shared out among `splits` blocks, of which the last one joins their partial results in their order
+// (kernels_route_sweep.cu), but for those of DX and DW.
 #include <cuda_bf16.h>
 #include <math_constants.h>
 
@@ -36,34 +37,37 @@ struct Space {
     uint16_t *b_step, *nl_step;  // b and nl as operands of a product
     uint16_t* xs;        // x with zeros for a position that takes part in no group
     float* part;         // partial results of a pass
-    float* part2;
-    // forward, per block of 256 positions and group: those that take part, those of them that have a weight (scores that are not all
-    // -inf), the sum of -log sigmoid(score);  per block of entries and group: the sum for the balance loss
-    int32_t *rows_part, *live_part;
+    float *part_dw, *part2;
+    int32_t *rows_part, *live_part;  // forward, see SweepArgs
     double *peak_part, *balance_part;
-    unsigned* done;      // [G] blocks of entries that are done
     float *ds, *sum, *wsum;  // gradient: coefficient of the picked entry [n][G], sums over an entry's positions
     void* seg;
+    unsigned* ticket[5];     // of the passes LSE, MEAN and R, back to back
+    int64_t n_tickets;
     int64_t bytes;
 };
-constexpr int kMeanEntries = 1024;  // of a block of mean_join_kernel
 
 Space layout(void* ws, int64_t n, int G, int d, int64_t m, bool grad)
 {
     Carve c(ws);
     Space s{};
-    const int64_t np = sweep_padded(n), mp = sweep_padded(m), blocks = (np + 255) / 256;
+    const int64_t np = sweep_padded(n), mp = sweep_padded(m);
+    for (int mode = grad ? SWEEP_R : SWEEP_LSE; mode <= (grad ? SWEEP_R : SWEEP_MEAN); ++mode) s.n_tickets += sweep_tickets(n, G, d, m, mode);
+    unsigned* ticket = c.take<unsigned>(s.n_tickets);
+    for (int mode = grad ? SWEEP_R : SWEEP_LSE; ticket && mode <= (grad ? SWEEP_R : SWEEP_MEAN); ++mode) {
+        s.ticket[mode] = ticket;
+        ticket += sweep_tickets(n, G, d, m, mode);
+    }
     s.b = c.take<float>(G * mp);
     s.nl = c.take<float>(G * np);
     s.b_step = c.take<uint16_t>(G * mp * 16);
     s.nl_step = c.take<uint16_t>(G * np * 16);
     s.xs = c.take<uint16_t>(n * d);
     if (!grad) {
-        s.rows_part = c.take<int32_t>(blocks * G);
-        s.live_part = c.take<int32_t>(blocks * G);
-        s.peak_part = c.take<double>(blocks * G);
-        s.balance_part = c.take<double>((m + kMeanEntries - 1) / kMeanEntries * G);
-        s.done = c.take<unsigned>(G);
+        s.rows_part = c.take<int32_t>(sweep_blocks(n) * G);
+        s.live_part = c.take<int32_t>(sweep_blocks(n) * G);
+        s.peak_part = c.take<double>(sweep_blocks(n) * G);
+        s.balance_part = c.take<double>(sweep_blocks(m) * G);
         s.part = c.take<float>(std::max(2 * sweep_splits(n, G, d, m, SWEEP_LSE) * G * np, sweep_splits(n, G, d, m, SWEEP_MEAN) * G * mp));
     } else {
         s.h = c.take<float>(G * mp);
@@ -71,7 +75,8 @@ Space layout(void* ws, int64_t n, int G, int d, int64_t m, bool grad)
         s.ds = c.take<float>(n * G);
         s.sum = c.take<float>(G * m * d);
         s.wsum = c.take<float>(G * m);
-        s.part = c.take<float>(std::max(std::max(sweep_splits(n, G, d, m, SWEEP_R) * G * np, sweep_splits(n, G, d, m, SWEEP_DX) * n * d), sweep_splits(n, G, d, m, SWEEP_DW) * G * m * d));
+        s.part = c.take<float>(std::max(sweep_splits(n, G, d, m, SWEEP_R) * G * np, sweep_splits(n, G, d, m, SWEEP_DX) * n * d));
+        s.part_dw = c.take<float>(sweep_splits(n, G, d, m, SWEEP_DW) * G * m * d);
         s.part2 = c.take<float>(sweep_splits(n, G, d, m, SWEEP_DW) * G * mp);
         s.seg = c.take<char>(segment_workspace(n, G, d));
     }
@@ -82,7 +87,6 @@ Space layout(void* ws, int64_t n, int G, int d, int64_t m, bool grad)
 // ---- what the passes read
 __device__ __forceinline__ void prepare_entry(const RouteLossArgs& a, const RouteGradArgs& b, const Space& s, int64_t mp, int g, int64_t j)
 {
-    if (j == 0 && s.done) s.done[g] = 0;
     if (j >= mp) return;
     const float bias = j < a.m ? (a.bias ? a.bias[g * a.m + j] : 0.f) : -CUDART_INF_F;
     s.b[g * mp + j] = bias;
@@ -103,6 +107,7 @@ __global__ void __launch_bounds__(256) prepare_kernel(const RouteLossArgs a, con
 {
     constexpr int LANES = D / 8;
     grid_dependency_wait();
+    for (int64_t t = blockIdx.x * (int64_t)256 + threadIdx.x; t < s.n_tickets; t += (int64_t)gridDim.x * 256) (GRAD ? s.ticket[SWEEP_R] : s.ticket[SWEEP_LSE])[t] = 0;
     if ((int)blockIdx.x < entry_blocks) {
         const int per_group = entry_blocks / a.G;
         prepare_entry(a, b, s, mp, (int)blockIdx.x / per_group, (int64_t)((int)blockIdx.x % per_group) * 256 + threadIdx.x);
@@ -114,7 +119,7 @@ __global__ void __launch_bounds__(256) prepare_kernel(const RouteLossArgs a, con
     uint4 raw = make_uint4(0, 0, 0, 0);
     if (there) {
         const uint16_t* x = (const uint16_t*)a.x + i * D + 8 * sub;
-        if (whole) raw = __ldg(reinterpret_cast<const uint4*>(x));
+        if (whole) raw = ld(reinterpret_cast<const uint4*>(x));
         else {
             uint32_t w[4];
 #pragma unroll
@@ -126,11 +131,11 @@ __global__ void __launch_bounds__(256) prepare_kernel(const RouteLossArgs a, con
     int any = 0;
     if (GRAD) {
         for (int g = sub; g < a.G; g += LANES) {
-            const int32_t k = there ? __ldg(a.idx + i * a.G + g) : -1;
+            const int32_t k = there ? ld(a.idx + i * a.G + g) : -1;
             const bool real = k >= 0 && k < a.m;
             any |= real;
             if (i < np) {
-                const float lse = real ? __ldg(a.lse + i * a.G + g) : -CUDART_INF_F;
+                const float lse = real ? ld(a.lse + i * a.G + g) : -CUDART_INF_F;
                 const float nl = lse == -CUDART_INF_F ? lse : -lse;
                 s.nl[g * np + i] = nl;
                 put_step(s.nl_step, g * np + i, nl);
@@ -138,9 +143,9 @@ __global__ void __launch_bounds__(256) prepare_kernel(const RouteLossArgs a, con
             if (there) {
                 float v = 0.f;
                 if (real) {
-                    const int32_t rows = __ldg(b.offset + (int64_t)g * (a.m + 1) + a.m);
-                    v = -b.w_peak / (float)max(rows, 1) * sigmoid(-__ldg(a.score + i * a.G + g));
-                    if (b.d_score) v += __ldg(b.d_score + i * a.G + g);
+                    const int32_t rows = ld(b.offset + (int64_t)g * (a.m + 1) + a.m);
+                    v = -b.w_peak / (float)max(rows, 1) * sigmoid(-ld(a.score + i * a.G + g));
+                    if (b.d_score) v += ld(b.d_score + i * a.G + g);
                 }
                 s.ds[i * a.G + g] = v;
             }
@@ -150,12 +155,12 @@ __global__ void __launch_bounds__(256) prepare_kernel(const RouteLossArgs a, con
     } else {
 #pragma unroll 2
         for (int g = 0; g < a.G; ++g) {
-            const int32_t k = there ? __ldg(a.idx + i * a.G + g) : -1;
+            const int32_t k = there ? ld(a.idx + i * a.G + g) : -1;
             const bool real = k >= 0 && k < a.m;
             any |= real;
             float sc = 0.f;
             if (real) {
-                const uint4 w = __ldg(reinterpret_cast<const uint4*>((const uint16_t*)a.W + ((int64_t)g * a.m + k) * D) + sub);
+                const uint4 w = ld(reinterpret_cast<const uint4*>((const uint16_t*)a.W + ((int64_t)g * a.m + k) * D) + sub);
                 const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
@@ -165,152 +170,17 @@ __global__ void __launch_bounds__(256) prepare_kernel(const RouteLossArgs a, con
             }
 #pragma unroll
             for (int d = LANES / 2; d > 0; d /= 2) sc += __shfl_xor_sync(0xffffffffu, sc, d);
-            if (sub == 0 && there) a.score[i * a.G + g] = real && a.bias ? sc + __ldg(a.bias + (int64_t)g * a.m + k) : sc;
+            if (sub == 0 && there) a.score[i * a.G + g] = real && a.bias ? sc + ld(a.bias + (int64_t)g * a.m + k) : sc;
         }
     }
     if (there) reinterpret_cast<uint4*>(s.xs + i * D)[sub] = any ? raw : make_uint4(0, 0, 0, 0);
 }
 
 // ---- joins
-// Sums over the 256 threads of a block, in a fixed order.
-template <int N>
-__device__ __forceinline__ void block_sum(double (&v)[N])
-{
-    __shared__ double part[N][8];
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < N; ++k) {
-#pragma unroll
-        for (int d = 16; d > 0; d /= 2) v[k] += __shfl_xor_sync(0xffffffffu, v[k], d);
-        if ((threadIdx.x & 31) == 0) part[k][threadIdx.x >> 5] = v[k];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < N; ++k) {
-        v[k] = 0;
-#pragma unroll
-        for (int w = 0; w < 8; ++w) v[k] += part[k][w];
-    }
-}
-
-__global__ void __launch_bounds__(256) lse_join_kernel(const RouteLossArgs a, const SweepArgs p, const Space s)
-{
-    const int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x;
-    const int g = blockIdx.y;
-    grid_dependency_wait();
-    const int32_t k = i < a.n ? __ldg(a.idx + i * a.G + g) : -1;
-    const bool real = k >= 0 && k < a.m;
-    float lse = 0.f, neg = -CUDART_INF_F;
-    double soft = 0;
-    if (real) {
-        const float2* part = reinterpret_cast<const float2*>(p.part) + g * p.np + i;
-        const int64_t step = a.G * p.np;
-        float top = -CUDART_INF_F, sum = 0.f;
-        for (int z = 0; z < p.splits; ++z) {
-            const float2 v = part[z * step];
-            const float both = fmaxf(top, v.x);
-            if (both > -CUDART_INF_F) sum = sum * expf(top - both) + v.y * expf(v.x - both);
-            top = both;
-        }
-        if (top == -CUDART_INF_F) lse = top;  // every entry's score is -inf: no weight anywhere
-        else {
-            lse = top + logf(sum);
-            neg = -lse;
-        }
-        const float sc = a.score[i * a.G + g];
-        soft = fmaxf(-sc, 0.f) + log1pf(expf(-fabsf(sc)));  // -log sigmoid(sc)
-    }
-    if (i < p.np) {
-        s.nl[g * p.np + i] = neg;
-        put_step(s.nl_step, g * p.np + i, neg);
-    }
-    if (i < a.n) a.lse[i * a.G + g] = lse;
-    const int rows = __syncthreads_count(real), live = __syncthreads_count(neg != -CUDART_INF_F);
-    double sum1[1] = {soft};
-    block_sum(sum1);
-    if (threadIdx.x == 0) {
-        const int64_t at = (int64_t)g * gridDim.x + blockIdx.x;
-        s.rows_part[at] = rows;
-        s.live_part[at] = live;
-        s.peak_part[at] = sum1[0];
-    }
-}
-
-// The mean weights, and in a group's last block both losses, from partial sums in the order of the blocks.  mean log(mean m) is
-// summed as (u log u - u + 1) / m with u = mean m: the weights sum to one, so that nothing is added, and near balance, where u
-// log u and the sum's other terms cancel, each term is as small as what it stands for.  (They sum to less by the share of the
-// positions that have no weight.)
-__global__ void __launch_bounds__(256) mean_join_kernel(const RouteLossArgs a, const SweepArgs p, const Space s, int blocks)
-{
-    __shared__ bool last;
-    const int g = blockIdx.y;
-    grid_dependency_wait();
-    // what the last block wants is asked for at once by all
-    double of_rows[3] = {};  // positions that take part, those with a weight, peak losses
-    for (int b = threadIdx.x; b < blocks; b += 256) {
-        of_rows[0] += s.rows_part[(int64_t)g * blocks + b];
-        of_rows[1] += s.live_part[(int64_t)g * blocks + b];
-        of_rows[2] += s.peak_part[(int64_t)g * blocks + b];
-    }
-    float sum[kMeanEntries / 256];
-#pragma unroll
-    for (int q = 0; q < kMeanEntries / 256; ++q) {
-        const int64_t j = blockIdx.x * (int64_t)kMeanEntries + q * 256 + threadIdx.x;
-        sum[q] = 0.f;
-        if (j < a.m)
-#pragma unroll 4
-            for (int z = 0; z < p.splits; ++z) sum[q] += p.part[((int64_t)z * a.G + g) * p.mp + j];
-    }
-    block_sum(of_rows);
-    const double rows = of_rows[0];
-    const float inv = rows > 0 ? (float)(1.0 / rows) : 0.f;
-    double balance[1] = {};
-#pragma unroll
-    for (int q = 0; q < kMeanEntries / 256; ++q) {
-        const int64_t j = blockIdx.x * (int64_t)kMeanEntries + q * 256 + threadIdx.x;
-        if (j >= a.m) continue;
-        const float mean = sum[q] * inv;
-        a.mean[(int64_t)g * a.m + j] = mean;
-        const double u = (double)mean * (double)a.m;
-        balance[0] += (u > 0 ? u * log(u) : u * 0) - u + 1;
-    }
-    block_sum(balance);
-    if (threadIdx.x == 0) {
-        s.balance_part[(int64_t)g * gridDim.x + blockIdx.x] = balance[0];
-        __threadfence();
-        last = atomicAdd(s.done + g, 1u) + 1 == gridDim.x;
-        __threadfence();
-    }
-    __syncthreads();
-    if (!last) return;
-    if (gridDim.x > 1) {
-        balance[0] = 0;
-        for (int b = threadIdx.x; b < (int)gridDim.x; b += 256) balance[0] += *(volatile double*)(s.balance_part + (int64_t)g * gridDim.x + b);
-        block_sum(balance);
-    }
-    if (threadIdx.x == 0) {
-        a.loss[2 * g] = rows > 0 ? (float)(balance[0] / (double)a.m + (of_rows[1] - rows) / rows) : 0.f;
-        a.loss[2 * g + 1] = rows > 0 ? (float)(of_rows[2] / rows) : 0.f;
-    }
-}
-
-__global__ void __launch_bounds__(256) r_join_kernel(const SweepArgs p, float* __restrict__ nr)
-{
-    const int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x;
-    const int g = blockIdx.y;
-    grid_dependency_wait();
-    if (i >= p.np) return;
-    float sum = 0.f;
-    if (i < p.n)
-#pragma unroll 4
-        for (int z = 0; z < p.splits; ++z) sum += p.part[((int64_t)z * p.G + g) * p.np + i];
-    nr[g * p.np + i] = -sum;
-}
-
 // Eight elements of a row: partial sums added in their order, and rounded.
 __device__ __forceinline__ void add8(float (&v)[8], const float* p)
 {
-    const float4 x = __ldg(reinterpret_cast<const float4*>(p)), y = __ldg(reinterpret_cast<const float4*>(p) + 1);
+    const float4 x = ld(reinterpret_cast<const float4*>(p)), y = ld(reinterpret_cast<const float4*>(p) + 1);
     v[0] += x.x, v[1] += x.y, v[2] += x.z, v[3] += x.w, v[4] += y.x, v[5] += y.y, v[6] += y.z, v[7] += y.w;
 }
 __device__ __forceinline__ void put8(uint16_t* out, const float (&v)[8], bool whole)
@@ -324,48 +194,45 @@ __device__ __forceinline__ void put8(uint16_t* out, const float (&v)[8], bool wh
     }
 }
 
-// dx: the partial sums, and the picked entries' rows
-__global__ void __launch_bounds__(256) dx_join_kernel(const RouteLossArgs a, const RouteGradArgs b, const SweepArgs p, const float* __restrict__ ds)
+// The first dx_blocks blocks: dx, the partial sums and the picked entries' rows.  The others: dW and db, the partial sums and the sums over the
+// positions that picked the entry.
+__global__ void __launch_bounds__(256) grad_join_kernel(const RouteLossArgs a, const RouteGradArgs b, const SweepArgs p, int dx_blocks)
 {
-    const int64_t e = (blockIdx.x * (int64_t)256 + threadIdx.x) * 8, total = a.n * a.d;
     grid_dependency_wait();
-    if (e >= total) return;
-    const int64_t i = e / a.d;
-    const int c = (int)(e - i * a.d);
     float v[8] = {};
+    if ((int)blockIdx.x < dx_blocks) {
+        const int64_t e = (blockIdx.x * (int64_t)256 + threadIdx.x) * 8, total = a.n * a.d;
+        if (e >= total) return;
+        const int64_t i = e / a.d;
+        const int c = (int)(e - i * a.d);
 #pragma unroll 4
-    for (int z = 0; z < p.splits; ++z) add8(v, p.part + z * total + e);
+        for (int z = 0; z < p.splits; ++z) add8(v, p.part + z * total + e);
 #pragma unroll 4
-    for (int g = 0; g < a.G; ++g) {
-        const int32_t k = __ldg(a.idx + i * a.G + g);
-        if (k < 0 || k >= a.m) continue;
-        const float f = __ldg(ds + i * a.G + g);
-        const uint4 w = __ldg(reinterpret_cast<const uint4*>((const uint16_t*)a.W + ((int64_t)g * a.m + k) * a.d + c));
-        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+        for (int g = 0; g < a.G; ++g) {
+            const int32_t k = ld(a.idx + i * a.G + g);
+            if (k < 0 || k >= a.m) continue;
+            const float f = ld(p.ds + i * a.G + g);
+            const uint4 w = ld(reinterpret_cast<const uint4*>(p.W + ((int64_t)g * a.m + k) * a.d + c));
+            const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            v[2 * q] = fmaf(f, __uint_as_float(u[q] << 16), v[2 * q]);
-            v[2 * q + 1] = fmaf(f, __uint_as_float(u[q] & 0xffff0000u), v[2 * q + 1]);
+            for (int q = 0; q < 4; ++q) {
+                v[2 * q] = fmaf(f, __uint_as_float(u[q] << 16), v[2 * q]);
+                v[2 * q + 1] = fmaf(f, __uint_as_float(u[q] & 0xffff0000u), v[2 * q + 1]);
+            }
         }
+        put8((uint16_t*)b.dx + e, v, ((uintptr_t)b.dx & 15) == 0);
+        return;
     }
-    put8((uint16_t*)b.dx + e, v, ((uintptr_t)b.dx & 15) == 0);
-}
-
-// dW and db: the partial sums, and the sums over the positions that picked the entry
-__global__ void __launch_bounds__(256) dw_join_kernel(const RouteLossArgs a, const RouteGradArgs b, const SweepArgs p, const Space s)
-{
-    const int64_t e = (blockIdx.x * (int64_t)256 + threadIdx.x) * 8, total = a.G * a.m * a.d;
-    grid_dependency_wait();
+    const int64_t e = ((int64_t)((int)blockIdx.x - dx_blocks) * 256 + threadIdx.x) * 8, total = a.G * a.m * a.d;
     if (e >= total) return;
-    float v[8] = {};
-    add8(v, s.sum + e);
+    add8(v, p.sum + e);
 #pragma unroll 4
-    for (int z = 0; z < p.splits; ++z) add8(v, p.part + z * total + e);
+    for (int z = 0; z < p.splits_dw; ++z) add8(v, p.part_dw + z * total + e);
     put8((uint16_t*)b.dW + e, v, ((uintptr_t)b.dW & 15) == 0);
     if (b.dbias && e % a.d == 0) {
         const int64_t row = e / a.d, g = row / a.m;
-        float db = s.wsum[row];
-        for (int z = 0; z < p.splits; ++z) db += p.part2[((int64_t)z * a.G + g) * p.mp + (row - g * a.m)];
+        float db = ld(p.wsum + row);
+        for (int z = 0; z < p.splits_dw; ++z) db += ld(p.part2 + ((int64_t)z * a.G + g) * p.mp + (row - g * a.m));
         b.dbias[row] = db;
     }
 }
@@ -382,7 +249,21 @@ cudaError_t launch_prepare(const RouteLossArgs& a, const RouteGradArgs& b, const
 
 SweepArgs pass_args(const RouteLossArgs& a, const Space& s)
 {
-    return SweepArgs{a.n, a.m, sweep_padded(a.n), sweep_padded(a.m), a.G, 1, s.xs, (const uint16_t*)a.W, s.b, s.h, s.nl, s.nr, s.b_step, s.nl_step, s.part, s.part2};
+    SweepArgs p{};
+    p.n = a.n, p.m = a.m, p.np = sweep_padded(a.n), p.mp = sweep_padded(a.m);
+    p.G = a.G;
+    p.x = s.xs, p.W = (const uint16_t*)a.W;
+    p.b = s.b, p.h = s.h, p.nl = s.nl, p.nr = s.nr, p.b_step = s.b_step, p.nl_step = s.nl_step;
+    p.part = s.part, p.part_dw = s.part_dw, p.part2 = s.part2;
+    p.idx = a.idx, p.score = a.score, p.lse = a.lse, p.mean = a.mean, p.loss = a.loss;
+    p.rows_part = s.rows_part, p.live_part = s.live_part, p.peak_part = s.peak_part, p.balance_part = s.balance_part;
+    p.ds = s.ds, p.sum = s.sum, p.wsum = s.wsum;
+    return p;
+}
+cudaError_t pass(int mode, int d, SweepArgs& p, const Space& s, cudaStream_t st)
+{
+    p.ticket = s.ticket[mode];
+    return launch_sweep(mode, d, p, st);
 }
 
 }  // namespace
@@ -400,21 +281,15 @@ cudaError_t launch_route_loss(const RouteLossArgs& a, void* ws, cudaStream_t st)
 {
     const Space s = layout(ws, a.n, a.G, a.d, a.m, false);
     SweepArgs p = pass_args(a, s);
-    const Launch l{st, nullptr, nullptr, true};
-    const unsigned blocks = (unsigned)((p.np + 255) / 256), G = (unsigned)a.G;
     TRY(launch_prepare<false>(a, RouteGradArgs{}, s, a.n, p.np, p.mp, st));
-    TRY(launch_sweep(SWEEP_LSE, a.d, p, st));
-    if (a.n) TRY(launch_kernel(l, lse_join_kernel, dim3(blocks, G), 256, 0, 1, a, p, s));
-    TRY(launch_sweep(SWEEP_MEAN, a.d, p, st));
-    return launch_kernel(l, mean_join_kernel, dim3((unsigned)((a.m + kMeanEntries - 1) / kMeanEntries), G), 256, 0, 1, a, p, s, (int)blocks);
+    TRY(pass(SWEEP_LSE, a.d, p, s, st));
+    return pass(SWEEP_MEAN, a.d, p, s, st);
 }
 
 cudaError_t launch_route_grad(const RouteLossArgs& a, const RouteGradArgs& b, void* ws, cudaStream_t st)
 {
     const Space s = layout(ws, a.n, a.G, a.d, a.m, true);
     SweepArgs p = pass_args(a, s);
-    const Launch l{st, nullptr, nullptr, true};
-    const unsigned G = (unsigned)a.G;
     TRY(launch_prepare<true>(a, b, s, a.n ? p.np : 0, p.np, p.mp, st));
     SegmentArgs seg{};
     seg.order = b.order;
@@ -429,12 +304,10 @@ cudaError_t launch_route_grad(const RouteLossArgs& a, const RouteGradArgs& b, vo
     seg.sum = s.sum;
     seg.weight_sum = s.wsum;
     TRY(launch_segment_sum(CKV_BF16, seg, s.seg, st));
-    TRY(launch_sweep(SWEEP_R, a.d, p, st));
-    if (a.n) TRY(launch_kernel(l, r_join_kernel, dim3((unsigned)((p.np + 255) / 256), G), 256, 0, 1, p, s.nr));
-    TRY(launch_sweep(SWEEP_DX, a.d, p, st));
-    if (a.n) TRY(launch_kernel(l, dx_join_kernel, dim3((unsigned)((a.n * a.d / 8 + 255) / 256)), 256, 0, 1, a, b, p, s.ds));
-    TRY(launch_sweep(SWEEP_DW, a.d, p, st));
-    return launch_kernel(l, dw_join_kernel, dim3((unsigned)((a.G * a.m * a.d / 8 + 255) / 256)), 256, 0, 1, a, b, p, s);
+    TRY(pass(SWEEP_R, a.d, p, s, st));
+    TRY(launch_sweep_grad(a.d, p, st));
+    const int64_t dx_blocks = (a.n * a.d / 8 + 255) / 256, dw_blocks = (a.G * a.m * a.d / 8 + 255) / 256;
+    return launch_kernel(Launch{st, nullptr, nullptr, true}, grad_join_kernel, dim3((unsigned)(dx_blocks + dw_blocks)), 256, 0, 1, a, b, p, (int)dx_blocks);
 }
 
 }  // namespace ckv

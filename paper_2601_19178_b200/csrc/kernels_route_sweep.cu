@@ -24,6 +24,13 @@
 namespace ckv {
 namespace {
 
+// LSE, MEAN, R: three blocks of standing rows per CTA, four reading warps and an issuing one each, and a loading warp
+constexpr int kBlocks = 3, kRows = 128 * kBlocks;
+static_assert(kRows == kSweepPad, "a standing block is one of the blocks that the arrays are padded to");
+constexpr int kReadWarps = 4 * kBlocks, kIssueWarp = kReadWarps, kLoadWarp = kIssueWarp + kBlocks;
+constexpr int kSweepThreads = (kLoadWarp + 1) * 32;
+constexpr int kStages = 6;
+
 constexpr uint32_t kSpin = 1u << 18, kSuspend = 4000;
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -254,6 +261,144 @@ struct LongSum {
     }
 };
 
+// ---- LSE, MEAN, R: joining the partial results of the blocks that shared a standing block's streaming rows, in the order of those blocks: by
+// the one of them that is done last where all run at a time, else in a launch of its own.  (200 positions x 1024 entries x 2
+// groups, both losses: 23 us and 28; 32768 x 16384 x 4, in seven rounds of blocks that each wait for their stores: 1030 and 984.)
+
+// Every thread's results stand in memory: true in the block that is the last of n_blocks to say so.
+__device__ __forceinline__ bool last_of(unsigned* ticket, unsigned n_blocks)
+{
+    __shared__ bool last;
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0) last = atomicAdd(ticket, 1u) + 1 == n_blocks;
+    __syncthreads();
+    __threadfence();
+    return last;
+}
+// Sums over the threads of a block, in a fixed order.
+template <int N>
+__device__ __forceinline__ void block_sum(double (&v)[N])
+{
+    __shared__ double part[N][kSweepThreads / 32];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+#pragma unroll
+        for (int d = 16; d > 0; d /= 2) v[k] += __shfl_xor_sync(0xffffffffu, v[k], d);
+        if ((threadIdx.x & 31) == 0) part[k][threadIdx.x >> 5] = v[k];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        v[k] = 0;
+#pragma unroll
+        for (int w = 0; w < kSweepThreads / 32; ++w) v[k] += part[k][w];
+    }
+}
+
+// lse of position row0 + thread (the first kSweepPad threads), and what the peak loss and the mean weights want of the block's positions.
+__device__ __forceinline__ void join_lse(const SweepArgs& a, int g, int64_t row0)
+{
+    const int64_t i = row0 + threadIdx.x;
+    const bool has_row = threadIdx.x < kSweepPad;
+    const int32_t k = has_row && i < a.n ? ld(a.idx + i * a.G + g) : -1;
+    const bool real = k >= 0 && k < a.m;
+    float lse = 0.f, neg = -CUDART_INF_F;
+    double soft[1] = {};
+    if (real) {
+        const float sc = ld(a.score + i * a.G + g);
+        const float2* part = reinterpret_cast<const float2*>(a.part) + g * a.np + i;
+        const int64_t step = a.G * a.np;
+        float top = -CUDART_INF_F, sum = 0.f;
+#pragma unroll 4
+        for (int z = 0; z < a.splits; ++z) {
+            const float2 v = __ldcg(part + z * step);
+            const float both = fmaxf(top, v.x);
+            if (both > -CUDART_INF_F) sum = sum * expf(top - both) + v.y * expf(v.x - both);
+            top = both;
+        }
+        if (top == -CUDART_INF_F) lse = top;  // every entry's score is -inf: no weight anywhere
+        else {
+            lse = top + logf(sum);
+            neg = -lse;
+        }
+        soft[0] = fmaxf(-sc, 0.f) + log1pf(expf(-fabsf(sc)));  // -log sigmoid(sc)
+    }
+    if (has_row) {
+        a.nl[g * a.np + i] = neg;
+        put_step(a.nl_step, g * a.np + i, neg);
+        if (i < a.n) a.lse[i * a.G + g] = lse;
+    }
+    const int rows = __syncthreads_count(real), live = __syncthreads_count(neg != -CUDART_INF_F);
+    block_sum<1>(soft);
+    if (threadIdx.x == 0) {
+        const int64_t at = g * (a.np / kSweepPad) + row0 / kSweepPad;
+        a.rows_part[at] = rows;
+        a.live_part[at] = live;
+        a.peak_part[at] = soft[0];
+    }
+}
+
+// The mean weight of entry row0 + thread, and in a group's last block both losses, from partial sums in the order of the blocks.
+// mean log(mean m) is summed as (u log u - u + 1) / m with u = mean m: the weights sum to one, so that nothing is added, and near
+// balance, where u log u and the sum's other terms cancel, each term is as small as what it stands for.  (They sum to less by
+// the share of the positions that have no weight.)
+__device__ __forceinline__ void join_mean(const SweepArgs& a, int g, int64_t row0)
+{
+    const int blocks = (int)(a.np / kSweepPad), entry_blocks = (int)(a.mp / kSweepPad);
+    double of_rows[3] = {};  // positions that take part, those with a weight, peak losses
+    for (int b = threadIdx.x; b < blocks; b += kSweepThreads) {
+        of_rows[0] += a.rows_part[(int64_t)g * blocks + b];
+        of_rows[1] += a.live_part[(int64_t)g * blocks + b];
+        of_rows[2] += a.peak_part[(int64_t)g * blocks + b];
+    }
+    const int64_t j = row0 + threadIdx.x;
+    const bool real = threadIdx.x < kSweepPad && j < a.m;
+    float sum = 0.f;
+    if (real)
+#pragma unroll 4
+        for (int z = 0; z < a.splits; ++z) sum += __ldcg(a.part + ((int64_t)z * a.G + g) * a.mp + j);
+    block_sum<3>(of_rows);
+    const double rows = of_rows[0];
+    double balance[1] = {};
+    if (real) {
+        const float mean = rows > 0 ? sum * (float)(1.0 / rows) : 0.f;
+        a.mean[(int64_t)g * a.m + j] = mean;
+        const double u = (double)mean * (double)a.m;
+        balance[0] = (u > 0 ? u * log(u) : u * 0) - u + 1;
+    }
+    block_sum<1>(balance);
+    if (threadIdx.x == 0) a.balance_part[(int64_t)g * entry_blocks + row0 / kSweepPad] = balance[0];
+    if (!last_of(a.ticket + (int64_t)a.G * entry_blocks + g, (unsigned)entry_blocks)) return;
+    balance[0] = 0;
+    for (int b = threadIdx.x; b < entry_blocks; b += kSweepThreads) balance[0] += __ldcg(a.balance_part + (int64_t)g * entry_blocks + b);
+    block_sum<1>(balance);
+    if (threadIdx.x == 0) {
+        a.loss[2 * g] = rows > 0 ? (float)(balance[0] / (double)a.m + (of_rows[1] - rows) / rows) : 0.f;
+        a.loss[2 * g + 1] = rows > 0 ? (float)(of_rows[2] / rows) : 0.f;
+    }
+}
+
+__device__ __forceinline__ void join_r(const SweepArgs& a, int g, int64_t row0)
+{
+    const int64_t i = row0 + threadIdx.x;
+    if (threadIdx.x >= kSweepPad) return;
+    float sum = 0.f;
+    if (i < a.n)
+#pragma unroll 4
+        for (int z = 0; z < a.splits; ++z) sum += __ldcg(a.part + ((int64_t)z * a.G + g) * a.np + i);
+    a.nr[g * a.np + i] = -sum;
+}
+
+template <int MODE>
+__device__ __forceinline__ void join(const SweepArgs& a, int g, int64_t row0)
+{
+    if (MODE == SWEEP_LSE) join_lse(a, g, row0);
+    else if (MODE == SWEEP_MEAN) join_mean(a, g, row0);
+    else join_r(a, g, row0);
+}
+
 // Where a row's inputs come from, and its A operand: two bf16 per TMEM column, zeros for a row that is none.
 template <int DIN>
 __device__ __forceinline__ void load_inputs(uint32_t taddr, const uint16_t* row, bool in)
@@ -264,7 +409,7 @@ __device__ __forceinline__ void load_inputs(uint32_t taddr, const uint16_t* row,
         uint32_t v[16];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            const uint4 w = in ? __ldg(src + 4 * h + q) : make_uint4(0, 0, 0, 0);
+            const uint4 w = in ? ld(src + 4 * h + q) : make_uint4(0, 0, 0, 0);
             v[4 * q] = w.x;
             v[4 * q + 1] = w.y;
             v[4 * q + 2] = w.z;
@@ -275,12 +420,7 @@ __device__ __forceinline__ void load_inputs(uint32_t taddr, const uint16_t* row,
     wait_st();
 }
 
-// ---- LSE, MEAN, R
-constexpr int kBlocks = 3, kRows = 128 * kBlocks;
-constexpr int kReadWarps = 4 * kBlocks, kIssueWarp = kReadWarps, kLoadWarp = kIssueWarp + kBlocks;
-constexpr int kSweepThreads = (kLoadWarp + 1) * 32;
-constexpr int kStages = 6;
-
+// ---- LSE, MEAN, R: the passes
 template <int DIN>
 struct Sweep {
     static constexpr int AN = DIN == 128 ? 96 : 64;    // columns of an accumulator
@@ -501,6 +641,16 @@ __global__ void __launch_bounds__(kSweepThreads, 1) sweep_kernel(const __grid_co
         if (MODE == SWEEP_LSE) reinterpret_cast<float2*>(a.part)[at] = make_float2(*abort_flag ? CUDART_INF_F : top, r);
         else a.part[at] = r;
     }
+    if (!a.join_here || !last_of(a.ticket + (int64_t)grp * (gridDim.x / (uint32_t)a.splits) + blockIdx.x / (uint32_t)a.splits, (unsigned)a.splits)) return;
+    join<MODE>(a, grp, row0);
+}
+
+// The same in a launch of its own.
+template <int MODE>
+__global__ void __launch_bounds__(kSweepThreads) join_kernel(const SweepArgs a)
+{
+    grid_dependency_wait();
+    join<MODE>(a, (int)blockIdx.y, (int64_t)blockIdx.x * kSweepPad);
 }
 
 // ---- DX, DW
@@ -525,7 +675,7 @@ struct Grad {
 };
 
 template <int DIN, int MODE>
-__global__ void __launch_bounds__(Grad<DIN>::THREADS, 1) grad_kernel(const __grid_constant__ CUtensorMap map, const SweepArgs a)
+__device__ __forceinline__ void grad_block(const CUtensorMap& map, const SweepArgs& a, const int splits, const uint32_t block, const int of_group, float* const part)
 {
     using L = Grad<DIN>;
     constexpr int TN = L::TN;
@@ -536,16 +686,16 @@ __global__ void __launch_bounds__(Grad<DIN>::THREADS, 1) grad_kernel(const __gri
     const uint32_t sb = smem_u32(sm);
     auto bar = [&](int i) { return sb + L::OFF_BAR + 8u * (uint32_t)i; };
     volatile int* abort_flag = reinterpret_cast<volatile int*>(sm + L::OFF_ABORT);
-    const int split = (int)(blockIdx.x % (uint32_t)a.splits);
+    const int split = (int)(block % (uint32_t)splits);
     const int64_t n_stand = kEntriesStand ? a.m : a.n, n_stream = kEntriesStand ? a.n : a.m;
-    const int64_t row0 = (int64_t)(blockIdx.x / (uint32_t)a.splits) * (128 * L::BLOCKS);
+    const int64_t row0 = (int64_t)(block / (uint32_t)splits) * (128 * L::BLOCKS);
     const int n_blocks = (int)min((n_stand - row0 + 127) / 128, (int64_t)L::BLOCKS);
     // tiles of one group after the other (DW: the block's group alone)
     const int per_group = (int)((n_stream + TN - 1) / TN);
     const int64_t all_tiles = (int64_t)per_group * (kEntriesStand ? 1 : a.G);
-    const int64_t tile0 = all_tiles * split / a.splits;
-    const int n_tiles = (int)(all_tiles * (split + 1) / a.splits - tile0);
-    const int first_group = kEntriesStand ? (int)blockIdx.y : (int)(tile0 / max(per_group, 1)), first_tile = (int)(tile0 - (kEntriesStand ? 0 : (int64_t)first_group * per_group));
+    const int64_t tile0 = all_tiles * split / splits;
+    const int n_tiles = (int)(all_tiles * (split + 1) / splits - tile0);
+    const int first_group = kEntriesStand ? of_group : (int)(tile0 / max(per_group, 1)), first_tile = (int)(tile0 - (kEntriesStand ? 0 : (int64_t)first_group * per_group));
 
     const int e = warp >> 3, buf = (warp >> 2) & 1;
     const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
@@ -573,7 +723,7 @@ __global__ void __launch_bounds__(Grad<DIN>::THREADS, 1) grad_kernel(const __gri
     const uint32_t tmem = tmem_slot, tblock = tmem + (uint32_t)e * L::COL_BLOCK;
     if (warp < 4) store_ones(tmem + lane_base + L::COL_ONES);
     if (warp < 8 * n_blocks && buf == 0)
-        load_inputs<DIN>(tblock + lane_base + L::COL_A, (kEntriesStand ? a.W + ((int64_t)blockIdx.y * a.m + row) * DIN : a.x + row * DIN), in);
+        load_inputs<DIN>(tblock + lane_base + L::COL_A, (kEntriesStand ? a.W + ((int64_t)of_group * a.m + row) * DIN : a.x + row * DIN), in);
     if (warp < L::LOAD_WARP) {  // (the loading warp is on its way)
         tc_before();
         asm volatile("bar.sync 1, %0;" ::"n"(L::LOAD_WARP * 32) : "memory");
@@ -716,7 +866,7 @@ __global__ void __launch_bounds__(Grad<DIN>::THREADS, 1) grad_kernel(const __gri
     tc_after();
     if (warp < 8 * n_blocks && buf == 0) {
         const bool bad = *abort_flag != 0;
-        float* out = kEntriesStand ? a.part + (((int64_t)split * a.G + blockIdx.y) * a.m + row) * DIN : a.part + ((int64_t)split * a.n + row) * DIN;
+        float* out = kEntriesStand ? part + (((int64_t)split * a.G + of_group) * a.m + row) * DIN : part + ((int64_t)split * a.n + row) * DIN;
 #pragma unroll
         for (int c = 0; c < DIN / 32; ++c) {
             uint32_t v[32];
@@ -731,13 +881,23 @@ __global__ void __launch_bounds__(Grad<DIN>::THREADS, 1) grad_kernel(const __gri
                 reinterpret_cast<float4*>(out)[8 * c + q] = o;
             }
         }
-        if (kEntriesStand && in) a.part2[((int64_t)split * a.G + blockIdx.y) * a.mp + row] = bad ? CUDART_NAN_F : sum.s + half[at_row];
+        if (kEntriesStand && in) a.part2[((int64_t)split * a.G + of_group) * a.mp + row] = bad ? CUDART_NAN_F : sum.s + half[at_row];
     }
     tc_before();
     __syncthreads();
     tc_after();
     if (warp == L::ISSUE_WARP)
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+}
+
+// The blocks of DX, then those of DW, which want nothing of one another.
+template <int DIN>
+__global__ void __launch_bounds__(Grad<DIN>::THREADS, 1)
+    grad_kernel(const __grid_constant__ CUtensorMap map_W, const __grid_constant__ CUtensorMap map_x, const SweepArgs a, const int dx_blocks, const int dw_blocks)
+{
+    const uint32_t b = blockIdx.x;
+    if (b < (uint32_t)dx_blocks) grad_block<DIN, SWEEP_DX>(map_W, a, a.splits, b, 0, a.part);
+    else grad_block<DIN, SWEEP_DW>(map_x, a, a.splits_dw, (b - dx_blocks) % (uint32_t)dw_blocks, (int)((b - dx_blocks) / (uint32_t)dw_blocks), a.part_dw);
 }
 
 struct Shape {
@@ -750,17 +910,34 @@ Shape shape_of(int d, int mode)
     return Shape{kRows, d == 128 ? 96 : 128, 4, 0.25};
 }
 
+bool entries_stand(int mode) { return mode == SWEEP_MEAN || mode == SWEEP_DW; }
+// Blocks of standing rows, of all groups.
+int64_t blocks_of(int64_t n, int G, int d, int64_t m, int mode)
+{
+    const int rows = shape_of(d, mode).rows;
+    return ((entries_stand(mode) ? m : n) + rows - 1) / rows * (mode == SWEEP_DX ? 1 : G);
+}
+bool map_of(CUtensorMap* map, const void* rows, int64_t n, int G, int d, int tile)
+{
+    return encode_groups(map, rows, d, n, G, d < 64 ? d : 64, tile, d < 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
+                         CU_TENSOR_MAP_L2_PROMOTION_L2_128B);
+}
+
 template <int DIN>
-cudaError_t launch_t(int mode, const SweepArgs& a, const CUtensorMap& map, dim3 grid, cudaStream_t s)
+cudaError_t launch_sweep_t(int mode, const SweepArgs& a, const CUtensorMap& map, dim3 grid, cudaStream_t s)
 {
     const Launch l{s, nullptr, nullptr, true};
     switch (mode) {
         case SWEEP_LSE: return launch_kernel(l, sweep_kernel<DIN, SWEEP_LSE>, grid, kSweepThreads, Sweep<DIN>::SMEM, 1, map, a);
         case SWEEP_MEAN: return launch_kernel(l, sweep_kernel<DIN, SWEEP_MEAN>, grid, kSweepThreads, Sweep<DIN>::SMEM, 1, map, a);
-        case SWEEP_R: return launch_kernel(l, sweep_kernel<DIN, SWEEP_R>, grid, kSweepThreads, Sweep<DIN>::SMEM, 1, map, a);
-        case SWEEP_DX: return launch_kernel(l, grad_kernel<DIN, SWEEP_DX>, grid, Grad<DIN>::THREADS, Grad<DIN>::SMEM, 1, map, a);
-        default: return launch_kernel(l, grad_kernel<DIN, SWEEP_DW>, grid, Grad<DIN>::THREADS, Grad<DIN>::SMEM, 1, map, a);
+        default: return launch_kernel(l, sweep_kernel<DIN, SWEEP_R>, grid, kSweepThreads, Sweep<DIN>::SMEM, 1, map, a);
     }
+}
+template <int DIN>
+cudaError_t launch_grad_t(const SweepArgs& a, const CUtensorMap& map_W, const CUtensorMap& map_x, int64_t dx, int64_t dw, cudaStream_t s)
+{
+    return launch_kernel(Launch{s, nullptr, nullptr, true}, grad_kernel<DIN>, dim3((unsigned)(dx + dw * a.G)), Grad<DIN>::THREADS, Grad<DIN>::SMEM, 1, map_W, map_x, a,
+                         (int)dx, (int)dw);
 }
 
 }  // namespace
@@ -769,10 +946,8 @@ cudaError_t launch_t(int mode, const SweepArgs& a, const CUtensorMap& map, dim3 
 int sweep_splits(int64_t n, int G, int d, int64_t m, int mode)
 {
     const Shape sh = shape_of(d, mode);
-    const bool entries = mode == SWEEP_MEAN || mode == SWEEP_DW;
-    const int64_t groups = mode == SWEEP_DX ? G : 1;
-    const int64_t blocks = ((entries ? m : n) + sh.rows - 1) / sh.rows * (mode == SWEEP_DX ? 1 : G);
-    const int64_t tiles = ((entries ? n : m) + sh.tile - 1) / sh.tile * groups;
+    const int64_t blocks = blocks_of(n, G, d, m, mode);
+    const int64_t tiles = ((entries_stand(mode) ? n : m) + sh.tile - 1) / sh.tile * (mode == SWEEP_DX ? G : 1);
     int best = 1;
     double best_cost = 1e300;
     for (int sp = 1; sp <= kSweepMaxSplits && sp <= std::max<int64_t>(tiles, 1); ++sp) {
@@ -786,25 +961,34 @@ int sweep_splits(int64_t n, int G, int d, int64_t m, int mode)
     return best;
 }
 
+int64_t sweep_tickets(int64_t n, int G, int d, int64_t m, int mode) { return blocks_of(n, G, d, m, mode) + (mode == SWEEP_MEAN ? G : 0); }
+
 cudaError_t launch_sweep(int mode, int d, SweepArgs& a, cudaStream_t s)
 {
-    const Shape sh = shape_of(d, mode);
-    const bool entries = mode == SWEEP_MEAN || mode == SWEEP_DW;
+    const bool entries = entries_stand(mode);
+    const int64_t blocks = blocks_of(a.n, a.G, d, a.m, mode);
+    if (blocks == 0) return cudaSuccess;
     a.splits = sweep_splits(a.n, a.G, d, a.m, mode);
-    const int64_t stand = entries ? a.m : a.n;
-    if (stand == 0) return cudaSuccess;
+    a.join_here = blocks * a.splits <= 148;
     CUtensorMap map;
-    const CUtensorMapSwizzle swizzle = d < 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B;
-    // (without positions nothing streams, and the map is not used)
-    if (!encode_groups(&map, entries && a.n > 0 ? (const void*)a.x : a.W, d, entries && a.n > 0 ? a.n : a.m, entries && a.n > 0 ? 1 : a.G, d < 64 ? d : 64,
-                       sh.tile, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_128B))
-        return cudaErrorInvalidValue;
-    const dim3 grid((unsigned)((stand + sh.rows - 1) / sh.rows * a.splits), mode == SWEEP_DX ? 1u : (unsigned)a.G);
-    switch (d) {
-        case 32: return launch_t<32>(mode, a, map, grid, s);
-        case 64: return launch_t<64>(mode, a, map, grid, s);
-        default: return launch_t<128>(mode, a, map, grid, s);
-    }
+    const bool x_streams = entries && a.n > 0;  // (without positions nothing streams, and the map is not used)
+    if (!map_of(&map, x_streams ? a.x : a.W, x_streams ? a.n : a.m, x_streams ? 1 : a.G, d, shape_of(d, mode).tile)) return cudaErrorInvalidValue;
+    const dim3 grid((unsigned)(blocks / a.G * a.splits), (unsigned)a.G);
+    cudaError_t e = d == 32 ? launch_sweep_t<32>(mode, a, map, grid, s) : d == 64 ? launch_sweep_t<64>(mode, a, map, grid, s) : launch_sweep_t<128>(mode, a, map, grid, s);
+    if (e != cudaSuccess || a.join_here) return e;
+    return launch_kernel(Launch{s, nullptr, nullptr, true}, mode == SWEEP_LSE ? join_kernel<SWEEP_LSE> : mode == SWEEP_MEAN ? join_kernel<SWEEP_MEAN> : join_kernel<SWEEP_R>,
+                         dim3((unsigned)(blocks / a.G), (unsigned)a.G), kSweepThreads, 0, 1, a);
+}
+
+cudaError_t launch_sweep_grad(int d, SweepArgs& a, cudaStream_t s)
+{
+    a.splits = sweep_splits(a.n, a.G, d, a.m, SWEEP_DX);
+    a.splits_dw = sweep_splits(a.n, a.G, d, a.m, SWEEP_DW);
+    const int64_t dx = blocks_of(a.n, a.G, d, a.m, SWEEP_DX) * a.splits, dw = blocks_of(a.n, a.G, d, a.m, SWEEP_DW) / a.G * a.splits_dw;
+    CUtensorMap map_W, map_x;
+    const int tile = shape_of(d, SWEEP_DX).tile;
+    if (!map_of(&map_W, a.W, a.m, a.G, d, tile) || !map_of(&map_x, a.n ? a.x : a.W, a.n ? a.n : a.m, 1, d, tile)) return cudaErrorInvalidValue;
+    return d == 32 ? launch_grad_t<32>(a, map_W, map_x, dx, dw, s) : d == 64 ? launch_grad_t<64>(a, map_W, map_x, dx, dw, s) : launch_grad_t<128>(a, map_W, map_x, dx, dw, s);
 }
 
 }  // namespace ckv

@@ -32,7 +32,7 @@ struct Pass {
 };
 __device__ __forceinline__ int digit_of(uint32_t key, int shift) { return (int)((key >> shift) & (uint32_t)((1 << kDigitBits) - 1)); }
 
-__global__ void __launch_bounds__(256) count_kernel(const Pass p, int32_t* __restrict__ table)
+__global__ void __launch_bounds__(256) count_kernel(const Pass p, int32_t* table)
 {
     extern __shared__ int32_t bins[];
     const int g = blockIdx.y;
@@ -44,7 +44,7 @@ __global__ void __launch_bounds__(256) count_kernel(const Pass p, int32_t* __res
 #pragma unroll 8
     for (int64_t i = begin + threadIdx.x; i < end; i += 256) {
         uint32_t k;
-        if (p.idx) keys[i] = k = key_of(__ldg(p.idx + i * p.G + g), p.m);
+        if (p.idx) keys[i] = k = key_of(ld(p.idx + i * p.G + g), p.m);
         else k = keys[i];
         atomicAdd(bins + digit_of(k, p.shift), 1);
     }
@@ -55,7 +55,7 @@ __global__ void __launch_bounds__(256) count_kernel(const Pass p, int32_t* __res
 
 // table[g][c][j] becomes the count of the chunks before c, total[g][j] that of all
 constexpr int kScanAhead = 16;
-__global__ void __launch_bounds__(128) chunk_scan_kernel(int32_t* __restrict__ table, int32_t* __restrict__ total, int chunks, int stride)
+__global__ void __launch_bounds__(128) chunk_scan_kernel(int32_t* table, int32_t* total, int chunks, int stride)
 {
     const int j = blockIdx.x * 128 + threadIdx.x, g = blockIdx.y;
     grid_dependency_wait();
@@ -102,7 +102,7 @@ __device__ __forceinline__ int32_t block_prefix(int32_t v, int32_t* all)
 }
 
 // exclusive prefix sums of a group's totals, in place; copied to offset (rows of `bins`) if given
-__global__ void __launch_bounds__(1024) bin_scan_kernel(int32_t* __restrict__ total, int32_t* __restrict__ offset, int bins, int stride)
+__global__ void __launch_bounds__(1024) bin_scan_kernel(int32_t* total, int32_t* offset, int bins, int stride)
 {
     const int g = blockIdx.x;
     int32_t* t = total + (int64_t)g * stride;
@@ -141,7 +141,7 @@ __device__ __forceinline__ int32_t take_places(volatile int32_t* next, int d, un
 // A chunk's positions to their places, by one warp (the block's others help to fetch next[]).  Bound by the instructions of its turns.
 // (Eight warps with a part of a larger chunk each, which count their parts first: 121 us instead of 81 for 1048576 x 8
 // positions; votes on the 13 bits of a key instead of the match 113.)
-__global__ void __launch_bounds__(128) place_kernel(const Pass p, const int32_t* __restrict__ table, const int32_t* __restrict__ base)
+__global__ void __launch_bounds__(128) place_kernel(const Pass p, const int32_t* table, const int32_t* base)
 {
     extern __shared__ __align__(16) int32_t next[];
     const int g = blockIdx.y, lane = threadIdx.x & 31;
@@ -149,7 +149,7 @@ __global__ void __launch_bounds__(128) place_kernel(const Pass p, const int32_t*
     const int32_t *t = table + ((int64_t)g * p.chunks + blockIdx.x) * p.stride, *b = base + (int64_t)g * p.stride;
 #pragma unroll 4
     for (int j = threadIdx.x * 4; j < p.stride; j += 512) {
-        const int4 x = __ldg(reinterpret_cast<const int4*>(t + j)), y = __ldg(reinterpret_cast<const int4*>(b + j));
+        const int4 x = ld(reinterpret_cast<const int4*>(t + j)), y = ld(reinterpret_cast<const int4*>(b + j));
         *reinterpret_cast<int4*>(next + j) = make_int4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
     }
     __syncthreads();
@@ -161,8 +161,8 @@ __global__ void __launch_bounds__(128) place_kernel(const Pass p, const int32_t*
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
             const int64_t i = i0 + 32 * k + lane;
-            key[k] = i < end ? __ldg(p.key + row + i) : 0xffffffffu;
-            val[k] = !p.val ? (int32_t)i : i < end ? __ldg(p.val + row + i) : 0;
+            key[k] = i < end ? ld(p.key + row + i) : 0xffffffffu;
+            val[k] = !p.val ? (int32_t)i : i < end ? ld(p.val + row + i) : 0;
         }
     };
     fetch(begin);
@@ -193,8 +193,8 @@ __global__ void __launch_bounds__(128) place_kernel(const Pass p, const int32_t*
 }
 
 // The whole sort of a group by one block.
-__global__ void __launch_bounds__(kBlockThreads) block_sort_kernel(int n, int G, int64_t m, const int32_t* __restrict__ idx,
-                                                                   int32_t* __restrict__ order, int32_t* __restrict__ offset)
+__global__ void __launch_bounds__(kBlockThreads) block_sort_kernel(int n, int G, int64_t m, const int32_t* idx,
+                                                                   int32_t* order, int32_t* offset)
 {
     extern __shared__ __align__(16) int32_t next[];
     const int g = blockIdx.x, tid = threadIdx.x, lane = tid & 31, bins = (int)m + 1;
@@ -204,7 +204,7 @@ __global__ void __launch_bounds__(kBlockThreads) block_sort_kernel(int n, int G,
     __syncthreads();
 #pragma unroll 4
     for (int i = tid; i < n; i += kBlockThreads) {
-        const int k = (int)key_of(__ldg(idx + (int64_t)i * G + g), m);
+        const int k = (int)key_of(ld(idx + (int64_t)i * G + g), m);
         keys[i] = (uint16_t)k;
         atomicAdd(next + k, 1);
     }
@@ -232,7 +232,7 @@ __global__ void __launch_bounds__(kBlockThreads) block_sort_kernel(int n, int G,
 }
 
 // offset[g][j] = number of sorted keys below j
-__global__ void __launch_bounds__(256) bounds_kernel(const uint32_t* __restrict__ key, int32_t* __restrict__ offset, int64_t n, int64_t m)
+__global__ void __launch_bounds__(256) bounds_kernel(const uint32_t* key, int32_t* offset, int64_t n, int64_t m)
 {
     const int64_t j = blockIdx.x * (int64_t)256 + threadIdx.x;
     grid_dependency_wait();
