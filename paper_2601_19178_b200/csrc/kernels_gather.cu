@@ -199,6 +199,146 @@ __device__ __forceinline__ void share_out(float (&dot)[AHEAD], int sub)
     }
 }
 
+// A run of rows added up by a warp.  GATED: pool is given, so that the weight is a sigmoid and d_score is wanted.
+template <typename E, int LANES, bool GATED>
+struct Run {
+    static constexpr int N = 16 / (int)sizeof(E), SIDE = 32 / LANES, AHEAD = LANES < 8 ? LANES : 8;  // elements of a lane, rows side by side, rows of a lane
+    static constexpr int ROWS = AHEAD * SIDE, WIDTH = LANES * N;
+    const SegmentArgs& a;
+    const int g, lane = threadIdx.x & 31, sub = lane % LANES, side = lane / LANES, col0 = sub * N;
+    const int32_t* const order;
+    const E* const rows;
+    const int user_bytes;  // of a row's part, if one store takes it
+    float acc[N], own[N], wsum;
+
+    __device__ __forceinline__ Run(const SegmentArgs& args, int group)
+        : a(args), g(group), order(args.order + (int64_t)group * args.n), rows((const E*)args.rows + group * args.group_stride + col0),
+          user_bytes(args.skip <= N && ((uintptr_t)args.d_user & (args.skip * sizeof(E) - 1)) == 0 ? args.skip * (int)sizeof(E) : 0)
+    {
+    }
+    __device__ __forceinline__ int32_t position(int64_t t, int64_t to) const
+    {
+        const int32_t p = lane < ROWS && t + lane < to ? ld(order + t + lane) : -1;
+        return p < a.n ? p : -1;  // (not an order)
+    }
+    // Adds positions [from, to) of entry j (m: no entry; their user parts are copied, and their d_score is zero).
+    __device__ __forceinline__ void add(int64_t from, int64_t to, int64_t j)
+    {
+#pragma unroll
+        for (int q = 0; q < N; ++q) acc[q] = 0.f;
+        wsum = 0.f;
+        int32_t next = position(from, to);
+        if (GATED) {
+            const E* p = (const E*)a.pool + ((int64_t)g * a.m + j) * (WIDTH - a.skip) + col0 - a.skip;
+#pragma unroll
+            for (int q = 0; q < N; ++q) own[q] = j < a.m && col0 + q >= a.skip ? widen(ld(p + q)) : 0.f;
+        }
+        for (int64_t t = from; t < to; t += ROWS) {
+            const int32_t pos = next;
+            const int n_rows = (int)min(to - t, (int64_t)ROWS);
+            const float sc = pos >= 0 && a.score ? ld(a.score + (int64_t)pos * a.G + g) : 0.f;
+            uint4 raw[AHEAD];
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                if (k * SIDE >= n_rows) break;
+                const int32_t p = __shfl_sync(0xffffffffu, pos, k * SIDE + side);
+                raw[k] = p >= 0 ? __ldcs(reinterpret_cast<const uint4*>(rows + p * a.stride)) : make_uint4(0, 0, 0, 0);  // (read once)
+            }
+            next = position(t + ROWS, to);
+            const float2 gate = pos < 0 ? make_float2(0.f, 0.f) : !a.score ? make_float2(1.f, 0.f) : GATED ? sigmoids(sc) : make_float2(sc, 0.f);
+            float dot[AHEAD] = {};
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                if (k * SIDE >= n_rows) break;
+                const float w = __shfl_sync(0xffffffffu, gate.x, k * SIDE + side);
+                const E* v = reinterpret_cast<const E*>(&raw[k]);
+#pragma unroll
+                for (int q = 0; q < N; ++q) {
+                    const float x = widen(v[q]);
+                    acc[q] = fmaf(w, x, acc[q]);
+                    if (GATED) dot[k] = fmaf(own[q], x, dot[k]);
+                }
+                if (a.d_user) {
+                    const int32_t p = __shfl_sync(0xffffffffu, pos, k * SIDE + side);
+                    if (p >= 0 && col0 < a.skip) {
+                        E* to_user = (E*)a.d_user + ((int64_t)p * a.G + g) * a.skip + col0;
+                        if (user_bytes == 2) *reinterpret_cast<uint16_t*>(to_user) = (uint16_t)raw[k].x;
+                        else if (user_bytes == 4) *reinterpret_cast<uint32_t*>(to_user) = raw[k].x;
+                        else if (user_bytes == 8) *reinterpret_cast<uint2*>(to_user) = make_uint2(raw[k].x, raw[k].y);
+                        else
+#pragma unroll
+                            for (int q = 0; q < N; ++q)
+                                if (col0 + q < a.skip) to_user[q] = v[q];
+                    }
+                }
+            }
+            wsum += gate.x;  // a lane's own rows
+            if (GATED && a.d_score) {
+                share_out<LANES, AHEAD>(dot, sub);  // row (sub % AHEAD) SIDE + side
+                const int r = sub % AHEAD * SIDE + side;
+                const int32_t p = __shfl_sync(0xffffffffu, pos, r);
+                const float w = __shfl_sync(0xffffffffu, gate.x, r), less = __shfl_sync(0xffffffffu, gate.y, r);
+                if (p >= 0 && sub < AHEAD) a.d_score[(int64_t)p * a.G + g] = j < a.m ? dot[0] * w * less : 0.f;
+            }
+        }
+    }
+    // The sums of the whole warp, in every lane that holds their columns.
+    __device__ __forceinline__ void finish()
+    {
+#pragma unroll
+        for (int d = LANES; d < 32; d *= 2)
+#pragma unroll
+            for (int q = 0; q < N; ++q) acc[q] += __shfl_xor_sync(0xffffffffu, acc[q], d);
+        if (!GATED && a.weight_sum)
+#pragma unroll
+            for (int d = 1; d < 32; d *= 2) wsum += __shfl_xor_sync(0xffffffffu, wsum, d);
+    }
+    __device__ __forceinline__ void put(int64_t j, int wide) const  // an entry's sums
+    {
+        float* to = a.sum + ((int64_t)g * a.m + j) * (WIDTH - a.skip) + col0 - a.skip;
+        if (side == 0) {
+            if (wide == 4) {
+                if (col0 >= a.skip)
+#pragma unroll
+                    for (int q = 0; q < N; q += 4) *reinterpret_cast<float4*>(to + q) = make_float4(acc[q], acc[q + 1], acc[q + 2], acc[q + 3]);
+            } else if (wide == 2) {
+#pragma unroll
+                for (int q = 0; q < N; q += 2)
+                    if (col0 + q >= a.skip) *reinterpret_cast<float2*>(to + q) = make_float2(acc[q], acc[q + 1]);
+            } else {
+#pragma unroll
+                for (int q = 0; q < N; ++q)
+                    if (col0 + q >= a.skip) to[q] = acc[q];
+            }
+        }
+        if (a.weight_sum && lane == 0) a.weight_sum[(int64_t)g * a.m + j] = wsum;
+    }
+};
+
+// Few positions: a warp to each entry, which loops over its run, and one to every 32 positions without an entry (behind `entry_blocks`).  Next to
+// the kernel for many it saves the search for a chunk's entries, the joins and a launch: 200 positions x 1024 entries x 2 groups 3.2 us
+// and 10 + 6.
+template <typename E, int LANES, bool GATED>
+__global__ void __launch_bounds__(kSegThreads) few_kernel(const SegmentArgs a, int entry_blocks, int wide)
+{
+    const int g = blockIdx.y, warp = threadIdx.x >> 5;
+    const int32_t* offset = a.offset + (int64_t)g * (a.m + 1);
+    Run<E, LANES, GATED> run(a, g);
+    grid_dependency_wait();
+    if ((int)blockIdx.x < entry_blocks) {
+        const int64_t j = (int64_t)blockIdx.x * (kSegThreads / 32) + warp;
+        if (j >= a.m) return;
+        const int64_t from = ld(offset + j), to = ld(offset + j + 1);
+        run.add(from, from >= 0 && to <= a.n ? to : from, j);  // (else these are no offsets)
+        run.finish();
+        run.put(j, wide);
+        return;
+    }
+    const int64_t from = max((int64_t)ld(offset + a.m), (int64_t)0) + ((int64_t)((int)blockIdx.x - entry_blocks) * (kSegThreads / 32) + warp) * 32;
+    run.add(from, min(from + 32, a.n), a.m);
+}
+constexpr int64_t kFewPositions = 512;
+
 // What a chunk leaves for its block.
 struct Ends {
     int32_t head, tail;  // entries of the run that began before the chunk, and of the one that began in it and goes on; -1: none
@@ -526,18 +666,23 @@ struct SegmentSpace {
 template <typename E>
 cudaError_t launch_segments(const SegmentArgs& a, const SegmentSpace& sp, int blocks, int wide, cudaStream_t s)
 {
-    auto go = [&](auto gated, auto plain) {
+    auto go = [&](auto gated, auto plain, auto few_gated, auto few_plain) {
+        if (a.n <= kFewPositions) {
+            const int warps = kSegThreads / 32, entry_blocks = (int)((a.m + warps - 1) / warps), others = a.d_user || a.d_score ? (int)((a.n + 32 * warps - 1) / (32 * warps)) : 0;
+            return launch_kernel(Launch{s, nullptr, nullptr, true}, a.pool ? few_gated : few_plain, dim3((unsigned)(entry_blocks + others), (unsigned)a.G), kSegThreads, 0, 1,
+                                 a, entry_blocks, wide);
+        }
         return launch_kernel(Launch{s, nullptr, nullptr, true}, a.pool ? gated : plain, dim3((unsigned)blocks, (unsigned)a.G), kSegThreads, 0, 1, a, sp.part,
                              sp.wpart, sp.goes_on, chunk_of(a.n, a.G), wide);
     };
     switch (a.width * (int)sizeof(E)) {
         case 32:
-            if constexpr (sizeof(E) == 2) return go(segment_kernel<E, 2, true>, segment_kernel<E, 2, false>);
-        case 64: return go(segment_kernel<E, 4, true>, segment_kernel<E, 4, false>);
-        case 128: return go(segment_kernel<E, 8, true>, segment_kernel<E, 8, false>);
-        case 256: return go(segment_kernel<E, 16, true>, segment_kernel<E, 16, false>);
+            if constexpr (sizeof(E) == 2) return go(segment_kernel<E, 2, true>, segment_kernel<E, 2, false>, few_kernel<E, 2, true>, few_kernel<E, 2, false>);
+        case 64: return go(segment_kernel<E, 4, true>, segment_kernel<E, 4, false>, few_kernel<E, 4, true>, few_kernel<E, 4, false>);
+        case 128: return go(segment_kernel<E, 8, true>, segment_kernel<E, 8, false>, few_kernel<E, 8, true>, few_kernel<E, 8, false>);
+        case 256: return go(segment_kernel<E, 16, true>, segment_kernel<E, 16, false>, few_kernel<E, 16, true>, few_kernel<E, 16, false>);
         default:
-            if constexpr (sizeof(E) == 4) return go(segment_kernel<E, 32, true>, segment_kernel<E, 32, false>);
+            if constexpr (sizeof(E) == 4) return go(segment_kernel<E, 32, true>, segment_kernel<E, 32, false>, few_kernel<E, 32, true>, few_kernel<E, 32, false>);
             return cudaErrorInvalidValue;
     }
 }
@@ -624,7 +769,8 @@ cudaError_t launch_segment_sum(int dtype, const SegmentArgs& a, void* ws, cudaSt
     const int wide = ((uintptr_t)a.sum & 15) == 0 && ds % 4 == 0 && a.skip % (16 / elem) == 0 ? 4
                      : ((uintptr_t)a.sum & 7) == 0 && ds % 2 == 0 && a.skip % 2 == 0 ? 2 : 1;
     cudaError_t e = cudaSuccess;
-    if (blocks > 0) e = dtype == CKV_F32 ? launch_segments<float>(a, sp, blocks, wide, s) : launch_segments<uint16_t>(a, sp, blocks, wide, s);
+    e = dtype == CKV_F32 ? launch_segments<float>(a, sp, blocks, wide, s) : launch_segments<uint16_t>(a, sp, blocks, wide, s);
+    if (a.n <= kFewPositions) return e;
     const int join_blocks = (blocks + kJoinWarps - 1) / kJoinWarps, empty_blocks = (int)((a.m + 32 * kJoinWarps - 1) / (32 * kJoinWarps));
     if (e == cudaSuccess)
         e = launch_kernel(Launch{s, nullptr, nullptr, true}, join_kernel, dim3((unsigned)(join_blocks + empty_blocks), (unsigned)a.G), 32 * kJoinWarps, 0, 1, a,

@@ -8,6 +8,7 @@
 // per chunk then places its positions in their order, so that equal keys keep it and the result does not depend on how
 // blocks are scheduled.  Keys of more than kDigitBits bits are sorted digit by digit, the low ones first.
 #include <algorithm>
+#include <cmath>
 
 #include "fit.h"
 #include "ptx_helpers.cuh"
@@ -15,7 +16,7 @@
 namespace ckv {
 namespace {
 
-constexpr int kDigitBits = 15, kBlockSort = 8192, kBlockThreads = 512;
+constexpr int kDigitBits = 14, kOnePassBins = 25000, kBlockSort = 8192, kBlockThreads = 512;
 constexpr int kAhead = 8;  // batches of 32 positions whose keys a placing warp has on their way
 
 __device__ __forceinline__ uint32_t key_of(int32_t v, int64_t m) { return v >= 0 && v < m ? (uint32_t)v : (uint32_t)m; }
@@ -28,9 +29,9 @@ struct Pass {
     uint32_t* key_out;     // [G][n], or null: nothing reads them any more
     int32_t* val_out;
     int64_t n, m, chunk;
-    int G, chunks, bins, stride, shift;  // stride: of a row of the table, a multiple of four
+    int G, chunks, bins, stride, shift, mask;  // stride: of a row of the table, a multiple of four; mask: of a digit
 };
-__device__ __forceinline__ int digit_of(uint32_t key, int shift) { return (int)((key >> shift) & (uint32_t)((1 << kDigitBits) - 1)); }
+__device__ __forceinline__ int digit_of(uint32_t key, const Pass& p) { return (int)(key >> p.shift) & p.mask & 0x7fff; }
 
 __global__ void __launch_bounds__(256) count_kernel(const Pass p, int32_t* table)
 {
@@ -46,7 +47,7 @@ __global__ void __launch_bounds__(256) count_kernel(const Pass p, int32_t* table
         uint32_t k;
         if (p.idx) keys[i] = k = key_of(ld(p.idx + i * p.G + g), p.m);
         else k = keys[i];
-        atomicAdd(bins + digit_of(k, p.shift), 1);
+        atomicAdd(bins + digit_of(k, p), 1);
     }
     __syncthreads();
     int32_t* t = table + ((int64_t)g * p.chunks + blockIdx.x) * p.stride;
@@ -124,9 +125,6 @@ __global__ void __launch_bounds__(1024) bin_scan_kernel(int32_t* total, int32_t*
 }
 
 // One warp's turn with 32 positions: the place of each, next[] moved on.  Lanes with equal keys (`same`) stay in order.  The warp has
-// next[] to itself: a read, and a write by one lane of each key (with shared-memory additions instead, of which the results
-// were awaited at the end, a turn took 600 clocks).
-// One warp's turn with 32 positions: the place of each, next[] moved on.  Lanes with equal keys (`same`) stay in order.  The warp has
 // next[] to itself: a read, and a write by one lane of each key.
 __device__ __forceinline__ int32_t take_places(volatile int32_t* next, int d, unsigned same)  // d < 0: none
 {
@@ -138,9 +136,11 @@ __device__ __forceinline__ int32_t take_places(volatile int32_t* next, int d, un
     return at + __popc(same & ((1u << lane) - 1));
 }
 
-// A chunk's positions to their places, by one warp (the block's others help to fetch next[]).  Bound by the instructions of its turns.
-// (Eight warps with a part of a larger chunk each, which count their parts first: 121 us instead of 81 for 1048576 x 8
-// positions; votes on the 13 bits of a key instead of the match 113.)
+// A chunk's positions to their places, by one warp (the block's others help to fetch next[]).  Bound by its turns, of which a match
+// instruction is the longest part (its time grows with the number of different keys in the warp; 0.3 us a turn): 1048576 x 8
+// positions, 4096 entries 81 us.  (Lanes that find each other through a word per key, as in block_sort_kernel, halve a turn, but with
+// half as many warps to an SM: 85; eight warps with a part of a larger chunk each, which count their parts first, 121; votes on
+// the 13 bits of a key instead of the match 113.)
 __global__ void __launch_bounds__(128) place_kernel(const Pass p, const int32_t* table, const int32_t* base)
 {
     extern __shared__ __align__(16) int32_t next[];
@@ -178,7 +178,7 @@ __global__ void __launch_bounds__(128) place_kernel(const Pass p, const int32_t*
         fetch(i0 + 32 * kAhead);
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
-            d[k] = i0 + 32 * k + lane < end ? digit_of(k_now[k], p.shift) : -1;
+            d[k] = i0 + 32 * k + lane < end ? digit_of(k_now[k], p) : -1;
             same[k] = __match_any_sync(0xffffffffu, d[k]);
         }
 #pragma unroll
@@ -192,30 +192,54 @@ __global__ void __launch_bounds__(128) place_kernel(const Pass p, const int32_t*
     }
 }
 
-// The whole sort of a group by one block.
+// A key's word pair: the lanes that hold it in the turn at hand, and the place of its next position.
+struct Slot {
+    unsigned lanes;
+    int32_t next;
+};
+// take_places for lanes that find each other through the slots.
+__device__ __forceinline__ int32_t take_places(Slot* slots, int d)  // d < 0: none
+{
+    const int lane = threadIdx.x & 31;
+    if (d >= 0) atomicOr(&slots[d].lanes, 1u << lane);
+    __syncwarp();
+    Slot s{0, 0};
+    if (d >= 0) {
+        const unsigned long long v = *reinterpret_cast<volatile unsigned long long*>(slots + d);
+        s.lanes = (unsigned)v;
+        s.next = (int32_t)(v >> 32);
+    }
+    __syncwarp();
+    if (d >= 0 && lane == __ffs(s.lanes) - 1)
+        *reinterpret_cast<volatile unsigned long long*>(slots + d) = (unsigned long long)(uint32_t)(s.next + __popc(s.lanes)) << 32;
+    __syncwarp();
+    return s.next + __popc(s.lanes & ((1u << lane) - 1));
+}
+
+// The whole sort of a group by one block, of which one warp places: 8000 positions x 8 groups x 300 entries 29 us (55 with a match).
 __global__ void __launch_bounds__(kBlockThreads) block_sort_kernel(int n, int G, int64_t m, const int32_t* idx,
                                                                    int32_t* order, int32_t* offset)
 {
-    extern __shared__ __align__(16) int32_t next[];
+    extern __shared__ __align__(16) Slot slots[];
     const int g = blockIdx.x, tid = threadIdx.x, lane = tid & 31, bins = (int)m + 1;
-    uint16_t* keys = reinterpret_cast<uint16_t*>(next + ((bins + 3) & ~3));
-    for (int j = tid; j < bins; j += kBlockThreads) next[j] = 0;
+    uint16_t* keys = reinterpret_cast<uint16_t*>(slots + ((bins + 3) & ~3));
+    for (int j = tid; j < bins; j += kBlockThreads) slots[j] = Slot{0, 0};
     grid_dependency_wait();
     __syncthreads();
 #pragma unroll 4
     for (int i = tid; i < n; i += kBlockThreads) {
         const int k = (int)key_of(ld(idx + (int64_t)i * G + g), m);
         keys[i] = (uint16_t)k;
-        atomicAdd(next + k, 1);
+        atomicAdd(&slots[k].next, 1);
     }
     __syncthreads();
     int32_t carry = 0;
     for (int j0 = 0; j0 < bins; j0 += kBlockThreads) {
         const int j = j0 + tid;
         int32_t all;
-        const int32_t at = carry + block_prefix<kBlockThreads>(j < bins ? next[j] : 0, &all);
+        const int32_t at = carry + block_prefix<kBlockThreads>(j < bins ? slots[j].next : 0, &all);
         if (j < bins) {
-            next[j] = at;
+            slots[j].next = at;
             offset[(int64_t)g * bins + j] = at;
         }
         carry += all;
@@ -226,7 +250,7 @@ __global__ void __launch_bounds__(kBlockThreads) block_sort_kernel(int n, int G,
     for (int i0 = 0; i0 < n; i0 += 32) {
         const int i = i0 + lane;
         const int d = i < n ? keys[i] : -1;
-        const int32_t at = take_places(next, d, __match_any_sync(0xffffffffu, d));
+        const int32_t at = take_places(slots, d);
         if (i < n) order[(int64_t)g * n + at] = i;
     }
 }
@@ -253,16 +277,28 @@ int bits_of(int64_t m)  // of the largest key, m
     while (m >> b) ++b;
     return b;
 }
-int passes_of(int64_t m) { return (bits_of(m) + kDigitBits - 1) / kDigitBits; }
-int bins_of(int64_t m) { return passes_of(m) == 1 ? (int)m + 1 : 1 << kDigitBits; }
+int passes_of(int64_t m) { return m < kOnePassBins ? 1 : (bits_of(m) + kDigitBits - 1) / kDigitBits; }
+int digit_bits(int64_t m) { return (bits_of(m) + passes_of(m) - 1) / passes_of(m); }
+int bins_of(int64_t m) { return passes_of(m) == 1 ? (int)m + 1 : 1 << digit_bits(m); }
 int stride_of(int64_t m) { return (bins_of(m) + 3) & ~3; }
 bool by_block(int64_t n, int64_t m) { return n <= kBlockSort && passes_of(m) == 1; }
-// Chunks: some 1200 of them in all, but no shorter than half a row of counts, which every chunk writes, adds up and reads.
+// Positions of a chunk, a power of two: the number with the shortest run, in microseconds.  A turn of 32 positions takes a warp 0.3, an SM holds as
+// many chunks as their counts leave room for (at most 16), a chunk's counts are written, read, written and read, at some 1.5 TB/s,
+// and adding up sixteen chunks of a group takes 1.  (1048576 x 8 positions, 4000 entries: 147 us with chunks of 8192, 172 with 4096; 200000
+// x 2, 1000 entries: 24 with 1024, 29 with 512; 50000 x 4, 5000 entries: 24 with 1024, 34 with 4096.)
 int64_t chunk_of(int64_t n, int G, int64_t m)
 {
-    int64_t c = 1024;
-    while (c * 1184 < n * G || 2 * c < bins_of(m)) c *= 2;
-    return c;
+    int64_t best = 512;
+    double best_t = 1e300;
+    for (int64_t c = 512; c <= 32768; c *= 2) {
+        const double chunks = (double)((n + c - 1) / c) * G, room = 148.0 * std::min(16, 220 * 1024 / (stride_of(m) * 4));
+        const double t = std::ceil(chunks / room) * c / 32 * 0.3 + chunks * stride_of(m) * 16 / 1.5e6 + chunks / G / 16;
+        if (t < best_t) {
+            best_t = t;
+            best = c;
+        }
+    }
+    return best;
 }
 
 struct SortSpace {
@@ -294,7 +330,7 @@ cudaError_t launch_sort_indices(int64_t n, int G, int64_t m, const int32_t* idx,
 {
     const Launch l{s, nullptr, nullptr, true};
     if (by_block(n, m))
-        return launch_kernel(l, block_sort_kernel, dim3((unsigned)G), kBlockThreads, stride_of(m) * 4 + (n + 1) / 2 * 4, 1, (int)n, G, m, idx, order, offset);
+        return launch_kernel(l, block_sort_kernel, dim3((unsigned)G), kBlockThreads, stride_of(m) * 8 + (n + 1) / 2 * 4, 1, (int)n, G, m, idx, order, offset);
     const SortSpace sp(ws, n, G, m);
     const int passes = passes_of(m);
     Pass p{};
@@ -305,11 +341,12 @@ cudaError_t launch_sort_indices(int64_t n, int G, int64_t m, const int32_t* idx,
     p.chunks = (int)((n + p.chunk - 1) / p.chunk);
     p.bins = bins_of(m);
     p.stride = stride_of(m);
+    p.mask = passes == 1 ? -1 : (1 << digit_bits(m)) - 1;
     const dim3 grid((unsigned)p.chunks, (unsigned)G);
     // pass i reads keys i & 1 (the first writes them beforehand) and leaves the other ones
     for (int i = 0; i < passes; ++i) {
         const bool last = i + 1 == passes;
-        p.shift = i * kDigitBits;
+        p.shift = i * digit_bits(m);
         p.idx = i == 0 ? idx : nullptr;
         p.key = sp.key[i & 1];
         p.val = i == 0 ? nullptr : sp.val[i & 1];
