@@ -299,7 +299,7 @@ CKV_API ckv_status ckv_project(int32_t device, int32_t n, int32_t n_groups, int3
  * their elements, W and d_out to 16 bytes.  `workspace` is device memory on a 256-byte boundary of at least the size that the _bytes
  * function of the call gives (NULL where that is 0), of any contents; calls that may overlap on the GPU, captured graphs among them, need one each.
  * Errors of all of them: INVALID_ARG (sizes, null, host or misaligned pointers, workspace too small), UNSUPPORTED (d_in,
- * head_dim, more than 65535 groups), SHAPE (d_shared outside [1, head_dim]), CUDA.
+ * head_dim, more than 65535 groups or 2^32 - 2 pool rows), SHAPE (d_shared outside [1, head_dim]), CUDA.
  */
 
 /*

@@ -54,7 +54,8 @@ ckv_status check_gather(int32_t device, int32_t dtype, int32_t n, int32_t n_grou
     if (st != CKV_OK) return st;
     if (dtype != CKV_F32 && dtype != CKV_BF16) return CKV_ERR_INVALID_ARG;
     if (head_dim != 16 && head_dim != 32 && head_dim != 64 && head_dim != 128) return CKV_ERR_UNSUPPORTED;
-    return d_shared < 1 || d_shared > head_dim ? CKV_ERR_SHAPE : CKV_OK;
+    if (d_shared < 1 || d_shared > head_dim) return CKV_ERR_SHAPE;
+    return (int64_t)n_groups * n_entries >= 0xffffffffll ? CKV_ERR_UNSUPPORTED : CKV_OK;  // pool rows are counted in 32 bits
 }
 
 }  // namespace

@@ -60,24 +60,33 @@ __global__ void __launch_bounds__(256) gather_kernel(int64_t rows, int G, int lo
     const int lane = threadIdx.x & 31, bytes = (skip + ds) * (int)sizeof(E);  // skip + ds: a row of `out`
     const int64_t step = (int64_t)gridDim.x * 8 << log_rows;
     grid_dependency_wait();
-    for (int64_t r0 = (blockIdx.x * (int64_t)8 + (threadIdx.x >> 5)) << log_rows; r0 < rows; r0 += step) {
+    constexpr uint32_t kNone = 0xffffffffu;
+    // index and score of the next rows are on their way while rows are copied
+    int32_t idx_next = -1;
+    float score_next = 0.f;
+    auto look_ahead = [&](int64_t r0) {
+        const int64_t r = r0 + lane;
+        const bool there = lane < 1 << log_rows && r < rows;
+        idx_next = there ? ld(idx + r) : -1;
+        if (score) score_next = there ? ld(score + r) : 0.f;
+    };
+    int64_t r0 = (blockIdx.x * (int64_t)8 + (threadIdx.x >> 5)) << log_rows;
+    look_ahead(r0);
+    for (; r0 < rows; r0 += step) {
         const int n_rows = (int)min(rows - r0, (int64_t)1 << log_rows);
-        int64_t from = -1;
-        float gate = 1.f;
-        if (lane < n_rows) {
-            const int32_t j = ld(idx + r0 + lane);
-            if (j >= 0 && j < m) from = ((r0 + lane) % G * m + j) * ds;
-            if (score) gate = sigmoid(ld(score + r0 + lane));
-        }
+        const uint32_t from = idx_next >= 0 && idx_next < m ? (uint32_t)((r0 + lane) % G * m + idx_next) : kNone;  // (no pool has as many rows)
+        const float gate = score ? sigmoid(score_next) : 1.f;
+        look_ahead(r0 + step);
         char* const to = reinterpret_cast<char*>(out) + r0 * bytes;
 #pragma unroll 4
         for (int i = 0; i < 1 << (log_pieces + log_rows - 5); ++i) {
             const int w = 32 * i + lane, k = w >> log_pieces, c = (w - (k << log_pieces)) * N;
-            const int64_t at = __shfl_sync(0xffffffffu, from, k);
+            const uint32_t picked = __shfl_sync(0xffffffffu, from, k);
             const float f = __shfl_sync(0xffffffffu, gate, k);
             if (k >= n_rows) continue;
+            const int64_t at = (int64_t)picked * ds;
             uint32_t v[4] = {};
-            if (at >= 0) {
+            if (picked != kNone) {
                 if (c >= skip) load16<LOAD>(v, pool + at + (c - skip));
                 else {  // a piece with elements of both parts, or of the user's alone
 #pragma unroll
@@ -97,7 +106,8 @@ __global__ void __launch_bounds__(256) gather_kernel(int64_t rows, int G, int lo
                 else if (user_bytes == 8) {
                     const uint2 x = ld(reinterpret_cast<const uint2*>(u));
                     v[0] = x.x, v[1] = x.y;
-                } else if (user_bytes == 2) v[0] = (v[0] & 0xffff0000u) | ld(reinterpret_cast<const uint16_t*>(u));
+                } else if (user_bytes == 16) load16<16>(v, u);  // whole pieces are the user's
+                else if (user_bytes == 2) v[0] = (v[0] & 0xffff0000u) | ld(reinterpret_cast<const uint16_t*>(u));
                 else
 #pragma unroll
                 for (int q = 0; q < N; ++q)
@@ -704,7 +714,7 @@ __global__ void __launch_bounds__(256) widen_pool_kernel(int64_t pieces, int log
 }
 
 // Whether a lookup copies the pool first.  Four loads of a piece's words (eight of its elements) keep the L1 busy for longer than the row
-// takes to store (1048576 x 8 rows of 64 bytes 261 us, WIDE us behind the copy), which pays once there are some rows per entry.
+// takes to store (1048576 x 8 rows of 64 bytes 261 us, 160 behind a copy of 5), which pays once there are some rows per entry.
 bool widens(int64_t n, int D, int ds, int64_t m, int elem) { return n >= 2 * m && (ds * elem % 16 != 0 || (D - ds) * elem % 16 != 0); }
 
 template <typename E>
@@ -725,8 +735,8 @@ cudaError_t launch_gather_t(int64_t n, int G, int D, int ds, int64_t m, const vo
         ds = D;
     }
     auto lies_on = [](const void* p, int step) { return ((uintptr_t)p | (uintptr_t)step) % 16 == 0 ? 16 : ((uintptr_t)p | (uintptr_t)step) % 4 == 0 ? 4 : 2; };
-    // a user part that one load takes
-    const int ub = user_width * e, user_bytes = (ub == 2 || ub == 4 || ub == 8) && (uintptr_t)user % ub == 0 ? ub : 0;
+    // a user part that one load takes, or pieces that one load each takes
+    const int ub = user_width * e % 16 == 0 ? 16 : user_width * e, user_bytes = (ub == 2 || ub == 4 || ub == 8 || ub == 16) && (uintptr_t)user % ub == 0 ? ub : 0;
     const int load = std::min(lies_on(pool, ds * e), lies_on(nullptr, skip * e)), store = lies_on(out, 16);
     while (log_pieces + log_rows > 5 && log_rows > 0 && (n * G >> log_rows) < 148 * 32) --log_rows;
     const int64_t per_block = (int64_t)8 << log_rows, blocks = std::min<int64_t>((n * G + per_block - 1) / per_block, 148 * 8);

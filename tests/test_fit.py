@@ -116,6 +116,7 @@ def test_sizes_are_refused_without_a_gpu():
         assert L.ckv_route_loss(0, 1, 1, d, 1, *[None] * 9, 0, None) == no
     assert L.ckv_gather(0, 1, 1, 1, 48, 30, 4, *[None] * 6, 0, None) == no
     assert L.ckv_gather(0, 2, 1, 1, 32, 30, 4, *[None] * 6, 0, None) == bad
+    assert L.ckv_gather(0, 1, 1, 3, 32, 30, 2 ** 31 - 1, *[None] * 6, 0, None) == no              # more pool rows than 32 bits count
     for ds in (0, 33, -1):
         assert L.ckv_gather(0, 1, 1, 1, 32, ds, 4, *[None] * 6, 0, None) == ckv.CKV_ERR_SHAPE
         assert L.ckv_gather_grad(0, 1, 1, 1, 32, ds, 4, *[None] * 9, 0, None) == ckv.CKV_ERR_SHAPE
@@ -358,7 +359,7 @@ def _gather_case(seed, dtype, n, G, m, D, du, gated, pad=0.2):
 
 GATHERS = [("bf16", 1, 1, 1, 16, 0), ("bf16", 200, 2, 1024, 32, 4), ("f32", 200, 2, 1024, 32, 4), ("bf16", 1000, 3, 77, 64, 1),
            ("bf16", 3001, 1, 5000, 64, 4), ("bf16", 777, 2, 3, 128, 8), ("f32", 999, 4, 50, 16, 3), ("f32", 300, 1, 9, 128, 127),
-           ("bf16", 129, 5, 130, 32, 31), ("bf16", 50, 3, 900, 32, 1), ("bf16", 700, 2, 3000, 128, 2), ("bf16", 65, 8, 64, 128, 0), ("f32", 5000, 1, 1, 64, 2), ("bf16", 40000, 2, 300, 32, 2)]
+           ("bf16", 129, 5, 130, 32, 31), ("bf16", 50, 3, 900, 32, 1), ("f32", 400, 2, 90, 32, 20), ("bf16", 400, 2, 90, 64, 24), ("bf16", 700, 2, 3000, 128, 2), ("bf16", 65, 8, 64, 128, 0), ("f32", 5000, 1, 1, 64, 2), ("bf16", 40000, 2, 300, 32, 2)]
 
 
 @pytest.mark.gpu
