@@ -43,7 +43,7 @@ ckv_status status_of(cudaError_t e)
 {
     if (e == cudaSuccess) return CKV_OK;
     cudaGetLastError();
-    return CKV_ERR_CUDA;
+    return e == kNoRoom ? CKV_ERR_INVALID_ARG : CKV_ERR_CUDA;
 }
 
 bool route_width(int32_t d_in) { return d_in == 32 || d_in == 64 || d_in == 128; }
@@ -59,6 +59,18 @@ ckv_status check_gather(int32_t device, int32_t dtype, int32_t n, int32_t n_grou
 }
 
 }  // namespace
+
+namespace ckv {
+
+SmemGrants* fit_grants()
+{
+    constexpr int kDevices = 16;
+    static thread_local SmemGrants grants[kDevices];
+    int device = -1;
+    return cudaGetDevice(&device) == cudaSuccess && device >= 0 && device < kDevices ? &grants[device] : nullptr;
+}
+
+}  // namespace ckv
 
 extern "C" {
 
@@ -107,10 +119,9 @@ ckv_status ckv_route_loss(int32_t device, int32_t n, int32_t n_groups, int32_t d
     if (!on_device(Arg{x, 2, none}, Arg{W, 16}, Arg{bias, 4, true}, Arg{idx, 4, none}, Arg{loss, 4}, Arg{lse, 4, none},
                    Arg{score, 4, none}, Arg{mean, 4}))
         return CKV_ERR_INVALID_ARG;
-    st = check_workspace(workspace, workspace_bytes, route_loss_workspace(n, n_groups, d_in, n_entries));
-    if (st != CKV_OK) return st;
+    if (!on_device(Arg{workspace, 256})) return CKV_ERR_INVALID_ARG;
     const RouteLossArgs a{n, n_entries, n_groups, d_in, x, W, bias, idx, loss, lse, score, mean};
-    return status_of(launch_route_loss(a, workspace, (cudaStream_t)stream));
+    return status_of(launch_route_loss(a, workspace, workspace_bytes, (cudaStream_t)stream));
 }
 
 ckv_status ckv_route_loss_grad(int32_t device, int32_t n, int32_t n_groups, int32_t d_in, int32_t n_entries, const void* x,
@@ -129,12 +140,11 @@ ckv_status ckv_route_loss_grad(int32_t device, int32_t n, int32_t n_groups, int3
                    Arg{lse, 4, none}, Arg{score, 4, none}, Arg{mean, 4}, Arg{d_score, 4, true}, Arg{dx, 2, none}, Arg{dW, 2},
                    Arg{dbias, 4, true}))
         return CKV_ERR_INVALID_ARG;
-    st = check_workspace(workspace, workspace_bytes, route_grad_workspace(n, n_groups, d_in, n_entries));
-    if (st != CKV_OK) return st;
+    if (!on_device(Arg{workspace, 256})) return CKV_ERR_INVALID_ARG;
     const RouteLossArgs a{n, n_entries, n_groups, d_in, x, W, bias, idx, nullptr, const_cast<float*>(lse), const_cast<float*>(score),
                           const_cast<float*>(mean)};
     const RouteGradArgs b{order, offset, balance_weight, peak_weight, d_score, dx, dW, dbias};
-    return status_of(launch_route_grad(a, b, workspace, (cudaStream_t)stream));
+    return status_of(launch_route_grad(a, b, workspace, workspace_bytes, (cudaStream_t)stream));
 }
 
 ckv_status ckv_gather_bytes(int32_t dtype, int32_t n, int32_t n_groups, int32_t head_dim, int32_t d_shared, int32_t n_entries,

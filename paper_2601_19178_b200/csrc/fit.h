@@ -18,6 +18,23 @@ __device__ __forceinline__ T ld(const T* p)
 }
 #endif
 
+// Kernels of these calls that have been allowed how much shared memory on the current device, as far as this thread knows.
+SmemGrants* fit_grants();
+// launch_kernel with that record.  (A permission is lost with a device that the process resets: then the record starts anew.)
+template <typename... P, typename... A>
+cudaError_t launch_granted(cudaStream_t s, void (*fn)(P...), dim3 grid, int threads, size_t smem, A&&... args)
+{
+    SmemGrants* const g = fit_grants();
+    const int known = g ? g->n : 0;
+    cudaError_t e = launch_kernel(Launch{s, nullptr, g, true}, fn, grid, threads, smem, 1, args...);
+    if (e == cudaErrorInvalidValue && known) {
+        cudaGetLastError();
+        g->n = 0;
+        e = launch_kernel(Launch{s, nullptr, g, true}, fn, grid, threads, smem, 1, args...);
+    }
+    return e;
+}
+
 // Pieces of a caller's workspace, each on a 256-byte boundary.  A null base only adds up the size.
 struct Carve {
     char* base;
@@ -105,8 +122,8 @@ __device__ __forceinline__ void put_step(uint16_t* step, int64_t row, float v)
 }
 #endif
 int sweep_splits(int64_t n, int G, int d, int64_t m, int mode);
-cudaError_t launch_sweep(int mode, int d, SweepArgs& a, cudaStream_t s);  // LSE, MEAN, R, and what joins their partial results
-cudaError_t launch_sweep_grad(int d, SweepArgs& a, cudaStream_t s);       // DX and DW; sets a.splits and a.splits_dw
+cudaError_t launch_sweep(int mode, int d, SweepArgs& a, cudaStream_t s);  // LSE, MEAN, R with a.splits, and what joins their partial results
+cudaError_t launch_sweep_grad(int d, SweepArgs& a, cudaStream_t s);       // DX with a.splits, DW with a.splits_dw
 
 // ---- kernels_route_loss.cu
 struct RouteLossArgs {
@@ -118,7 +135,9 @@ struct RouteLossArgs {
     float *loss, *lse, *score, *mean;  // outputs of the forward pass, inputs of the gradient
 };
 int64_t route_loss_workspace(int64_t n, int G, int d, int64_t m);
-cudaError_t launch_route_loss(const RouteLossArgs& a, void* ws, cudaStream_t s);
+// kNoRoom where the workspace is smaller than that
+constexpr cudaError_t kNoRoom = cudaErrorMemoryAllocation;
+cudaError_t launch_route_loss(const RouteLossArgs& a, void* ws, int64_t bytes, cudaStream_t s);
 struct RouteGradArgs {
     const int32_t *order, *offset;
     float w_balance, w_peak;
@@ -127,6 +146,6 @@ struct RouteGradArgs {
     float* dbias;          // or null
 };
 int64_t route_grad_workspace(int64_t n, int G, int d, int64_t m);
-cudaError_t launch_route_grad(const RouteLossArgs& a, const RouteGradArgs& b, void* ws, cudaStream_t s);
+cudaError_t launch_route_grad(const RouteLossArgs& a, const RouteGradArgs& b, void* ws, int64_t bytes, cudaStream_t s);
 
 }  // namespace ckv

@@ -44,6 +44,7 @@ struct Space {
     void* seg;
     unsigned* ticket[5];     // of the passes LSE, MEAN and R, back to back
     int64_t n_tickets;
+    int splits[5];           // of each pass
     int64_t bytes;
 };
 
@@ -52,6 +53,7 @@ Space layout(void* ws, int64_t n, int G, int d, int64_t m, bool grad)
     Carve c(ws);
     Space s{};
     const int64_t np = sweep_padded(n), mp = sweep_padded(m);
+    for (int mode = grad ? SWEEP_R : SWEEP_LSE; mode <= (grad ? SWEEP_DW : SWEEP_MEAN); ++mode) s.splits[mode] = sweep_splits(n, G, d, m, mode);
     for (int mode = grad ? SWEEP_R : SWEEP_LSE; mode <= (grad ? SWEEP_R : SWEEP_MEAN); ++mode) s.n_tickets += sweep_tickets(n, G, d, m, mode);
     unsigned* ticket = c.take<unsigned>(s.n_tickets);
     for (int mode = grad ? SWEEP_R : SWEEP_LSE; ticket && mode <= (grad ? SWEEP_R : SWEEP_MEAN); ++mode) {
@@ -68,16 +70,16 @@ Space layout(void* ws, int64_t n, int G, int d, int64_t m, bool grad)
         s.live_part = c.take<int32_t>(sweep_blocks(n) * G);
         s.peak_part = c.take<double>(sweep_blocks(n) * G);
         s.balance_part = c.take<double>(sweep_blocks(m) * G);
-        s.part = c.take<float>(std::max(2 * sweep_splits(n, G, d, m, SWEEP_LSE) * G * np, sweep_splits(n, G, d, m, SWEEP_MEAN) * G * mp));
+        s.part = c.take<float>(std::max(2 * (int64_t)s.splits[SWEEP_LSE] * G * np, (int64_t)s.splits[SWEEP_MEAN] * G * mp));
     } else {
         s.h = c.take<float>(G * mp);
         s.nr = c.take<float>(G * np);
         s.ds = c.take<float>(n * G);
         s.sum = c.take<float>(G * m * d);
         s.wsum = c.take<float>(G * m);
-        s.part = c.take<float>(std::max(sweep_splits(n, G, d, m, SWEEP_R) * G * np, sweep_splits(n, G, d, m, SWEEP_DX) * n * d));
-        s.part_dw = c.take<float>(sweep_splits(n, G, d, m, SWEEP_DW) * G * m * d);
-        s.part2 = c.take<float>(sweep_splits(n, G, d, m, SWEEP_DW) * G * mp);
+        s.part = c.take<float>(std::max((int64_t)s.splits[SWEEP_R] * G * np, (int64_t)s.splits[SWEEP_DX] * n * d));
+        s.part_dw = c.take<float>((int64_t)s.splits[SWEEP_DW] * G * m * d);
+        s.part2 = c.take<float>((int64_t)s.splits[SWEEP_DW] * G * mp);
         s.seg = c.take<char>(segment_workspace(n, G, d));
     }
     s.bytes = c.used;
@@ -263,6 +265,7 @@ SweepArgs pass_args(const RouteLossArgs& a, const Space& s)
 cudaError_t pass(int mode, int d, SweepArgs& p, const Space& s, cudaStream_t st)
 {
     p.ticket = s.ticket[mode];
+    p.splits = s.splits[mode];
     return launch_sweep(mode, d, p, st);
 }
 
@@ -277,18 +280,20 @@ int64_t route_grad_workspace(int64_t n, int G, int d, int64_t m) { return layout
         if (e_ != cudaSuccess) return e_;    \
     } while (0)
 
-cudaError_t launch_route_loss(const RouteLossArgs& a, void* ws, cudaStream_t st)
+cudaError_t launch_route_loss(const RouteLossArgs& a, void* ws, int64_t bytes, cudaStream_t st)
 {
     const Space s = layout(ws, a.n, a.G, a.d, a.m, false);
+    if (bytes < s.bytes) return kNoRoom;
     SweepArgs p = pass_args(a, s);
     TRY(launch_prepare<false>(a, RouteGradArgs{}, s, a.n, p.np, p.mp, st));
     TRY(pass(SWEEP_LSE, a.d, p, s, st));
     return pass(SWEEP_MEAN, a.d, p, s, st);
 }
 
-cudaError_t launch_route_grad(const RouteLossArgs& a, const RouteGradArgs& b, void* ws, cudaStream_t st)
+cudaError_t launch_route_grad(const RouteLossArgs& a, const RouteGradArgs& b, void* ws, int64_t bytes, cudaStream_t st)
 {
     const Space s = layout(ws, a.n, a.G, a.d, a.m, true);
+    if (bytes < s.bytes) return kNoRoom;
     SweepArgs p = pass_args(a, s);
     TRY(launch_prepare<true>(a, b, s, a.n ? p.np : 0, p.np, p.mp, st));
     SegmentArgs seg{};
@@ -305,6 +310,8 @@ cudaError_t launch_route_grad(const RouteLossArgs& a, const RouteGradArgs& b, vo
     seg.weight_sum = s.wsum;
     TRY(launch_segment_sum(CKV_BF16, seg, s.seg, st));
     TRY(pass(SWEEP_R, a.d, p, s, st));
+    p.splits = s.splits[SWEEP_DX];
+    p.splits_dw = s.splits[SWEEP_DW];
     TRY(launch_sweep_grad(a.d, p, st));
     const int64_t dx_blocks = (a.n * a.d / 8 + 255) / 256, dw_blocks = (a.G * a.m * a.d / 8 + 255) / 256;
     return launch_kernel(Launch{st, nullptr, nullptr, true}, grad_join_kernel, dim3((unsigned)(dx_blocks + dw_blocks)), 256, 0, 1, a, b, p, (int)dx_blocks);

@@ -927,18 +927,13 @@ bool map_of(CUtensorMap* map, const void* rows, int64_t n, int G, int d, int til
 template <int DIN>
 cudaError_t launch_sweep_t(int mode, const SweepArgs& a, const CUtensorMap& map, dim3 grid, cudaStream_t s)
 {
-    const Launch l{s, nullptr, nullptr, true};
-    switch (mode) {
-        case SWEEP_LSE: return launch_kernel(l, sweep_kernel<DIN, SWEEP_LSE>, grid, kSweepThreads, Sweep<DIN>::SMEM, 1, map, a);
-        case SWEEP_MEAN: return launch_kernel(l, sweep_kernel<DIN, SWEEP_MEAN>, grid, kSweepThreads, Sweep<DIN>::SMEM, 1, map, a);
-        default: return launch_kernel(l, sweep_kernel<DIN, SWEEP_R>, grid, kSweepThreads, Sweep<DIN>::SMEM, 1, map, a);
-    }
+    return launch_granted(s, mode == SWEEP_LSE ? sweep_kernel<DIN, SWEEP_LSE> : mode == SWEEP_MEAN ? sweep_kernel<DIN, SWEEP_MEAN> : sweep_kernel<DIN, SWEEP_R>, grid,
+                          kSweepThreads, Sweep<DIN>::SMEM, map, a);
 }
 template <int DIN>
 cudaError_t launch_grad_t(const SweepArgs& a, const CUtensorMap& map_W, const CUtensorMap& map_x, int64_t dx, int64_t dw, cudaStream_t s)
 {
-    return launch_kernel(Launch{s, nullptr, nullptr, true}, grad_kernel<DIN>, dim3((unsigned)(dx + dw * a.G)), Grad<DIN>::THREADS, Grad<DIN>::SMEM, 1, map_W, map_x, a,
-                         (int)dx, (int)dw);
+    return launch_granted(s, grad_kernel<DIN>, dim3((unsigned)(dx + dw * a.G)), Grad<DIN>::THREADS, Grad<DIN>::SMEM, map_W, map_x, a, (int)dx, (int)dw);
 }
 
 }  // namespace
@@ -951,9 +946,11 @@ int sweep_splits(int64_t n, int G, int d, int64_t m, int mode)
     const int64_t tiles = ((entries_stand(mode) ? n : m) + sh.tile - 1) / sh.tile * (mode == SWEEP_DX ? G : 1);
     int best = 1;
     double best_cost = 1e300;
-    for (int sp = 1; sp <= kSweepMaxSplits && sp <= std::max<int64_t>(tiles, 1); ++sp) {
+    const int most = (int)std::min<int64_t>(kSweepMaxSplits, std::max<int64_t>(tiles, 1));
+    const uint32_t n_tiles = (uint32_t)std::min<int64_t>(tiles, 1 << 30);
+    for (int sp = 1; sp <= most; ++sp) {
         const int64_t rounds = (blocks * sp + 147) / 148;
-        const double cost = rounds * ((double)((tiles + sp - 1) / sp) + sh.start) + sh.join * sp;
+        const double cost = (double)rounds * ((n_tiles + sp - 1) / (uint32_t)sp + sh.start) + sh.join * sp;
         if (cost < best_cost) {
             best_cost = cost;
             best = sp;
@@ -969,7 +966,6 @@ cudaError_t launch_sweep(int mode, int d, SweepArgs& a, cudaStream_t s)
     const bool entries = entries_stand(mode);
     const int64_t blocks = blocks_of(a.n, a.G, d, a.m, mode);
     if (blocks == 0) return cudaSuccess;
-    a.splits = sweep_splits(a.n, a.G, d, a.m, mode);
     a.join_here = blocks * a.splits <= 148;
     CUtensorMap map;
     const bool x_streams = entries && a.n > 0;  // (without positions nothing streams, and the map is not used)
@@ -983,8 +979,6 @@ cudaError_t launch_sweep(int mode, int d, SweepArgs& a, cudaStream_t s)
 
 cudaError_t launch_sweep_grad(int d, SweepArgs& a, cudaStream_t s)
 {
-    a.splits = sweep_splits(a.n, a.G, d, a.m, SWEEP_DX);
-    a.splits_dw = sweep_splits(a.n, a.G, d, a.m, SWEEP_DW);
     const int64_t dx = blocks_of(a.n, a.G, d, a.m, SWEEP_DX) * a.splits, dw = blocks_of(a.n, a.G, d, a.m, SWEEP_DW) / a.G * a.splits_dw;
     CUtensorMap map_W, map_x;
     const int tile = shape_of(d, SWEEP_DX).tile;

@@ -305,11 +305,13 @@ struct SortSpace {
     int32_t *table = nullptr, *total = nullptr, *val[2] = {};
     uint32_t* key[2] = {};
     int64_t bytes = 0;
+    int64_t chunk = 1;
     SortSpace(void* ws, int64_t n, int G, int64_t m)
     {
         if (by_block(n, m)) return;
         Carve c(ws);
-        const int64_t chunks = (n + chunk_of(n, G, m) - 1) / chunk_of(n, G, m);
+        chunk = chunk_of(n, G, m);
+        const int64_t chunks = (n + chunk - 1) / chunk;
         table = c.take<int32_t>(chunks * G * stride_of(m));
         total = c.take<int32_t>((int64_t)G * stride_of(m));
         key[0] = c.take<uint32_t>(n * G);
@@ -330,14 +332,14 @@ cudaError_t launch_sort_indices(int64_t n, int G, int64_t m, const int32_t* idx,
 {
     const Launch l{s, nullptr, nullptr, true};
     if (by_block(n, m))
-        return launch_kernel(l, block_sort_kernel, dim3((unsigned)G), kBlockThreads, stride_of(m) * 8 + (n + 1) / 2 * 4, 1, (int)n, G, m, idx, order, offset);
+        return launch_granted(s, block_sort_kernel, dim3((unsigned)G), kBlockThreads, stride_of(m) * 8 + (n + 1) / 2 * 4, (int)n, G, m, idx, order, offset);
     const SortSpace sp(ws, n, G, m);
     const int passes = passes_of(m);
     Pass p{};
     p.n = n;
     p.m = m;
     p.G = G;
-    p.chunk = chunk_of(n, G, m);
+    p.chunk = sp.chunk;
     p.chunks = (int)((n + p.chunk - 1) / p.chunk);
     p.bins = bins_of(m);
     p.stride = stride_of(m);
@@ -352,12 +354,12 @@ cudaError_t launch_sort_indices(int64_t n, int G, int64_t m, const int32_t* idx,
         p.val = i == 0 ? nullptr : sp.val[i & 1];
         p.key_out = passes == 1 ? nullptr : sp.key[(i + 1) & 1];
         p.val_out = last ? order : sp.val[(i + 1) & 1];
-        cudaError_t e = p.chunks ? launch_kernel(l, count_kernel, grid, 256, p.stride * 4, 1, p, sp.table) : cudaSuccess;
+        cudaError_t e = p.chunks ? launch_granted(s, count_kernel, grid, 256, p.stride * 4, p, sp.table) : cudaSuccess;
         if (e == cudaSuccess)
             e = launch_kernel(l, chunk_scan_kernel, dim3((p.stride + 127) / 128, (unsigned)G), 128, 0, 1, sp.table, sp.total, p.chunks, p.stride);
         if (e == cudaSuccess)
             e = launch_kernel(l, bin_scan_kernel, dim3((unsigned)G), 1024, 0, 1, sp.total, passes == 1 ? offset : nullptr, p.bins, p.stride);
-        if (e == cudaSuccess && p.chunks) e = launch_kernel(l, place_kernel, grid, 128, p.stride * 4, 1, p, sp.table, sp.total);
+        if (e == cudaSuccess && p.chunks) e = launch_granted(s, place_kernel, grid, 128, p.stride * 4, p, sp.table, sp.total);
         if (e != cudaSuccess) return e;
     }
     if (passes > 1)

@@ -78,8 +78,9 @@ def route_loss(x: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor], i
     n, d, G, m = _check_router(x, W, bias, idx, dev)
     nbytes = _loss_bytes(n, G, d, m)[0]
     f32 = torch.float32
-    loss, lse, score, mean = (x.new_empty((G, 2), dtype=f32), x.new_empty((n, G), dtype=f32), x.new_empty((n, G), dtype=f32),
-                              x.new_empty((G, m), dtype=f32))
+    loss, lse = x.new_empty((G, 2), dtype=f32), x.new_empty((n, G), dtype=f32)
+    score = torch.empty_like(lse)  # (less of the host's time than spelling it out)
+    mean = x.new_empty((G, m), dtype=f32) if bias is None else torch.empty_like(bias)
     B.ckv_route_loss(dev, n, G, d, m, x, W, bias, idx, loss, lse, score, mean, x.new_empty(nbytes, dtype=torch.uint8), nbytes, stream)
     return loss, lse, score, mean
 
@@ -100,7 +101,7 @@ def route_loss_grad(x: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tenso
     _check("mean", mean, (G, m), f32, dev)
     _check("d_score", d_score, (n, G), f32, dev)
     nbytes = _loss_bytes(n, G, d, m)[1]
-    dx, dW, dbias = x.new_empty((n, d)), x.new_empty((G, m, d)), x.new_empty((G, m), dtype=f32)
+    dx, dW, dbias = torch.empty_like(x), torch.empty_like(W), torch.empty_like(mean)
     B.ckv_route_loss_grad(dev, n, G, d, m, x, W, bias, idx, order, offset, lse, score, mean, balance_weight, peak_weight, d_score,
                           dx, dW, dbias, x.new_empty(nbytes, dtype=torch.uint8), nbytes, stream)
     return dx, dW, dbias
@@ -149,7 +150,7 @@ def gather_grad(pool: torch.Tensor, ordered: Tuple[torch.Tensor, torch.Tensor], 
     nbytes = _gather_grad_bytes(n, G, D)
     d_pool = pool.new_empty((G, m, ds), dtype=f32)
     d_user = pool.new_empty((n, G, D - ds)) if D > ds else None
-    d_score = None if score is None else pool.new_empty((n, G), dtype=f32)
+    d_score = None if score is None else torch.empty_like(score)
     B.ckv_gather_grad(dev, dt, n, G, D, ds, m, pool, order, offset, score, d_out, d_pool, d_user, d_score,
                       pool.new_empty(nbytes, dtype=torch.uint8), nbytes, stream)
     return d_pool, d_user, d_score
