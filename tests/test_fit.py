@@ -5,6 +5,7 @@ score, whose fp32 sum of d + 1 terms is off by at most (d + 2) 2^-23 S (the tens
 relative error of a softmax weight, is twice that (score and lse) and 2^-19 for the exponential of arguments of some tens.
 """
 import ctypes
+import ctypes as C
 import os
 
 import numpy as np
@@ -132,6 +133,88 @@ def test_wrong_tensors_are_refused_without_a_gpu():
         ckv.route_loss(z(3, 32, dtype=torch.bfloat16), z(1, 4, 32, dtype=torch.bfloat16), None, z(3, 1, dtype=torch.int32))
     with pytest.raises(ValueError, match="CUDA"):
         ckv.gather(z(1, 4, 30), z(3, 1, dtype=torch.int32), None)
+
+
+from test_host_side import device_block, lib, objects, ptr  # noqa: E402,F401  (the library's host side on a stand-in for the CUDA runtime)
+
+
+def _calls(lib):
+    """Every call with arguments that it takes (sizes n = 20, G = 2, m = 30), as (function, arguments): device blocks for the arrays."""
+    d = device_block(lib, 1 << 20)
+    w = C.c_void_p((d.value + 255) // 256 * 256)
+    big = C.c_int64(1 << 19)
+    f = C.c_float
+    return d, w, {
+        "sort": (lib.ckv_sort_indices, [0, 20, 2, 30, d, d, d, w, big, None]),
+        "loss": (lib.ckv_route_loss, [0, 20, 2, 64, 30, d, d, None, d, d, d, d, d, w, big, None]),
+        "grad": (lib.ckv_route_loss_grad, [0, 20, 2, 64, 30, d, d, None, d, d, d, d, d, d, f(1), f(1), None, d, d, None, w, big, None]),
+        "gather": (lib.ckv_gather, [0, 1, 20, 2, 32, 30, 30, d, d, d, None, d, w, big, None]),
+        "gather_grad": (lib.ckv_gather_grad, [0, 1, 20, 2, 32, 30, 30, d, d, d, d, d, d, d, d, w, big, None])}
+
+
+REQUIRED = {"sort": (4, 5, 6), "loss": (5, 6, 8, 9, 10, 11, 12, 13), "grad": (5, 6, 8, 9, 10, 11, 12, 13, 17, 18, 20),
+            "gather": (7, 8, 9, 11), "gather_grad": (7, 8, 9, 11, 12, 14, 15)}
+OPTIONAL = {"loss": (7,), "grad": (7, 16, 19), "gather": (10,), "gather_grad": (13,)}
+
+
+@pytest.mark.parametrize("name", list(REQUIRED))
+def test_pointers_are_refused_without_a_gpu(lib, name):
+    d, w, calls = _calls(lib)
+    fn, args = calls[name]
+    assert fn(*args) == 0
+    host = np.zeros(1 << 20, np.uint8)
+    odd = C.c_void_p(d.value + 1)
+    for at in REQUIRED[name]:
+        for wrong in (None, ptr(host), odd):
+            assert fn(*args[:at], wrong, *args[at + 1:]) == 1, (at, wrong)
+    for at in OPTIONAL.get(name, ()):
+        for wrong in (ptr(host), odd):
+            assert fn(*args[:at], wrong, *args[at + 1:]) == 1, (at, wrong)
+    assert fn(-1, *args[1:]) == 1
+    assert lib.fake_count(b"cudaLaunchKernelExC") >= 1
+
+
+def test_workspaces_are_refused_without_a_gpu(lib):
+    d, w, calls = _calls(lib)
+    v, u = C.c_int64(), C.c_int64()
+    assert lib.ckv_route_loss_bytes(20, 2, 64, 30, C.byref(v), C.byref(u)) == 0
+    need = {"loss": (13, v.value), "grad": (20, u.value)}
+    assert lib.ckv_gather_bytes(1, 70, 2, 32, 30, 30, C.byref(v)) == 0 and v.value > 0
+    calls["gather"][1][2] = 70                                            # (rows enough for a copy of the pool)
+    need["gather"] = (12, v.value)
+    assert lib.ckv_sort_indices_bytes(9000, 2, 30, C.byref(v)) == 0 and v.value > 0
+    calls["sort"][1][1] = 9000
+    need["sort"] = (7, v.value)
+    assert lib.ckv_gather_grad_bytes(20, 2, 32, C.byref(v)) == 0
+    need["gather_grad"] = (15, v.value)
+    for name, (at, size) in need.items():
+        fn, args = calls[name]
+        assert fn(*args[:at], w, C.c_int64(size), *args[at + 2:]) == 0
+        assert fn(*args[:at], w, C.c_int64(size - 1), *args[at + 2:]) == 1, name
+        assert fn(*args[:at], C.c_void_p(w.value + 128), *args[at + 1:]) == 1, name
+
+
+def test_calls_allocate_nothing_and_launch_few_kernels(lib):
+    d, w, calls = _calls(lib)
+    for name, launches in (("sort", 1), ("loss", 3), ("grad", 5), ("gather", 1), ("gather_grad", 1)):
+        fn, args = calls[name]
+        assert fn(*args) == 0
+        lib.fake_reset()
+        assert fn(*args) == 0
+        assert lib.fake_count(b"cudaLaunchKernelExC") == launches, name
+        for other in (b"cudaMalloc", b"cudaMallocHost", b"cudaHostAlloc", b"cudaFree", b"cudaStreamSynchronize", b"cudaMemcpyAsync", b"cudaFuncSetAttribute"):
+            assert lib.fake_count(other) == 0, (name, other)
+
+
+def test_a_launch_that_fails_is_reported(lib):
+    d, w, calls = _calls(lib)
+    for name in calls:
+        fn, args = calls[name]
+        lib.fake_reset()
+        lib.fake_fail(b"cudaLaunchKernelExC", 1)
+        assert fn(*args) != 0, name
+        lib.fake_reset()
+        assert fn(*args) == 0, name
 
 
 # ---- the kernels ------------------------------------------------------------------------------------------------
@@ -452,17 +535,97 @@ def test_gpu_refusals():
 
 
 @pytest.mark.gpu
-def test_gpu_an_order_that_is_none_reads_and_writes_in_bounds():
+@pytest.mark.parametrize("n", [500, 3000])
+def test_gpu_an_order_that_is_none_reads_and_writes_in_bounds(n):
     """order and offset come from ckv_sort_indices; whatever else lies there, the calls stay inside their arrays."""
     import torch
     import paper_2601_19178_b200 as ckv
-    pool, idx, user, score, d_out = [_dev(t) for t in _gather_case(0, "bf16", 500, 2, 40, 32, 2, True)]
+    pool, idx, user, score, d_out = [_dev(t) for t in _gather_case(0, "bf16", n, 2, 40, 32, 2, True)]
+    x, W, b, picked = [_dev(t) for t in _router(2, n, 40, 2, 32)]
+    _, lse, s, mean = ckv.route_loss(x, W, b, picked)
     g = torch.Generator(device="cuda").manual_seed(1)
-    for lo, hi in ((-5, 600), (-2 ** 31, 2 ** 31 - 1)):
-        order = torch.randint(lo, hi, (2, 500), generator=g, device="cuda", dtype=torch.int32)
+    for lo, hi in ((-5, n + 100), (-2 ** 31, 2 ** 31 - 1)):
+        order = torch.randint(lo, hi, (2, n), generator=g, device="cuda", dtype=torch.int32)
         offset = torch.randint(lo, hi, (2, 41), generator=g, device="cuda", dtype=torch.int32)
-        ckv.gather_grad(pool, (order, offset), score, d_out)
+        for o in ((order, offset), (order, torch.sort(offset)[0]), (order, ckv.sort_indices(idx, 40)[1])):
+            ckv.gather_grad(pool, o, score, d_out)
+            ckv.route_loss_grad(x, W, b, picked, o, lse, s, mean, 1.0, 1.0, s)
     torch.cuda.synchronize()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,m", [(512, 7), (513, 7), (9000, 33), (60000, 20000)])
+def test_gpu_a_collapsed_router(n, m):
+    """Nearly all positions pick one entry: its run goes through many blocks; most entries have none."""
+    import paper_2601_19178_b200 as ckv
+    rng = np.random.default_rng(n)
+    idx = np.full((n, 2), m // 2, np.int32)
+    few = rng.random((n, 2)) < 0.02
+    idx[few] = rng.integers(-1, m, int(few.sum()))
+    order, offset = ckv.sort_indices(_dev(idx), m)
+    want_order, want_offset = F.sort_indices(idx, m)
+    assert np.array_equal(order.cpu().numpy(), want_order) and np.array_equal(offset.cpu().numpy(), want_offset)
+    pool, _, _, score, d_out = _gather_case(4, "bf16", n, 2, m, 64, 3, True)
+    d_pool, d_user, d_score = ckv.gather_grad(_dev(pool), (order, offset), _dev(score), _dev(d_out))
+    w_pool, w_user, w_score, a_pool, a_score = F.gather_grad(pool, idx, score, d_out)
+    _close(_host(d_pool), w_pool, (4096 * 2.0 ** -24 + 2.0 ** -20) * a_pool, "d_pool")      # sums of blocks of rows, and of the blocks
+    assert np.array_equal(_host(d_user), w_user)
+    _close(_host(d_score), w_score, (64 * 2.0 ** -24 + 2.0 ** -19) * a_score, "d_score")
+    if n <= 9000:
+        x, W, b, _ = _router(5, n, m, 2, 64)
+        _check_loss(x, W, b, idx, "collapsed")
+        _check_grad(x, W, b, idx, what="collapsed")
+
+
+@pytest.mark.gpu
+def test_gpu_arrays_of_more_than_2_to_the_31_elements():
+    import torch
+    import paper_2601_19178_b200 as ckv
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("needs 40 GB")
+    g = torch.Generator(device="cuda").manual_seed(3)
+    n, G, m, D = 700001, 25, 300, 128                                       # rows of d_out and out: 2.24e9 elements
+    idx = torch.randint(-1, m, (n, G), generator=g, device="cuda", dtype=torch.int32)
+    pool = torch.randn((G, m, D - 2), generator=g, device="cuda").bfloat16()
+    user = torch.randn((n, G, 2), generator=g, device="cuda").bfloat16()
+    out = ckv.gather(pool, idx, user)
+    order = ckv.sort_indices(idx, m)
+    last = slice(n - 5000, n)
+    for k in (0, G - 1):
+        i = idx[last, k].long()
+        want = torch.cat([user[last, k], torch.where((i >= 0)[:, None], pool[k][i.clamp(min=0)], torch.zeros((), dtype=pool.dtype, device="cuda"))], 1)
+        assert torch.equal(out[last, k], want)
+    d_pool, d_user, d_score = ckv.gather_grad(pool, order, None, out)         # (the rows themselves as gradient: sums of equal rows)
+    assert torch.equal(d_user, user) and d_score is None
+    count = (order[1][:, 1:] - order[1][:, :-1]).float()[:, :, None]
+    want = pool.float() * count
+    assert ((d_pool - want).abs() <= 4096 * 2.0 ** -24 * want.abs()).all()
+    del out, user, d_pool, d_user, want
+    n, G, m, d = 70, 33, 1 << 20, 64                                        # W and dW: 2.2e9 elements
+    x = (torch.randn((n, d), generator=g, device="cuda") / 8).bfloat16()
+    W = torch.empty((G, m, d), dtype=torch.bfloat16, device="cuda")
+    for k in range(G):
+        W[k] = torch.randn((m, d), generator=g, device="cuda").bfloat16()
+    idx = torch.randint(0, m, (n, G), generator=g, device="cuda", dtype=torch.int32)
+    order = ckv.sort_indices(idx, m)
+    loss, lse, score, mean = ckv.route_loss(x, W, None, idx)
+    dx, dW, dbias = ckv.route_loss_grad(x, W, None, idx, order, lse, score, mean, 1.0, 1.0)
+    k = G - 1                                                               # the last group, by the definition in 64 bits
+    s = x.double() @ W[k].double().t()
+    p = torch.softmax(s, 1)
+    S = (x.double().abs().max() * W[k].double().abs().sum(1).max()).item()
+    es = (d + 2) * 2.0 ** -23 * S                                            # of a score, and of a weight, see above
+    e = 2 * es + 2.0 ** -19
+    assert ((lse[:, k] - torch.logsumexp(s, 1)).abs() <= es + 2.0 ** -21 * (1 + lse[:, k].abs())).all()
+    assert ((mean[k] - p.mean(0)).abs() <= e * p.mean(0)).all()
+    h = torch.log(mean[k].double() * m) / n
+    t = p * (h - (p @ h)[:, None])
+    t[torch.arange(n, device="cuda"), idx[:, k].long()] -= torch.sigmoid(-score[:, k].double()) / n
+    A = p * (h.abs() + (p @ h.abs())[:, None])
+    half = 2.0 ** -8
+    tol = 2 * e * (A.t() @ x.double().abs()) + (2 * half + 2.0 ** -18) * (t.abs().t() @ x.double().abs()) + 1e-37
+    assert ((dW[k].double() - t.t() @ x.double()).abs() <= tol).all()
+    assert ((dbias[k] - t.sum(0)).abs() <= 2 * e * A.sum(0) + 2.0 ** -18 * t.abs().sum(0)).all()
 
 
 @pytest.mark.gpu
