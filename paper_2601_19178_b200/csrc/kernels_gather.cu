@@ -664,6 +664,12 @@ struct SegmentSpace {
     int64_t bytes;
     SegmentSpace(void* ws, int64_t n, int G, int width, int elem)
     {
+        if (n <= kFewPositions) {
+            part = wpart = nullptr;
+            goes_on = nullptr;
+            bytes = 0;
+            return;
+        }
         Carve c(ws);
         const int64_t block = block_of(n, G, width, elem), blocks = (n + block - 1) / block;
         part = c.take<float>(blocks * G * 2 * width);

@@ -151,6 +151,6 @@ def gather_grad(pool: torch.Tensor, ordered: Tuple[torch.Tensor, torch.Tensor], 
     d_pool = pool.new_empty((G, m, ds), dtype=f32)
     d_user = pool.new_empty((n, G, D - ds)) if D > ds else None
     d_score = None if score is None else torch.empty_like(score)
-    B.ckv_gather_grad(dev, dt, n, G, D, ds, m, pool, order, offset, score, d_out, d_pool, d_user, d_score,
-                      pool.new_empty(nbytes, dtype=torch.uint8), nbytes, stream)
+    ws = pool.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
+    B.ckv_gather_grad(dev, dt, n, G, D, ds, m, pool, order, offset, score, d_out, d_pool, d_user, d_score, ws, nbytes, stream)
     return d_pool, d_user, d_score

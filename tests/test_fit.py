@@ -153,7 +153,7 @@ def _calls(lib):
 
 
 REQUIRED = {"sort": (4, 5, 6), "loss": (5, 6, 8, 9, 10, 11, 12, 13), "grad": (5, 6, 8, 9, 10, 11, 12, 13, 17, 18, 20),
-            "gather": (7, 8, 9, 11), "gather_grad": (7, 8, 9, 11, 12, 14, 15)}
+            "gather": (7, 8, 9, 11), "gather_grad": (7, 8, 9, 11, 12, 14)}
 OPTIONAL = {"loss": (7,), "grad": (7, 16, 19), "gather": (10,), "gather_grad": (13,)}
 
 
@@ -185,7 +185,8 @@ def test_workspaces_are_refused_without_a_gpu(lib):
     assert lib.ckv_sort_indices_bytes(9000, 2, 30, C.byref(v)) == 0 and v.value > 0
     calls["sort"][1][1] = 9000
     need["sort"] = (7, v.value)
-    assert lib.ckv_gather_grad_bytes(20, 2, 32, C.byref(v)) == 0
+    assert lib.ckv_gather_grad_bytes(600, 2, 32, C.byref(v)) == 0 and v.value > 0
+    calls["gather_grad"][1][2] = 600
     need["gather_grad"] = (15, v.value)
     for name, (at, size) in need.items():
         fn, args = calls[name]
