@@ -320,8 +320,9 @@ CKV_API ckv_status ckv_sort_indices(int32_t device, int32_t n, int32_t n_groups,
  *   mean  fp32 [n_groups][n_entries]  p_j = 1 / rows * sum_i softmax(M[i])_j
  *   loss  fp32 [n_groups][2]          load balance sum_j p_j log(p_j / u), peak -1 / rows * sum_i log sigmoid(score_i)
  * x bf16 [n][d_in], W bf16 [n_groups][n_entries][d_in], bias fp32 [n_groups][n_entries] or NULL, d_in in {32, 64, 128}.
- * Products are exact, sums fp32 (the losses' fp64).  A group without rows has zeros.  A bias of -inf takes an entry out;
- * a position whose scores are all -inf adds to no p_j.
+ * Products are exact, sums fp32 (the losses' fp64).  A group without rows has zeros.  A bias of -2^20 or less (-inf, a type's
+ * lowest value) takes an entry out, whose row of W still has to be finite: it counts as -inf, but for `score`, which adds
+ * it as it is.  A position whose entries are all out has lse -inf and adds to no p_j.
  */
 CKV_API ckv_status ckv_route_loss_bytes(int32_t n, int32_t n_groups, int32_t d_in, int32_t n_entries, int64_t* forward,
                                         int64_t* grad);

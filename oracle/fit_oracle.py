@@ -55,6 +55,11 @@ def scores(x, W, bias, g):
     return M if bias is None else M + f64(bias[g])
 
 
+def taken_out(bias, g):
+    """What to add to the scores: -inf for an entry whose bias is -2^20 or less."""
+    return 0.0 if bias is None else np.where(f64(bias[g]) <= -2.0 ** 20, -np.inf, 0.0)
+
+
 def route_loss(x, W, bias, idx):
     n, (G, m, _) = x.shape[0], W.shape
     loss, lse, score, mean = np.zeros((G, 2)), np.zeros((n, G)), np.zeros((n, G)), np.zeros((G, m))
@@ -63,7 +68,7 @@ def route_loss(x, W, bias, idx):
         if len(rows) == 0:
             continue
         M = scores(x[rows], W, bias, g)
-        p, lse[rows, g] = _softmax(M)
+        p, lse[rows, g] = _softmax(M + taken_out(bias, g))
         score[rows, g] = M[np.arange(len(rows)), idx[rows, g]]
         mean[g] = p.mean(0)
         used = mean[g] > 0
@@ -85,10 +90,11 @@ def route_loss_grad(x, W, bias, idx, mean, w_balance, w_peak, d_score=None, lse=
             continue
         X, Wg = f64(x[rows]), f64(W[g])
         M = scores(x[rows], W, bias, g)
-        p, own = _softmax(M)
+        S = M + taken_out(bias, g)
+        p, own = _softmax(S)
         if lse is not None:
             with np.errstate(invalid="ignore"):
-                p = np.where(np.isneginf(M), 0.0, np.exp(M - lse[rows, g][:, None])) if len(rows) else p
+                p = np.where(np.isneginf(S), 0.0, np.exp(S - lse[rows, g][:, None])) if len(rows) else p
         u = mean[g] * m
         h = np.where(u > 0, np.log(np.where(u > 0, u, 1)), 0.0) * w_balance / len(rows)
         r = p @ h

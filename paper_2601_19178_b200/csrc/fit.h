@@ -135,8 +135,8 @@ struct RouteLossArgs {
     float *loss, *lse, *score, *mean;  // outputs of the forward pass, inputs of the gradient
 };
 int64_t route_loss_workspace(int64_t n, int G, int d, int64_t m);
-// kNoRoom where the workspace is smaller than that
-constexpr cudaError_t kNoRoom = cudaErrorMemoryAllocation;
+// kNoRoom (an error that no launch reports) where the workspace is smaller than that
+constexpr cudaError_t kNoRoom = cudaErrorInvalidPitchValue;
 cudaError_t launch_route_loss(const RouteLossArgs& a, void* ws, int64_t bytes, cudaStream_t s);
 struct RouteGradArgs {
     const int32_t *order, *offset;

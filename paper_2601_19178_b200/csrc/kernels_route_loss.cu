@@ -13,8 +13,8 @@
 //   R     positions stand, entries stream:  sum_j p_ij h_j
 //   DX    positions stand, entries of all groups stream:  sum_j T_ij W_j
 //   DW    entries stand, positions stream:  sum_i T_ij x_i, sum_i T_ij
-// and what streams is shared out among `splits` blocks, of which the last one joins their partial results in their order
-// (kernels_route_sweep.cu), but for those of DX and DW.
+// and what streams is shared out among `splits` blocks, whose partial results are joined in the order of those blocks: by the last
+// of them, or in a launch of its own (kernels_route_sweep.cu); those of DX and DW together, in grad_join_kernel.
 #include <cuda_bf16.h>
 #include <math_constants.h>
 
@@ -25,7 +25,6 @@
 
 namespace ckv {
 namespace {
-
 
 __device__ __forceinline__ float sigmoid(float x) { return 1.f / (1.f + expf(-x)); }
 
@@ -86,11 +85,16 @@ Space layout(void* ws, int64_t n, int G, int d, int64_t m, bool grad)
     return s;
 }
 
+// A bias of this or less takes its entry out, as masks by a type's lowest value want it.  The passes' exponents are s log2(e) - c with c
+// rounded once: at scores of 2^20 it is off by a twentieth, as the scores themselves are, at 2^31 by more than an exponential's range.
+constexpr float kTakenOut = -1048576.f;
+
 // ---- what the passes read
 __device__ __forceinline__ void prepare_entry(const RouteLossArgs& a, const RouteGradArgs& b, const Space& s, int64_t mp, int g, int64_t j)
 {
     if (j >= mp) return;
-    const float bias = j < a.m ? (a.bias ? a.bias[g * a.m + j] : 0.f) : -CUDART_INF_F;
+    float bias = j < a.m ? (a.bias ? a.bias[g * a.m + j] : 0.f) : -CUDART_INF_F;
+    if (bias <= kTakenOut) bias = -CUDART_INF_F;
     s.b[g * mp + j] = bias;
     put_step(s.b_step, g * mp + j, bias);
     if (!s.h) return;

@@ -98,7 +98,7 @@ __device__ __forceinline__ uint64_t tile_desc(uint32_t addr)
     constexpr uint64_t layout = ROWB == 128 ? 2 : 4;  // 128-byte / 64-byte swizzle
     return (uint64_t)((addr & 0x3ffffu) >> 4) | (1ull << 16) | ((uint64_t)(ROWB * 8 >> 4) << 32) | (1ull << 46) | (layout << 61);
 }
-// That step's B operand: 16 bf16 per row, in groups of eight rows of 16 bytes, no swizzle (StepLayout of fit.h).
+// That step's B operand: 16 bf16 per row, in groups of eight rows of 16 bytes, no swizzle (put_step of fit.h).
 __device__ __forceinline__ uint64_t step_desc(uint32_t addr)
 {
     return (uint64_t)((addr & 0x3ffffu) >> 4) | ((uint64_t)(128 >> 4) << 16) | ((uint64_t)(256 >> 4) << 32) | (1ull << 46);
@@ -231,16 +231,10 @@ struct Exp2 {
     }
 };
 
-// Pairs of sixteen whose exponentials run on the FMA pipe, spread over them.  32768 positions x 16384 entries x 4 groups, us, with 0, 3, 4, 5 and
-// 6 of them: LSE 589 521 507 509 524, MEAN 572 492 478 460 471, R 582 505 499 502 531, DX 633 599 612 628 634, DW 675 644 646 681 713.
-#ifndef FMA_LSE
-#define FMA_LSE 4
-#define FMA_MEAN 5
-#define FMA_R 4
-#define FMA_DX 3
-#define FMA_DW 3
-#endif
-constexpr int kFmaLse = FMA_LSE, kFmaMean = FMA_MEAN, kFmaR = FMA_R, kFmaDx = FMA_DX, kFmaDw = FMA_DW;
+// Pairs of sixteen whose exponentials run on the FMA pipe, spread over them.  32768 positions x 16384 entries x 4 groups, us, with none: LSE 589,
+// MEAN 572, R 582, DX 633, DW 675; with 3, 4, 5 and 6 of them: LSE 520 514 503 521, MEAN 493 478 468 481, R 547 536 543 541, DX and DW in
+// one launch 1325 1330 1412 1420 (alone, DX 599 612 628 634 and DW 644 646 681 713).
+constexpr int kFmaLse = 5, kFmaMean = 5, kFmaR = 4, kFmaGrad = 3;
 __device__ __forceinline__ constexpr bool on_fma(int q, int of16) { return (q + 1) * of16 / 16 > q * of16 / 16; }
 template <bool DW>
 __device__ __forceinline__ F2 weight(F2 u, bool fma)
@@ -776,8 +770,8 @@ __device__ __forceinline__ void grad_block(const CUtensorMap& map, const SweepAr
                     const F2 u0 = fma2(pair(v, 4 * q), both(kLog2e), both(log_own)), u1 = fma2(pair(v, 4 * q + 2), both(kLog2e), both(log_own));
                     // h_j - r_i, of which one is the thread's own and the other one the column's
                     const F2 d0 = add2({hk.x, hk.y}, both(h_own)), d1 = add2({hk.z, hk.w}, both(h_own));
-                    const F2 w0 = mul2(weight<kEntriesStand>(u0, on_fma(2 * q, kEntriesStand ? kFmaDw : kFmaDx)), d0);
-                    const F2 w1 = mul2(weight<kEntriesStand>(u1, on_fma(2 * q + 1, kEntriesStand ? kFmaDw : kFmaDx)), d1);
+                    const F2 w0 = mul2(weight<kEntriesStand>(u0, on_fma(2 * q, kFmaGrad)), d0);
+                    const F2 w1 = mul2(weight<kEntriesStand>(u1, on_fma(2 * q + 1, kFmaGrad)), d1);
                     if (kEntriesStand) part = add2(part, add2(w0, w1));
                     w[2 * q] = pack_bf16(w0.x, w0.y);
                     w[2 * q + 1] = pack_bf16(w1.x, w1.y);

@@ -354,6 +354,43 @@ def test_gpu_route_loss_of_padding_and_excluded_entries():
     assert np.isneginf(got[1][:, 0]).all() and not got[3][0].any()
 
 
+def test_oracle_takes_entries_out_by_their_bias():
+    x, W, b, idx = _router(8, 30, 20, 2, 32)
+    idx %= 7
+    out, low = b.copy(), b.copy()
+    out[:, 7:], low[:, 7:] = -np.inf, np.finfo(np.float32).min
+    low[1, 9:] = -2.0 ** 20
+    want = F.route_loss(x, W, out, idx)
+    for g, w in zip(F.route_loss(x, W, low, idx), want):
+        assert np.array_equal(g, w)
+    part = F.route_loss(x, W[:, :7], b[:, :7], idx)
+    assert np.allclose(part[1], want[1]) and np.allclose(part[3], want[3][:, :7]) and not want[3][:, 7:].any()
+    grads = [F.route_loss_grad(x, W, v, idx, want[3], 1.0, 0.1)[:3] for v in (out, low)]
+    assert all(np.array_equal(g, w) for g, w in zip(*grads))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("low", [-65504.0, -2.0 ** 20, -1e10, -1e30, float(np.finfo(np.float32).min)])
+@pytest.mark.parametrize("d", [32, 64, 128])
+def test_gpu_router_entries_masked_by_a_large_bias_are_out(d, low):
+    """Whole tiles of masked entries in front of the others, behind them, and all of a group: the bits that -inf gives."""
+    import paper_2601_19178_b200 as ckv
+    n, m, G = 150, 700, 3
+    x, W, b, idx = _router(12, n, m, G, d)
+    idx = (300 + idx % 40).astype(np.int32)
+    results = []
+    for v in (low, -np.inf):
+        b[0, :300] = b[1, 340:] = v
+        if low <= -2.0 ** 20:                          # (-65504 for all entries alike is no mask, but a shift)
+            b[2] = v
+        loss, lse, score, mean = _loss_case(x, W, b, idx)
+        order = ckv.sort_indices(_dev(idx), m)
+        grads = ckv.route_loss_grad(_dev(x), _dev(W), _dev(b), _dev(idx), order, lse, score, mean, 1.0, 0.0)
+        results.append([_host(t) for t in (loss[:, 0], lse, mean, *grads)])
+    for name, g, w in zip(("balance", "lse", "mean", "dx", "dW", "db"), *results):
+        assert not np.isnan(w).any() and np.array_equal(g, w), name
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("d", [32, 128])
 def test_gpu_router_inputs_and_gradients_off_the_16_byte_boundary(d):
