@@ -156,26 +156,25 @@ __device__ __forceinline__ int64_t entry_of(const int32_t* offset, int64_t pos, 
 }
 // The same for two positions, by LANES lanes that look at as many places at a time (all lanes of the warp take part).
 template <int LANES>
-__device__ __forceinline__ void entries_of_group(const int32_t* offset, const int64_t (&pos)[2], int64_t top, int64_t (&lo)[2])
+__device__ __forceinline__ void entries_of_group(const int32_t* offset, const int64_t (&pos)[2], uint32_t top, uint32_t (&lo)[2])
 {
     const int lane = threadIdx.x & 31, sub = lane % LANES;
     const unsigned mine = (LANES == 32 ? 0xffffffffu : (1u << LANES % 32) - 1) << (lane - sub);
-    int64_t hi[2] = {top, top};
+    uint32_t hi[2] = {top, top};
     lo[0] = lo[1] = 0;
     while (__any_sync(0xffffffffu, lo[0] < hi[0] || lo[1] < hi[1])) {
         bool below[2];
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-            const int64_t at = lo[k] + ((hi[k] - lo[k]) * (sub + 1) + LANES) / (LANES + 1);  // lo < at <= hi, rising with sub
-            below[k] = lo[k] < hi[k] && ld(offset + at) <= pos[k];
+            const uint32_t left = hi[k] - lo[k], ahead = (left + LANES - 1) / LANES * (sub + 1);  // (at most 2^31 + 31)
+            below[k] = left && ahead <= left && ld(offset + lo[k] + ahead) <= pos[k];
         }
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-            const int n = __popc(__ballot_sync(0xffffffffu, below[k]) & mine);  // places at or before the entry
-            if (lo[k] >= hi[k]) continue;
-            const int64_t wide = hi[k] - lo[k], from = lo[k];
-            if (n > 0) lo[k] = from + (wide * n + LANES) / (LANES + 1);
-            if (n < LANES) hi[k] = from + (wide * (n + 1) + LANES) / (LANES + 1) - 1;
+            const uint32_t n = __popc(__ballot_sync(0xffffffffu, below[k]) & mine);  // places at or before the entry
+            const uint32_t step = (hi[k] - lo[k] + LANES - 1) / LANES;
+            lo[k] += n * step;
+            hi[k] = min(hi[k], lo[k] + max(step, 1u) - 1);
         }
     }
 }
@@ -372,9 +371,19 @@ __global__ void __launch_bounds__(kSegThreads, GATED ? 5 : 6) segment_kernel(con
     const int64_t begin = min(((int64_t)blockIdx.x * GROUPS + grp) * chunk, a.n), end = min(begin + chunk, a.n);
     const bool live = begin < end;
     grid_dependency_wait();
+    // a lane's share of the next rows: position of row `sub` (and `sub` + LANES)
+    int32_t ahead[PER];
+    auto look_ahead = [&](int64_t t0) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int64_t t = t0 + sub + i * LANES;
+            ahead[i] = sub + i * LANES < AHEAD && t < end ? ld(order + t) : -1;
+        }
+    };
+    look_ahead(begin);
     // the entries of the first and the last position (m: no entry)
-    int64_t ends_at[2];
-    entries_of_group<LANES>(offset, {begin, end - 1}, live ? a.m : 0, ends_at);
+    uint32_t ends_at[2];
+    entries_of_group<LANES>(offset, {begin, end - 1}, live ? (uint32_t)a.m : 0, ends_at);
     int64_t j = ends_at[0];
     const int64_t j_last = ends_at[1];
     int64_t run_end = live && j < a.m ? offset[j + 1] : a.n;
@@ -422,18 +431,10 @@ __global__ void __launch_bounds__(kSegThreads, GATED ? 5 : 6) segment_kernel(con
         head = false;
     };
     if (live) fetch_pool();
-    // a lane's share of the next rows: position of row `sub` (and `sub` + LANES)
-    int32_t ahead[PER];
-    auto look_ahead = [&](int64_t t0) {
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int64_t t = t0 + sub + i * LANES;
-            ahead[i] = sub + i * LANES < AHEAD && t < end ? ld(order + t) : -1;
-        }
-    };
-    look_ahead(begin);
     const E* const rows = (const E*)a.rows + g * a.group_stride + col0;
-    const int user_bytes = a.skip <= N && ((uintptr_t)a.d_user & (a.skip * sizeof(E) - 1)) == 0 ? a.skip * (int)sizeof(E) : 0;
+    // user parts that lie on their own size, of two to eight bytes, or pieces on theirs
+    const int ub = a.skip * (int)sizeof(E), user_bytes = a.d_user && (ub == 2 || ub == 4 || ub == 8) && (uintptr_t)a.d_user % ub == 0 ? ub : 0;
+    const bool user_whole = ((uintptr_t)a.d_user | ub) % 16 == 0;
     for (int64_t t0 = begin; t0 < begin + chunk; t0 += AHEAD) {  // (as many turns for every chunk: a warp's stay together)
         int32_t pos[PER], key[PER];
         float2 gate[PER];  // weight of the row; GATED: and one less it
@@ -457,6 +458,11 @@ __global__ void __launch_bounds__(kSegThreads, GATED ? 5 : 6) segment_kernel(con
             for (int i = 0; i < PER; ++i) {
                 const int64_t t = t0 + sub + i * LANES;
                 key[i] = (int32_t)entry_of(offset, min(t, end - 1), j, j_last);
+                if (GATED && key[i] < a.m) {  // the runs' pool rows, which are wanted one after the other
+                    const E* p = (const E*)a.pool + ((int64_t)g * a.m + key[i]) * ds;
+                    asm volatile("prefetch.global.L1 [%0];" ::"l"(p));
+                    asm volatile("prefetch.global.L1 [%0];" ::"l"(p + ds - 1));
+                }
             }
         // Run by run: all rows of the entry at hand, then the next entry's, until no chunk of the warp has more.  (A flush between any two
         // rows made code that did not fit the instruction cache.)
@@ -499,22 +505,32 @@ __global__ void __launch_bounds__(kSegThreads, GATED ? 5 : 6) segment_kernel(con
             }
         } while (more);
         if (mixed) run_end = j < a.m ? ld(offset + j + 1) : a.n;
-        if (a.d_user) {
+        if (user_bytes) {  // a part that one store takes: of row `sub` (and `sub` + LANES)
+            uint2 part[PER] = {};
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                const uint32_t x = __shfl_sync(0xffffffffu, raw[k].x, 0, LANES), y = user_bytes == 8 ? __shfl_sync(0xffffffffu, raw[k].y, 0, LANES) : 0;
+                if (k % LANES == sub) part[k / LANES] = make_uint2(x, y);
+            }
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                char* const to = reinterpret_cast<char*>(a.d_user) + ((int64_t)pos[i] * a.G + g) * user_bytes;
+                if (pos[i] < 0) continue;
+                if (user_bytes == 2) *reinterpret_cast<uint16_t*>(to) = (uint16_t)part[i].x;
+                else if (user_bytes == 4) *reinterpret_cast<uint32_t*>(to) = part[i].x;
+                else *reinterpret_cast<uint2*>(to) = part[i];
+            }
+        } else if (a.d_user) {
 #pragma unroll
             for (int k = 0; k < AHEAD; ++k) {
                 const int32_t p = __shfl_sync(0xffffffffu, pos[k / LANES], k % LANES, LANES);
                 if (p < 0 || col0 >= a.skip) continue;
                 E* to = (E*)a.d_user + ((int64_t)p * a.G + g) * a.skip + col0;
-                switch (user_bytes) {  // one store for a row's whole part
-                    case 2: *reinterpret_cast<uint16_t*>(to) = (uint16_t)raw[k].x; break;
-                    case 4: *reinterpret_cast<uint32_t*>(to) = raw[k].x; break;
-                    case 8: *reinterpret_cast<uint2*>(to) = make_uint2(raw[k].x, raw[k].y); break;
-                    case 16: *reinterpret_cast<uint4*>(to) = raw[k]; break;
-                    default:
+                if (user_whole && col0 + N <= a.skip) *reinterpret_cast<uint4*>(to) = raw[k];
+                else
 #pragma unroll
-                        for (int q = 0; q < N; ++q)
-                            if (col0 + q < a.skip) to[q] = reinterpret_cast<const E*>(&raw[k])[q];
-                }
+                    for (int q = 0; q < N; ++q)
+                        if (col0 + q < a.skip) to[q] = reinterpret_cast<const E*>(&raw[k])[q];
             }
         }
         if (GATED && a.d_score) {
