@@ -365,6 +365,7 @@ __global__ void __launch_bounds__(kSegThreads, GATED ? 5 : 6) segment_kernel(con
     __shared__ __align__(16) float ends[GROUPS][2][WIDTH];
     __shared__ float wends[GROUPS][2];
     __shared__ Ends info[GROUPS];
+    __shared__ __align__(16) uint4 stage[2][AHEAD][kSegThreads];  // a turn's rows, and the next turn's on their way
     const int lane = threadIdx.x & 31, sub = lane % LANES, grp = threadIdx.x / LANES, g = blockIdx.y, col0 = sub * N, ds = WIDTH - a.skip;
     const unsigned mine = (LANES == 32 ? 0xffffffffu : (1u << LANES % 32) - 1) << (lane - sub);
     const int32_t *order = a.order + (int64_t)g * a.n, *offset = a.offset + (int64_t)g * (a.m + 1);
@@ -380,7 +381,30 @@ __global__ void __launch_bounds__(kSegThreads, GATED ? 5 : 6) segment_kernel(con
             ahead[i] = sub + i * LANES < AHEAD && t < end ? ld(order + t) : -1;
         }
     };
+    const E* const rows = (const E*)a.rows + g * a.group_stride + col0;
+    int32_t pos[PER];
+    float sc[PER];
+    uint64_t once;  // rows are read once, and leave the L2 to scores and results by position, of whose sectors a warp has a few bytes each
+    asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(once));
+    // rows and scores of the positions looked up, by asynchronous copies of a lane's 16 bytes of each row; then the next positions
+    auto fetch_rows = [&](int buf, int64_t next) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            pos[i] = ahead[i] < a.n ? ahead[i] : -1;  // (not an order)
+            sc[i] = pos[i] >= 0 && a.score ? ld(a.score + (int64_t)pos[i] * a.G + g) : 0.f;
+        }
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const int32_t p = __shfl_sync(0xffffffffu, pos[k / LANES], k % LANES, LANES);
+            if (p >= 0)
+                asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" ::"r"(smem_u32(&stage[buf][k][threadIdx.x])), "l"(rows + p * a.stride), "l"(once)
+                             : "memory");
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        look_ahead(next);
+    };
     look_ahead(begin);
+    fetch_rows(0, begin + AHEAD);
     // the entries of the first and the last position (m: no entry)
     uint32_t ends_at[2];
     entries_of_group<LANES>(offset, {begin, end - 1}, live ? (uint32_t)a.m : 0, ends_at);
@@ -431,27 +455,20 @@ __global__ void __launch_bounds__(kSegThreads, GATED ? 5 : 6) segment_kernel(con
         head = false;
     };
     if (live) fetch_pool();
-    const E* const rows = (const E*)a.rows + g * a.group_stride + col0;
     // user parts that lie on their own size, of two to eight bytes, or pieces on theirs
     const int ub = a.skip * (int)sizeof(E), user_bytes = a.d_user && (ub == 2 || ub == 4 || ub == 8) && (uintptr_t)a.d_user % ub == 0 ? ub : 0;
     const bool user_whole = ((uintptr_t)a.d_user | ub) % 16 == 0;
-    for (int64_t t0 = begin; t0 < begin + chunk; t0 += AHEAD) {  // (as many turns for every chunk: a warp's stay together)
-        int32_t pos[PER], key[PER];
+    int buf = 0;
+    for (int64_t t0 = begin; t0 < begin + chunk; t0 += AHEAD, buf ^= 1) {  // (as many turns for every chunk: a warp's stay together)
+        int32_t at[PER], key[PER];
         float2 gate[PER];  // weight of the row; GATED: and one less it
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            pos[i] = ahead[i] < a.n ? ahead[i] : -1;  // (not an order)
-            const float sc = pos[i] >= 0 && a.score ? ld(a.score + (int64_t)pos[i] * a.G + g) : 0.f;
-            gate[i] = pos[i] < 0 ? make_float2(0.f, 0.f) : !a.score ? make_float2(1.f, 0.f) : GATED ? sigmoids(sc) : make_float2(sc, 0.f);
+            at[i] = pos[i];
+            gate[i] = at[i] < 0 ? make_float2(0.f, 0.f) : !a.score ? make_float2(1.f, 0.f) : GATED ? sigmoids(sc[i]) : make_float2(sc[i], 0.f);
             key[i] = (int32_t)j;
         }
-        uint4 raw[AHEAD];
-#pragma unroll
-        for (int k = 0; k < AHEAD; ++k) {
-            const int32_t p = __shfl_sync(0xffffffffu, pos[k / LANES], k % LANES, LANES);
-            raw[k] = p >= 0 ? __ldcs(reinterpret_cast<const uint4*>(rows + p * a.stride)) : make_uint4(0, 0, 0, 0);
-        }
-        look_ahead(t0 + AHEAD);
+        fetch_rows(buf ^ 1, t0 + 2 * AHEAD);
         const bool mixed = t0 + AHEAD > run_end && j != j_last;
         if (mixed)
 #pragma unroll
@@ -464,6 +481,9 @@ __global__ void __launch_bounds__(kSegThreads, GATED ? 5 : 6) segment_kernel(con
                     asm volatile("prefetch.global.L1 [%0];" ::"l"(p + ds - 1));
                 }
             }
+        asm volatile("cp.async.wait_group 1;" ::: "memory");
+        __syncwarp();  // (a lane reads other lanes' pieces)
+        const uint4* const raw = &stage[buf][0][threadIdx.x];
         // Run by run: all rows of the entry at hand, then the next entry's, until no chunk of the warp has more.  (A flush between any two
         // rows made code that did not fit the instruction cache.)
         float dot[AHEAD] = {};
@@ -473,14 +493,15 @@ __global__ void __launch_bounds__(kSegThreads, GATED ? 5 : 6) segment_kernel(con
             int32_t next = INT32_MAX;
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                here[i] = (__ballot_sync(0xffffffffu, fresh && pos[i] >= 0 && key[i] == (int32_t)j) & mine) >> (lane - sub);
-                if (pos[i] >= 0 && key[i] > (int32_t)j) next = min(next, key[i]);
+                here[i] = (__ballot_sync(0xffffffffu, fresh && at[i] >= 0 && key[i] == (int32_t)j) & mine) >> (lane - sub);
+                if (at[i] >= 0 && key[i] > (int32_t)j) next = min(next, key[i]);
             }
 #pragma unroll
             for (int k = 0; k < AHEAD; ++k) {
                 const float w = __shfl_sync(0xffffffffu, gate[k / LANES].x, k % LANES, LANES);
                 if (here[k / LANES] >> (k % LANES) & 1) {
-                    const E* v = reinterpret_cast<const E*>(&raw[k]);
+                    const uint4 row = raw[k * kSegThreads];
+                    const E* v = reinterpret_cast<const E*>(&row);
                     float sum = 0.f;
 #pragma unroll
                     for (int q = 0; q < N; ++q) {
@@ -506,41 +527,38 @@ __global__ void __launch_bounds__(kSegThreads, GATED ? 5 : 6) segment_kernel(con
         } while (more);
         if (mixed) run_end = j < a.m ? ld(offset + j + 1) : a.n;
         if (user_bytes) {  // a part that one store takes: of row `sub` (and `sub` + LANES)
-            uint2 part[PER] = {};
-#pragma unroll
-            for (int k = 0; k < AHEAD; ++k) {
-                const uint32_t x = __shfl_sync(0xffffffffu, raw[k].x, 0, LANES), y = user_bytes == 8 ? __shfl_sync(0xffffffffu, raw[k].y, 0, LANES) : 0;
-                if (k % LANES == sub) part[k / LANES] = make_uint2(x, y);
-            }
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                char* const to = reinterpret_cast<char*>(a.d_user) + ((int64_t)pos[i] * a.G + g) * user_bytes;
-                if (pos[i] < 0) continue;
-                if (user_bytes == 2) *reinterpret_cast<uint16_t*>(to) = (uint16_t)part[i].x;
-                else if (user_bytes == 4) *reinterpret_cast<uint32_t*>(to) = part[i].x;
-                else *reinterpret_cast<uint2*>(to) = part[i];
+                char* const to = reinterpret_cast<char*>(a.d_user) + ((int64_t)at[i] * a.G + g) * user_bytes;
+                if (at[i] < 0) continue;
+                const uint2 part = *reinterpret_cast<const uint2*>(&stage[buf][sub + i * LANES][threadIdx.x - sub]);
+                if (user_bytes == 2) *reinterpret_cast<uint16_t*>(to) = (uint16_t)part.x;
+                else if (user_bytes == 4) *reinterpret_cast<uint32_t*>(to) = part.x;
+                else *reinterpret_cast<uint2*>(to) = part;
             }
         } else if (a.d_user) {
 #pragma unroll
             for (int k = 0; k < AHEAD; ++k) {
-                const int32_t p = __shfl_sync(0xffffffffu, pos[k / LANES], k % LANES, LANES);
+                const int32_t p = __shfl_sync(0xffffffffu, at[k / LANES], k % LANES, LANES);
                 if (p < 0 || col0 >= a.skip) continue;
                 E* to = (E*)a.d_user + ((int64_t)p * a.G + g) * a.skip + col0;
-                if (user_whole && col0 + N <= a.skip) *reinterpret_cast<uint4*>(to) = raw[k];
+                const uint4 row = raw[k * kSegThreads];
+                if (user_whole && col0 + N <= a.skip) *reinterpret_cast<uint4*>(to) = row;
                 else
 #pragma unroll
                     for (int q = 0; q < N; ++q)
-                        if (col0 + q < a.skip) to[q] = reinterpret_cast<const E*>(&raw[k])[q];
+                        if (col0 + q < a.skip) to[q] = reinterpret_cast<const E*>(&row)[q];
             }
         }
         if (GATED && a.d_score) {
             share_out<LANES, AHEAD>(dot, sub);
 #pragma unroll
             for (int i = 0; i < PER; ++i)
-                if (pos[i] >= 0) a.d_score[(int64_t)pos[i] * a.G + g] = key[i] < a.m ? dot[i] * gate[i].x * gate[i].y : 0.f;
+                if (at[i] >= 0) a.d_score[(int64_t)at[i] * a.G + g] = key[i] < a.m ? dot[i] * gate[i].x * gate[i].y : 0.f;
         }
+        __syncwarp();  // (the next turn's copies go where these rows are)
     }
-    __syncwarp(mine);
+    asm volatile("cp.async.wait_all;" ::: "memory");
     if (live) flush(j < a.m && run_end > end);
     __syncthreads();
     // the block's chunks in their order, a thread per column (and one for the weights)
