@@ -682,11 +682,12 @@ __global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const SegmentArgs
     }
 }
 
-// Positions of a chunk: short ones until the chunks' lanes fill the SMs, long ones to leave few partial sums.
+// Positions of a chunk: short ones until the chunks' lanes fill the SMs, long ones to leave few partial sums.  (1048576 x 4 positions: 234 us with
+// 32, 217 with 64, 227 with 128, 266 with 256.)
 int chunk_of(int64_t n, int G)
 {
     int c = 8;
-    while (c < 128 && n * G / c > 16384) c *= 2;
+    while (c < 64 && n * G / c > 16384) c *= 2;
     return c;
 }
 // of a block: kSegThreads / lanes chunks
