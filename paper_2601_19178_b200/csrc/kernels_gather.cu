@@ -50,7 +50,8 @@ __device__ __forceinline__ void load16(uint32_t (&w)[4], const void* p)
 // the gate; then the lanes run over the rows' 16-byte pieces side by side.  A pool row of 60 or 62 bytes lies on no wider
 // boundary than a word or an element: LOAD is what all pieces lie on.  log_pieces: of a row; log_rows: rows of a warp, fewer
 // where there are few, so that a warp's chain of loads is short.  skip: elements of a row in front of the pool's, the user's or
-// (widened pool) none.
+// (widened pool) none.  Bound by the rows written (537 MB alone take 106 us) and the L1, through which pool rows and user parts
+// come (issue slots 73 % used): 1048576 x 8 rows of 64 bytes, of which 4 bytes are the user's, 158 us with the copy of the pool.  200 x 2 rows: 2.4.
 // STREAMED: stores of 16 bytes that leave the L2 to the pool.
 template <typename E, int LOAD, bool STREAMED>
 __global__ void __launch_bounds__(256) gather_kernel(int64_t rows, int G, int log_pieces, int log_rows, int skip, int user_width, int user_bytes, int ds, int64_t m, int store,
@@ -72,12 +73,15 @@ __global__ void __launch_bounds__(256) gather_kernel(int64_t rows, int G, int lo
         if (score) score_next = there ? ld(score + r) : 0.f;
     };
     int64_t r0 = (blockIdx.x * (int64_t)8 + (threadIdx.x >> 5)) << log_rows;
+    int group = (int)((r0 + lane) % G);  // of the lane's row
+    const int step_groups = (int)(step % G);
     look_ahead(r0);
     for (; r0 < rows; r0 += step) {
         const int n_rows = (int)min(rows - r0, (int64_t)1 << log_rows);
-        const uint32_t from = idx_next >= 0 && idx_next < m ? (uint32_t)((r0 + lane) % G * m + idx_next) : kNone;  // (no pool has as many rows)
+        const uint32_t from = idx_next >= 0 && idx_next < m ? (uint32_t)group * (uint32_t)m + (uint32_t)idx_next : kNone;  // (no pool has as many rows)
         const float gate = score ? sigmoid(score_next) : 1.f;
         look_ahead(r0 + step);
+        group += step_groups - (group + step_groups >= G ? G : 0);
         char* const to = reinterpret_cast<char*>(out) + r0 * bytes;
 #pragma unroll 4
         for (int i = 0; i < 1 << (log_pieces + log_rows - 5); ++i) {
@@ -136,7 +140,10 @@ __global__ void __launch_bounds__(256) gather_kernel(int64_t rows, int G, int lo
 // The sorted positions of a group are cut into chunks of equal length, whatever the entries.  LANES lanes walk a chunk, 16 bytes of
 // a row each.  A run that lies inside the chunk is written; the one that began before it and the one that goes on behind it leave a
 // partial sum (head, tail), which the block joins in the order of its chunks, and of the blocks join_kernel.  Nothing
-// depends on the order in which warps run.
+// depends on the order in which warps run.  1048576 x 4 rows of 128 bytes with gate, d_score and d_user: 217 us, the
+// bare sums some two thirds of it; neither memory (2.8 TB/s) nor issue (43 %) is full: the turns' chains of loads, shuffles and shared memory
+// bind, at the 20 warps per SM that their registers and stages leave, next to three sectors per row of which a few bytes are
+// wanted.  20011 x 4 rows: 13 us and the join, all latency (search of the first entry 3, rows 1, runs of few positions 4).
 constexpr int kSegThreads = 128;
 
 // sigmoid(x) and 1 - sigmoid(x)
@@ -757,7 +764,7 @@ __global__ void __launch_bounds__(256) widen_pool_kernel(int64_t pieces, int log
 }
 
 // Whether a lookup copies the pool first.  Four loads of a piece's words (eight of its elements) keep the L1 busy for longer than the row
-// takes to store (1048576 x 8 rows of 64 bytes 261 us, 160 behind a copy of 5), which pays once there are some rows per entry.
+// takes to store (1048576 x 8 rows of 64 bytes 261 us, 158 behind a copy of 3), which pays once there are some rows per entry.
 bool widens(int64_t n, int D, int ds, int64_t m, int elem) { return n >= 2 * m && (ds * elem % 16 != 0 || (D - ds) * elem % 16 != 0); }
 
 template <typename E>
@@ -780,7 +787,7 @@ cudaError_t launch_gather_t(int64_t n, int G, int D, int ds, int64_t m, const vo
     auto lies_on = [](const void* p, int step) { return ((uintptr_t)p | (uintptr_t)step) % 16 == 0 ? 16 : ((uintptr_t)p | (uintptr_t)step) % 4 == 0 ? 4 : 2; };
     // a user part that one load takes, or pieces that one load each takes
     const int ub = user_width * e % 16 == 0 ? 16 : user_width * e, user_bytes = (ub == 2 || ub == 4 || ub == 8 || ub == 16) && (uintptr_t)user % ub == 0 ? ub : 0;
-    // A pool that takes a good part of the L2 keeps it better when the rows written leave first (300000 x 4 rows, pool of 146 MB: 91 us and 86; of
+    // A pool that takes a good part of the L2 keeps it better when the rows written leave first (300000 x 4 rows, pool of 146 MB: 90 us and 81; of
     // 29 MB: 87 and 82); a small one is there anyway (1048576 x 8 rows, 2 MB: 160 and 161).
     const int load = std::min(lies_on(pool, ds * e), lies_on(nullptr, skip * e)), store = lies_on(out, 16);
     const bool streamed = store == 16 && G * m * ds * e >= 8 << 20;

@@ -105,7 +105,7 @@ __device__ __forceinline__ void prepare_entry(const RouteLossArgs& a, const Rout
 }
 
 // Positions: x for the passes (zeros for one that takes part in no group, whose inputs may be anything); forward: the picked entry's
-// score; gradient: -lse and the picked entry's coefficient.  A position to D / 8 lanes, 16 bytes of it to each.  The first
+// score (rows of W by index, 32768 positions x 4 groups x 128 bytes 22 us: latency); gradient: -lse and the picked entry's coefficient (13 us).  A position to D / 8 lanes, 16 bytes of it to each.  The first
 // `entry_blocks` blocks, as many for each group, prepare the entries instead.
 template <int D, bool GRAD>
 __global__ void __launch_bounds__(256) prepare_kernel(const RouteLossArgs a, const RouteGradArgs b, const Space s, int64_t np, int64_t mp,
@@ -200,6 +200,7 @@ __device__ __forceinline__ void put8(uint16_t* out, const float (&v)[8], bool wh
     }
 }
 
+// Bound by memory, which gives the partial sums back: 200 positions x 1024 entries x 2 groups 4.7 us, 10007 x 4099 x 3 at d_in = 128 10 us.
 // The first dx_blocks blocks: dx, the partial sums and the picked entries' rows.  The others: dW and db, the partial sums and the sums over the
 // positions that picked the entry.
 __global__ void __launch_bounds__(256) grad_join_kernel(const RouteLossArgs a, const RouteGradArgs b, const SweepArgs p, int dx_blocks)

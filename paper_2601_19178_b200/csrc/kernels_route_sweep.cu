@@ -10,6 +10,9 @@
 //   grad_kernel (DX, DW)         turns it into weights T (bf16, over the head of the scores they came from), which multiply the
 //                                same tile once more, now as MN-major operand:  O += T tile.  Two blocks per CTA (one at d_in =
 //                                128), each with two score buffers whose turns belong to four warps each.
+// Bound by the special-function unit, 16 exponentials per clock and SM, and the FMA pipe, which takes its share of them: 32768 positions x 16384
+// entries x 4 groups (2.1e9 scores, whose exponentials would take that unit alone 477 us per pass), d_in = 64: LSE 503 us, MEAN 466, R 525
+// to 545, DX and DW 1280 to 1355; special-function unit 67 to 76 % busy, issue slots 57 to 65 %, tensor cores 31 to 46 %.
 // Every wait is bounded: a time-out raises the CTA's abort flag, which ends all others; the CTA waits for its copies and
 // products in flight, frees its TMEM, and its results are NaN.
 #include <cuda_bf16.h>

@@ -33,6 +33,7 @@ struct Pass {
 };
 __device__ __forceinline__ int digit_of(uint32_t key, const Pass& p) { return (int)(key >> p.shift) & p.mask & 0x7fff; }
 
+// Bound by shared-memory atomics (the data pipe 65 % busy) and the strided indices: 1048576 x 8 positions, 4096 entries 26 us.
 __global__ void __launch_bounds__(256) count_kernel(const Pass p, int32_t* table)
 {
     extern __shared__ int32_t bins[];
@@ -138,7 +139,7 @@ __device__ __forceinline__ int32_t take_places(volatile int32_t* next, int d, un
 
 // A chunk's positions to their places, by one warp (the block's others help to fetch next[]).  Bound by its turns, of which a match
 // instruction is the longest part (its time grows with the number of different keys in the warp; 0.3 us a turn): 1048576 x 8
-// positions, 4096 entries 81 us.  (Lanes that find each other through a word per key, as in block_sort_kernel, halve a turn, but with
+// positions, 4096 entries 73 us of 112.  (Lanes that find each other through a word per key, as in block_sort_kernel, halve a turn, but with
 // half as many warps to an SM: 85; two to eight warps with a part of a larger chunk each, whose parts the block counts first, no
 // less, for the match instructions of an SM take turns; votes on the 13 bits of a key instead of the match 113.)
 __global__ void __launch_bounds__(128) place_kernel(const Pass p, const int32_t* table, const int32_t* base)
