@@ -517,6 +517,47 @@ def test_gpu_gather_grad(dtype, n, G, m, D, du):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype,D,du", [("bf16", 64, 0), ("bf16", 64, 1), ("bf16", 64, 2), ("bf16", 64, 24), ("f32", 64, 4), ("f32", 64, 1)])
+def test_gpu_gather_from_a_large_pool(dtype, D, du):
+    """Pools of 8 MB and more, whose rows lie on elements, words or pieces, with fewer rows than twice the entries and with more."""
+    import paper_2601_19178_b200 as ckv
+    m = 40000
+    pool, idx, user, score, _ = _gather_case(2, dtype, 2 * m + 5, 2, m, D, du, True)
+    for n in (777, 2 * m + 5):
+        i, u, s = idx[:n], None if user is None else user[:n], score[:n]
+        got = _host(ckv.gather(_dev(pool), _dev(i), _dev(u), _dev(s)))
+        want = F.gather(pool, i, u, s)
+        _close(got, want, (2.0 ** -20 + (2.0 ** -8 if dtype == "bf16" else 2.0 ** -24)) * np.abs(want), f"n={n}")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [300, 2000])
+@pytest.mark.parametrize("dtype,D,du", [("bf16", 64, 1), ("bf16", 64, 4), ("bf16", 64, 8), ("bf16", 128, 24), ("bf16", 16, 3), ("f32", 32, 2), ("f32", 32, 4),
+                                        ("f32", 128, 12)])
+def test_gpu_gather_gradient_into_arrays_off_their_pieces(n, dtype, D, du):
+    """Results an element further on: the bits of the aligned ones.  NaN where no position has an entry, and in rows nobody picked."""
+    import torch
+    import paper_2601_19178_b200 as ckv
+    G, m = 3, 200
+    pool, idx, user, score, d_out = _gather_case(n + du, dtype, n, G, m, D, du, True)
+    nan = 0x7fc0 if dtype == "bf16" else np.nan
+    d_out[:, :, du:][(idx < 0) | (idx >= m)] = nan
+    for g in range(G):
+        pool[g, np.setdiff1d(np.arange(m), idx[:, g])] = nan
+    p, s, d = _dev(pool), _dev(score), _dev(d_out)
+    order = ckv.sort_indices(_dev(idx), m)
+    want = ckv.gather_grad(p, order, s, d)
+    assert all(torch.isfinite(t).all() for t in (want[0], want[2]))
+    moved = [torch.full((t.numel() + 8,), 7.0, dtype=t.dtype, device="cuda") for t in want]
+    into = [f[1:t.numel() + 1].view(t.shape) for f, t in zip(moved, want)]
+    need = ckv.ckv_gather_grad_bytes(n, G, D)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda") if need else None
+    ckv.ckv_gather_grad(0, ckv.CKV_BF16 if dtype == "bf16" else ckv.CKV_F32, n, G, D, D - du, m, p, *order, s, d, *into, ws, need)
+    for f, t, w in zip(moved, into, want):
+        assert torch.equal(t, w) and f[0] == 7 and (f[t.numel() + 1:] == 7).all()
+
+
+@pytest.mark.gpu
 def test_gpu_gather_and_gradient_without_positions():
     import torch
     import paper_2601_19178_b200 as ckv
