@@ -464,9 +464,10 @@ __global__ void __launch_bounds__(kSegThreads, GATED ? 5 : 6) segment_kernel(con
         head = false;
     };
     if (live) fetch_pool();
-    // user parts that lie on their own size, of two to eight bytes, or pieces on theirs
-    const int ub = a.skip * (int)sizeof(E), user_bytes = a.d_user && (ub == 2 || ub == 4 || ub == 8) && (uintptr_t)a.d_user % ub == 0 ? ub : 0;
-    const bool user_whole = ((uintptr_t)a.d_user | ub) % 16 == 0;
+    // A user part is copied in units that its size and address allow: one or two by the lane that has its row's position (500000 x 4 rows of 64
+    // bf16, parts of 16 bytes: 140 us), more by the lanes that have pieces of it (parts of 10 bytes 171; the other way 154 and 188).
+    const int user_bytes = a.skip * (int)sizeof(E), user_at = user_bytes | 16 | (int)((uintptr_t)a.d_user & 15), user_unit = user_at & -user_at;
+    const bool user_by_row = a.d_user && user_bytes <= 2 * user_unit;
     int buf = 0;
     for (int64_t t0 = begin; t0 < begin + chunk; t0 += AHEAD, buf ^= 1) {  // (as many turns for every chunk: a warp's stay together)
         int32_t at[PER], key[PER];
@@ -535,24 +536,29 @@ __global__ void __launch_bounds__(kSegThreads, GATED ? 5 : 6) segment_kernel(con
             }
         } while (more);
         if (mixed) run_end = j < a.m ? ld(offset + j + 1) : a.n;
-        if (user_bytes) {  // a part that one store takes: of row `sub` (and `sub` + LANES)
+        if (user_by_row) {  // lane `sub`: row `sub` (and `sub` + LANES)
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
                 char* const to = reinterpret_cast<char*>(a.d_user) + ((int64_t)at[i] * a.G + g) * user_bytes;
                 if (at[i] < 0) continue;
-                const uint2 part = *reinterpret_cast<const uint2*>(&stage[buf][sub + i * LANES][threadIdx.x - sub]);
-                if (user_bytes == 2) *reinterpret_cast<uint16_t*>(to) = (uint16_t)part.x;
-                else if (user_bytes == 4) *reinterpret_cast<uint32_t*>(to) = part.x;
-                else *reinterpret_cast<uint2*>(to) = part;
+                for (int o = 0; o < user_bytes; o += user_unit) {
+                    const char* const from = reinterpret_cast<const char*>(&stage[buf][sub + i * LANES][threadIdx.x - sub + o / 16]) + o % 16;
+                    switch (user_unit) {
+                        case 2: *reinterpret_cast<uint16_t*>(to + o) = *reinterpret_cast<const uint16_t*>(from); break;
+                        case 4: *reinterpret_cast<uint32_t*>(to + o) = *reinterpret_cast<const uint32_t*>(from); break;
+                        case 8: *reinterpret_cast<uint2*>(to + o) = *reinterpret_cast<const uint2*>(from); break;
+                        default: *reinterpret_cast<uint4*>(to + o) = *reinterpret_cast<const uint4*>(from);
+                    }
+                }
             }
-        } else if (a.d_user) {
+        } else if (a.d_user) {  // lane `sub`: its piece of every row
 #pragma unroll
             for (int k = 0; k < AHEAD; ++k) {
                 const int32_t p = __shfl_sync(0xffffffffu, at[k / LANES], k % LANES, LANES);
                 if (p < 0 || col0 >= a.skip) continue;
                 E* to = (E*)a.d_user + ((int64_t)p * a.G + g) * a.skip + col0;
                 const uint4 row = raw[k * kSegThreads];
-                if (user_whole && col0 + N <= a.skip) *reinterpret_cast<uint4*>(to) = row;
+                if (user_unit == 16) *reinterpret_cast<uint4*>(to) = row;
                 else
 #pragma unroll
                     for (int q = 0; q < N; ++q)
