@@ -4,6 +4,9 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
+#include <map>
+#include <mutex>
 #include <utility>
 
 #include "ckv.h"
@@ -122,6 +125,26 @@ struct Launch {
     bool early = false;  // programmatic launch: the blocks may be set up while the stream's previous kernel still runs
                          // (the kernel waits for that one's memory itself, grid_dependency_wait)
 };
+// A kernel's permission is the whole process's, on each device: whoever asks for less than somebody else was given asks for that again,
+// so that no thread or context takes from another what it is about to launch with.
+inline cudaError_t permit_smem(const void* fn, size_t* bytes)
+{
+    static std::mutex mu;
+    static std::map<std::pair<const void*, int>, size_t> permitted;
+    std::lock_guard<std::mutex> lock(mu);
+    int device = -1;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return e;
+    try {
+        size_t& most = permitted[{fn, device}];
+        *bytes = std::max(*bytes, most);
+        e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)*bytes);
+        if (e == cudaSuccess) most = *bytes;
+    } catch (...) {  // (no memory for the record)
+        e = cudaErrorMemoryAllocation;
+    }
+    return e;
+}
 inline cudaError_t grant_smem(SmemGrants* g, const void* fn, size_t bytes)
 {
     if (bytes <= 48 * 1024) return cudaSuccess;
@@ -130,7 +153,7 @@ inline cudaError_t grant_smem(SmemGrants* g, const void* fn, size_t bytes)
         while (i < g->n && g->fn[i] != fn) ++i;
         if (i < g->n && g->bytes[i] >= bytes) return cudaSuccess;
     }
-    const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    const cudaError_t e = permit_smem(fn, &bytes);
     if (e == cudaSuccess && g && i < SmemGrants::kMax) {
         g->fn[i] = fn;
         g->bytes[i] = bytes;

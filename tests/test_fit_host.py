@@ -1,0 +1,53 @@
+"""What the training-side calls do on the host, on the CPU: the library's object files linked with a stand-in for the CUDA runtime."""
+import ctypes as C
+import os
+import subprocess
+import threading
+
+import pytest
+
+from test_host_side import ROOT, device_block, objects  # noqa: F401
+
+
+def _stand_in(objects, tmp, source):
+    so = str(tmp / ("lib" + source.replace(".cpp", ".so")))
+    subprocess.run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wl,-Bsymbolic", "-I/usr/local/cuda/include", "-o", so,
+                    *objects, os.path.join(ROOT, "tests", source)], check=True)
+    return C.CDLL(so)
+
+
+@pytest.fixture(scope="module")
+def lib_smem(objects, tmp_path_factory):
+    return _stand_in(objects, tmp_path_factory.mktemp("smem"), "fake_smem.cpp")
+
+
+def _in_a_thread(work):
+    got = []
+    t = threading.Thread(target=lambda: got.append(work()))
+    t.start()
+    t.join(60)
+    assert not t.is_alive()
+    return got[0]
+
+
+@pytest.mark.parametrize("n,large,small", [(5000, 20000, 13000), (9000, 24000, 14000)])
+def test_a_sort_leaves_other_threads_their_shared_memory(lib_smem, n, large, small):
+    """A thread's first sort, while another thread's first one, with fewer entries, runs between its permission and its launch."""
+    lib = lib_smem
+    need, other = C.c_int64(), C.c_int64()
+    assert lib.ckv_sort_indices_bytes(n, 2, large, C.byref(need)) == lib.ckv_sort_indices_bytes(n, 2, small, C.byref(other)) == 0
+    need.value = max(need.value, other.value)
+    d, w = device_block(lib, 1 << 20), device_block(lib, max(need.value, 1) + 256)
+    ws = C.c_void_p((w.value + 255) // 256 * 256)
+
+    def sort(m):
+        return lib.ckv_sort_indices(0, n, 2, m, d, d, d, ws, C.c_int64(need.value), None)
+
+    inner = []
+    hook = C.CFUNCTYPE(None)(lambda: inner.append(_in_a_thread(lambda: sort(small))))
+
+    def outer():
+        lib.fake_before_launch(hook)
+        return sort(large)
+
+    assert _in_a_thread(outer) == 0 and inner == [0]
