@@ -132,6 +132,7 @@ __device__ __forceinline__ int32_t take_places(volatile int32_t* next, int d, un
     const int lane = threadIdx.x & 31;
     int32_t at = 0;
     if (d >= 0) at = next[d];
+    __syncwarp();  // (every lane has read before one writes)
     if (d >= 0 && lane == __ffs(same) - 1) next[d] = at + __popc(same);
     __syncwarp();
     return at + __popc(same & ((1u << lane) - 1));

@@ -1,6 +1,7 @@
 """What the training-side calls do on the host, on the CPU: the library's object files linked with a stand-in for the CUDA runtime."""
 import ctypes as C
 import os
+import re
 import subprocess
 import threading
 
@@ -51,3 +52,15 @@ def test_a_sort_leaves_other_threads_their_shared_memory(lib_smem, n, large, sma
         return sort(large)
 
     assert _in_a_thread(outer) == 0 and inner == [0]
+
+
+def test_lanes_that_share_a_counter_read_it_before_it_moves_on():
+    """Lanes with equal keys read the key's next place, and one of them writes the new one: the warp meets in between, for nothing else
+    keeps its lanes together.  No result tells, so the source is read."""
+    code = re.sub(r"//[^\n]*", "", open(os.path.join(ROOT, "paper_2601_19178_b200", "csrc", "kernels_sort.cu")).read())
+    bodies = re.findall(r"int32_t take_places\(.*?\n\{(.*?)\n\}", code, re.S)
+    assert len(bodies) == 2
+    for body in bodies:
+        read = max(m.start() for m in re.finditer(r"(= next\[d\]|volatile unsigned long long\*>\(slots \+ d\);)", body))
+        write = re.search(r"next\[d\] = |slots \+ d\) = ", body).start()
+        assert "__syncwarp();" in body[read:write], body
