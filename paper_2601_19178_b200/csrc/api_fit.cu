@@ -20,23 +20,25 @@ struct Arg {
     int align;
     bool optional = false;
 };
-// Device memory (or managed), aligned to its elements.
+// Memory of the call's device (or managed), aligned to its elements.
 template <typename... A>
-bool on_device(const A&... args)
+bool on_device(int device, const A&... args)
 {
     for (const Arg& a : {args...}) {
         if (!a.p) {
             if (a.optional) continue;
             return false;
         }
-        if ((uintptr_t)a.p % (uintptr_t)a.align || !is_device_ptr(a.p)) return false;
+        if ((uintptr_t)a.p % (uintptr_t)a.align) return false;
+        const int owner = memory_of(a.p);
+        if (owner != device && owner != kManagedMemory) return false;
     }
     return true;
 }
 
-ckv_status check_workspace(const void* ws, int64_t have, int64_t need)
+ckv_status check_workspace(int device, const void* ws, int64_t have, int64_t need)
 {
-    return have < need || (need > 0 && !on_device(Arg{ws, 256})) ? CKV_ERR_INVALID_ARG : CKV_OK;
+    return have < need || (need > 0 && !on_device(device, Arg{ws, 256})) ? CKV_ERR_INVALID_ARG : CKV_OK;
 }
 
 ckv_status status_of(cudaError_t e)
@@ -89,8 +91,8 @@ ckv_status ckv_sort_indices(int32_t device, int32_t n, int32_t n_groups, int32_t
     if (st != CKV_OK) return st;
     DeviceGuard dg(device);
     if (!dg.ok) return CKV_ERR_CUDA;
-    if (!on_device(Arg{idx, 4, n == 0}, Arg{order, 4, n == 0}, Arg{offset, 4})) return CKV_ERR_INVALID_ARG;
-    st = check_workspace(workspace, workspace_bytes, sort_workspace(n, n_groups, n_entries));
+    if (!on_device(device, Arg{idx, 4, n == 0}, Arg{order, 4, n == 0}, Arg{offset, 4})) return CKV_ERR_INVALID_ARG;
+    st = check_workspace(device, workspace, workspace_bytes, sort_workspace(n, n_groups, n_entries));
     if (st != CKV_OK) return st;
     return status_of(launch_sort_indices(n, n_groups, n_entries, idx, order, offset, workspace, (cudaStream_t)stream));
 }
@@ -116,10 +118,10 @@ ckv_status ckv_route_loss(int32_t device, int32_t n, int32_t n_groups, int32_t d
     DeviceGuard dg(device);
     if (!dg.ok) return CKV_ERR_CUDA;
     const bool none = n == 0;
-    if (!on_device(Arg{x, 2, none}, Arg{W, 16}, Arg{bias, 4, true}, Arg{idx, 4, none}, Arg{loss, 4}, Arg{lse, 4, none},
+    if (!on_device(device, Arg{x, 2, none}, Arg{W, 16}, Arg{bias, 4, true}, Arg{idx, 4, none}, Arg{loss, 4}, Arg{lse, 4, none},
                    Arg{score, 4, none}, Arg{mean, 4}))
         return CKV_ERR_INVALID_ARG;
-    if (!on_device(Arg{workspace, 256})) return CKV_ERR_INVALID_ARG;
+    if (!on_device(device, Arg{workspace, 256})) return CKV_ERR_INVALID_ARG;
     const RouteLossArgs a{n, n_entries, n_groups, d_in, x, W, bias, idx, loss, lse, score, mean};
     return status_of(launch_route_loss(a, workspace, workspace_bytes, (cudaStream_t)stream));
 }
@@ -136,11 +138,11 @@ ckv_status ckv_route_loss_grad(int32_t device, int32_t n, int32_t n_groups, int3
     DeviceGuard dg(device);
     if (!dg.ok) return CKV_ERR_CUDA;
     const bool none = n == 0;
-    if (!on_device(Arg{x, 2, none}, Arg{W, 16}, Arg{bias, 4, true}, Arg{idx, 4, none}, Arg{order, 4, none}, Arg{offset, 4},
+    if (!on_device(device, Arg{x, 2, none}, Arg{W, 16}, Arg{bias, 4, true}, Arg{idx, 4, none}, Arg{order, 4, none}, Arg{offset, 4},
                    Arg{lse, 4, none}, Arg{score, 4, none}, Arg{mean, 4}, Arg{d_score, 4, true}, Arg{dx, 2, none}, Arg{dW, 2},
                    Arg{dbias, 4, true}))
         return CKV_ERR_INVALID_ARG;
-    if (!on_device(Arg{workspace, 256})) return CKV_ERR_INVALID_ARG;
+    if (!on_device(device, Arg{workspace, 256})) return CKV_ERR_INVALID_ARG;
     const RouteLossArgs a{n, n_entries, n_groups, d_in, x, W, bias, idx, nullptr, const_cast<float*>(lse), const_cast<float*>(score),
                           const_cast<float*>(mean)};
     const RouteGradArgs b{order, offset, balance_weight, peak_weight, d_score, dx, dW, dbias};
@@ -166,8 +168,8 @@ ckv_status ckv_gather(int32_t device, int32_t dtype, int32_t n, int32_t n_groups
     DeviceGuard dg(device);
     if (!dg.ok) return CKV_ERR_CUDA;
     const int e = dtype == CKV_F32 ? 4 : 2;
-    if (!on_device(Arg{pool, e}, Arg{idx, 4}, Arg{user, e, d_shared == head_dim}, Arg{score, 4, true}, Arg{out, e})) return CKV_ERR_INVALID_ARG;
-    st = check_workspace(workspace, workspace_bytes, gather_workspace(dtype, n, n_groups, head_dim, d_shared, n_entries));
+    if (!on_device(device, Arg{pool, e}, Arg{idx, 4}, Arg{user, e, d_shared == head_dim}, Arg{score, 4, true}, Arg{out, e})) return CKV_ERR_INVALID_ARG;
+    st = check_workspace(device, workspace, workspace_bytes, gather_workspace(dtype, n, n_groups, head_dim, d_shared, n_entries));
     if (st != CKV_OK) return st;
     return status_of(launch_gather(dtype, n, n_groups, head_dim, d_shared, n_entries, pool, idx, user, score, out, workspace, (cudaStream_t)stream));
 }
@@ -191,11 +193,11 @@ ckv_status ckv_gather_grad(int32_t device, int32_t dtype, int32_t n, int32_t n_g
     if (!dg.ok) return CKV_ERR_CUDA;
     const int e = dtype == CKV_F32 ? 4 : 2;
     const bool none = n == 0;
-    if (!on_device(Arg{pool, e, !score}, Arg{order, 4, none}, Arg{offset, 4}, Arg{score, 4, true}, Arg{d_out, 16, none}, Arg{d_pool, 4},
+    if (!on_device(device, Arg{pool, e, !score}, Arg{order, 4, none}, Arg{offset, 4}, Arg{score, 4, true}, Arg{d_out, 16, none}, Arg{d_pool, 4},
                    Arg{d_user, e, true}, Arg{d_score, 4, none || !score}) ||
         (d_score && !score))
         return CKV_ERR_INVALID_ARG;
-    st = check_workspace(workspace, workspace_bytes, segment_workspace(n, n_groups, head_dim));
+    st = check_workspace(device, workspace, workspace_bytes, segment_workspace(n, n_groups, head_dim));
     if (st != CKV_OK) return st;
     SegmentArgs a{};
     a.order = order;

@@ -7,6 +7,7 @@ import threading
 
 import pytest
 
+from test_fit import OPTIONAL, REQUIRED, _calls
 from test_host_side import ROOT, device_block, objects  # noqa: F401
 
 
@@ -18,8 +19,8 @@ def _stand_in(objects, tmp, source):
 
 
 @pytest.fixture(scope="module")
-def lib_smem(objects, tmp_path_factory):
-    return _stand_in(objects, tmp_path_factory.mktemp("smem"), "fake_smem.cpp")
+def lib2(objects, tmp_path_factory):
+    return _stand_in(objects, tmp_path_factory.mktemp("fit"), "fake_fit.cpp")
 
 
 def _in_a_thread(work):
@@ -32,9 +33,9 @@ def _in_a_thread(work):
 
 
 @pytest.mark.parametrize("n,large,small", [(5000, 20000, 13000), (9000, 24000, 14000)])
-def test_a_sort_leaves_other_threads_their_shared_memory(lib_smem, n, large, small):
+def test_a_sort_leaves_other_threads_their_shared_memory(lib2, n, large, small):
     """A thread's first sort, while another thread's first one, with fewer entries, runs between its permission and its launch."""
-    lib = lib_smem
+    lib = lib2
     need, other = C.c_int64(), C.c_int64()
     assert lib.ckv_sort_indices_bytes(n, 2, large, C.byref(need)) == lib.ckv_sort_indices_bytes(n, 2, small, C.byref(other)) == 0
     need.value = max(need.value, other.value)
@@ -64,3 +65,21 @@ def test_lanes_that_share_a_counter_read_it_before_it_moves_on():
         read = max(m.start() for m in re.finditer(r"(= next\[d\]|volatile unsigned long long\*>\(slots \+ d\);)", body))
         write = re.search(r"next\[d\] = |slots \+ d\) = ", body).start()
         assert "__syncwarp();" in body[read:write], body
+
+
+@pytest.mark.parametrize("name", list(REQUIRED))
+def test_arrays_of_another_device_are_refused(lib2, name):
+    """Every array has to lie on the call's device, or in managed memory."""
+    lib = lib2
+    d, w, calls = _calls(lib)
+    fn, args = calls[name]
+    managed, far = device_block(lib, 1 << 20), device_block(lib, 1 << 20)
+    assert managed.value % 256 == far.value % 256 == 0
+    lib.fake_block_of(managed, -1)
+    lib.fake_block_of(far, 1)
+    workspace = {"loss": 13, "grad": 20}.get(name)
+    for at in (*REQUIRED[name], *OPTIONAL.get(name, ())):
+        assert fn(*args[:at], managed, *args[at + 1:]) == 0, at
+        assert fn(*args[:at], far, *args[at + 1:]) == 1, at
+        if at != workspace:
+            assert fn(1, *args[1:at], far, *args[at + 1:]) == 1, at      # (and the others on device 0)
