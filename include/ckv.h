@@ -322,7 +322,9 @@ CKV_API ckv_status ckv_sort_indices(int32_t device, int32_t n, int32_t n_groups,
  * x bf16 [n][d_in], W bf16 [n_groups][n_entries][d_in], bias fp32 [n_groups][n_entries] or NULL, d_in in {32, 64, 128}.
  * Products are exact, sums fp32 (the losses' fp64).  A group without rows has zeros.  A bias of -2^20 or less (-inf, a type's
  * lowest value) takes an entry out, whose row of W still has to be finite: it counts as -inf, but for `score`, which adds
- * it as it is.  A position whose entries are all out has lse -inf and adds to no p_j.
+ * it as it is.  A position whose entries are all out has lse -inf and adds to no p_j.  Large biases are scores of that size: an fp32
+ * score of 10^6 is a multiple of 1/16, and so is lse, so that a weight exp(M - lse) is off by as much; an entry that outweighs the
+ * others by its bias, of whatever finite size, has the weight one.
  */
 CKV_API ckv_status ckv_route_loss_bytes(int32_t n, int32_t n_groups, int32_t d_in, int32_t n_entries, int64_t* forward,
                                         int64_t* grad);

@@ -109,15 +109,21 @@ inline int64_t sweep_blocks(int64_t rows) { return sweep_padded(rows) / kSweepPa
 // tickets of a pass
 int64_t sweep_tickets(int64_t n, int G, int d, int64_t m, int mode);
 #ifdef __CUDACC__
-// A number as three bf16 parts whose sum it is (16 elements per row: 8 rows of 16 bytes, of which the first six hold the parts, then
-// the rows' zero halves), as a K-major operand without swizzle wants it.
-__device__ __forceinline__ void put_step(uint16_t* step, int64_t row, float v)
+// A number as three bf16 parts whose sum it is.
+__device__ __forceinline__ uint2 bf16_parts(float v)
 {
     const uint32_t hi = (__float_as_uint(v) & 0xffff0000u) | (v != v ? 0x400000u : 0u);  // (a NaN whose upper half alone would be an infinity)
     const float r1 = isfinite(v) ? v - __uint_as_float(hi) : 0.f;
     const uint32_t mid = __float_as_uint(r1) & 0xffff0000u, lo = __float_as_uint(r1 - __uint_as_float(mid));
+    return make_uint2((hi >> 16) | mid, lo >> 16);
+}
+// Those parts as a row of a K-major operand without swizzle (16 elements per row: 8 rows of 16 bytes, of which the first six hold the parts,
+// then the rows' zero halves).
+__device__ __forceinline__ void put_step(uint16_t* step, int64_t row, float v)
+{
+    const uint2 parts = bf16_parts(v);
     uint4* const to = reinterpret_cast<uint4*>(step) + (row >> 3) * 16 + (row & 7);
-    to[0] = make_uint4((hi >> 16) | mid, lo >> 16, 0, 0);
+    to[0] = make_uint4(parts.x, parts.y, 0, 0);
     to[8] = make_uint4(0, 0, 0, 0);
 }
 #endif

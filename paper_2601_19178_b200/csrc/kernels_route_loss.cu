@@ -85,8 +85,7 @@ Space layout(void* ws, int64_t n, int G, int d, int64_t m, bool grad)
     return s;
 }
 
-// A bias of this or less takes its entry out, as masks by a type's lowest value want it.  The passes' exponents are s log2(e) - c with c
-// rounded once: at scores of 2^20 it is off by a twentieth, as the scores themselves are, at 2^31 by more than an exponential's range.
+// A bias of this or less takes its entry out, as masks by a type's lowest value want it, also where it is all entries' bias.
 constexpr float kTakenOut = -1048576.f;
 
 // ---- what the passes read

@@ -4,7 +4,9 @@
 // through a ring of shared-memory stages, as B operand (a swizzled TMA box per 64 inputs).  What a streaming row adds to all its
 // scores (an entry's bias, a position's -lse) comes in with the product, as one more step of K = 16: ones times the number
 // cut into three bf16 parts, whose sum is the fp32 number exactly.  (Read beside the scores it cost a thread one 16-byte
-// load of shared memory per four columns, whose 512 bytes take the data path four clocks, and an addition.)  A tile of
+// load of shared memory per four columns, whose 512 bytes take the data path four clocks, and an addition.)  A standing row's number comes
+// in the same way, by a step of its own, its parts times ones: first the bias, so that every pass has the same bits for x W + b however large b
+// is, then -lse.  A tile of
 // scores appears in TMEM, its thread reads its row of it, and:
 //   sweep_kernel (LSE, MEAN, R)  keeps a running sum.  Three blocks per CTA, two accumulators of 64 columns each (one of 96 at d_in = 128).
 //   grad_kernel (DX, DW)         turns it into weights T (bf16, over the head of the scores they came from), which multiply the
@@ -153,6 +155,19 @@ __device__ __forceinline__ void store_ones(uint32_t taddr)
     const uint32_t ones[8] = {0x3f803f80u, 0x00003f80u, 0, 0, 0, 0, 0, 0};
     st8(taddr, ones);
 }
+// And of the one that adds a standing row's, whose B operand are `rows` rows of ones in shared memory, which the whole block writes.
+__device__ __forceinline__ void store_parts(uint32_t taddr, float v)
+{
+    const uint2 parts = bf16_parts(v);
+    const uint32_t w[8] = {parts.x, parts.y, 0, 0, 0, 0, 0, 0};
+    st8(taddr, w);
+}
+__device__ __forceinline__ void put_ones(unsigned char* to, int rows)
+{
+    for (int k = threadIdx.x; k < 2 * rows; k += blockDim.x)  // groups of eight rows: their first halves, their second ones
+        reinterpret_cast<uint4*>(to)[k] = k & 8 ? make_uint4(0, 0, 0, 0) : make_uint4(0x3f803f80u, 0x00003f80u, 0, 0);
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+}
 __device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void expect_bytes(uint32_t bar, uint32_t bytes)
 {
@@ -246,6 +261,21 @@ __device__ __forceinline__ F2 weight(F2 u, bool fma)
     const Exp2<DW ? 4 : 3> p(u);
     return mul2(p.p, p.scale);
 }
+
+// The exponent of a weight is s log2(e) - c with c = lse log2(e) rounded once, which is off by as much as lse is as an fp32 number: at 10^7 a weight by a
+// seventh, at 10^10 by its whole range.  MEAN, R and DW have the difference s - lse from the tensor core, where it is exact if small.  LSE, whose c is top
+// log2(e), takes its residue top log2(e) - c, which one fused operation gives exactly, out of the sum.  DX takes the difference first where lse is far from zero: a branch per 32 scores, which few rows take.
+constexpr float kFar = 1024.f;
+__device__ __forceinline__ bool is_far(float reference) { return fabsf(reference) > kFar && reference > -CUDART_INF_F; }
+__device__ __forceinline__ void move(uint32_t (&v)[32], float by)
+{
+#pragma unroll
+    for (int q = 0; q < 32; ++q) v[q] = __float_as_uint(__uint_as_float(v[q]) + by);
+}
+// (Residues of references that were given up differ by no more than such scores' own rounding; with f = 2^(c - c before), which keeps them alike,
+// the pass took 519 us instead of 509.)  From this `top` on, where the residue would be more than 32, lse is `top`: numbers lie 64 apart, which no
+// count of equal scores moves.
+constexpr float kCoarse = 536870912.f;
 
 // A sum of many parts: what an addition loses is added with the next part.
 struct LongSum {
@@ -428,12 +458,12 @@ struct Sweep {
     static constexpr int BOXES = DIN == 128 ? 2 : 1;
     static constexpr int BOX = TN * ROWB, TILE = BOXES * BOX;
     static constexpr int OFF_STEP = kStages * TILE, STEP = TN * 32, OFF_NUM = OFF_STEP + kStages * STEP, NUM = TN * 4,
-                         OFF_BAR = OFF_NUM + kStages * NUM;
+                         OFF_ONES = OFF_NUM + kStages * NUM, OFF_BAR = OFF_ONES + AN * 32;
     enum { FULL = 0, EMPTY = kStages, AFULL = 2 * kStages, AFREE = AFULL + kBlocks * ACCS, DRAIN = AFREE + kBlocks * ACCS, COUNT };
     static constexpr int OFF_ABORT = OFF_BAR + COUNT * 8, SMEM = OFF_ABORT + 16;
-    static_assert(SMEM <= 226 * 1024 && BOX % 1024 == 0, "shared memory");
-    static constexpr uint32_t COL_A = kBlocks * TN, COL_ONES = COL_A + kBlocks * (DIN / 2);
-    static_assert(COL_ONES + 8 <= 512, "TMEM columns");
+    static_assert(SMEM <= 226 * 1024 && BOX % 1024 == 0 && OFF_ONES % 16 == 0 && OFF_BAR % 8 == 0, "shared memory");
+    static constexpr uint32_t COL_A = kBlocks * TN, COL_ONES = COL_A + kBlocks * (DIN / 2), COL_OWN = COL_ONES + 8;  // (8 of each block)
+    static_assert(COL_OWN + 8 * kBlocks <= 512, "TMEM columns");
     static_assert(kSweepPad % TN == 0, "numbers are copied a tile at a time");
 };
 
@@ -474,6 +504,7 @@ __global__ void __launch_bounds__(kSweepThreads, 1) sweep_kernel(const __grid_co
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    if (MODE != SWEEP_LSE) put_ones(sm + L::OFF_ONES, AN);
     if (warp == kIssueWarp) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -485,6 +516,7 @@ __global__ void __launch_bounds__(kSweepThreads, 1) sweep_kernel(const __grid_co
     const uint32_t tmem = tmem_slot;
     if (warp < 4 * n_blocks) {
         if (e == 0) store_ones(tmem + lane_base + L::COL_ONES);
+        if (MODE != SWEEP_LSE) store_parts(tmem + lane_base + L::COL_OWN + 8 * e, !in ? 0.f : kEntriesStand ? a.b[grp * a.mp + row] : a.nl[grp * a.np + row]);
         load_inputs<DIN>(tmem + lane_base + L::COL_A + e * (DIN / 2), (kEntriesStand ? a.W + ((int64_t)grp * a.m + row) * DIN : a.x + row * DIN), in);
     }
     if (warp < kLoadWarp) {  // (the loading warp is on its way)
@@ -497,8 +529,7 @@ __global__ void __launch_bounds__(kSweepThreads, 1) sweep_kernel(const __grid_co
     float top = -CUDART_INF_F;
     if (warp < kReadWarps) {
         // ------------------------------------------------------------ thread = standing row
-        // log2 of a weight is  s log2(e) + own
-        float own = !in || MODE == SWEEP_LSE ? 0.f : (kEntriesStand ? a.b[grp * a.mp + row] : a.nl[grp * a.np + row]) * kLog2e;
+        float c = 0.f;  // LSE: log2 of a weight is  s log2(e) + c
         const uint32_t tacc = tmem + lane_base + (uint32_t)(TN * e);
         auto look = [&](uint32_t (&x)[32], const float4* num) {
             F2 u[16];
@@ -515,11 +546,11 @@ __global__ void __launch_bounds__(kSweepThreads, 1) sweep_kernel(const __grid_co
                     sum.s *= f;
                     sum.lost *= f;
                     top = m0;
-                    own = -m0 * kLog2e;
+                    c = -m0 * kLog2e;
                 }
             }
 #pragma unroll
-            for (int q = 0; q < 16; ++q) u[q] = fma2(pair(x, 2 * q), both(kLog2e), both(own));
+            for (int q = 0; q < 16; ++q) u[q] = MODE == SWEEP_LSE ? fma2(pair(x, 2 * q), both(kLog2e), both(c)) : mul2(pair(x, 2 * q), both(kLog2e));
             F2 part{0.f, 0.f};
 #pragma unroll
             for (int q = 0; q < 16; ++q) {
@@ -567,6 +598,7 @@ __global__ void __launch_bounds__(kSweepThreads, 1) sweep_kernel(const __grid_co
                 if (++s == kStages) s = 0;
             }
         }
+        if (MODE == SWEEP_LSE && top > -CUDART_INF_F) sum.s = fabsf(top) < kCoarse ? sum.s * ex2(-fmaf(top, kLog2e, c)) : 1.f;
     } else if (warp < kIssueWarp + kBlocks) {
         // ------------------------------------------------------------ products, one warp per block
         constexpr uint32_t idesc = idesc_bf16(128, AN, false);
@@ -586,7 +618,11 @@ __global__ void __launch_bounds__(kSweepThreads, 1) sweep_kernel(const __grid_co
 #pragma unroll
                     for (int ks = 0; ks < DIN / 16; ++ks)
                         mma_ts(d + AN * h, at + 8 * ks, w + (uint64_t)(((ks & 3) * 32 + (ks >> 2) * L::BOX) >> 4), idesc, ks > 0);
-                    mma_ts(d + AN * h, tmem + L::COL_ONES, step_desc(sb + L::OFF_STEP + s * L::STEP + AN * h * 32), idesc, 1u);
+                    const uint64_t ones = step_desc(sb + L::OFF_ONES), step = step_desc(sb + L::OFF_STEP + s * L::STEP + AN * h * 32);
+                    const uint32_t own = tmem + L::COL_OWN + 8 * blk;
+                    if (MODE == SWEEP_MEAN) mma_ts(d + AN * h, own, ones, idesc, 1u);  // (the bias first)
+                    mma_ts(d + AN * h, tmem + L::COL_ONES, step, idesc, 1u);
+                    if (MODE == SWEEP_R) mma_ts(d + AN * h, own, ones, idesc, 1u);
                     tc_commit_to(bar(L::AFULL + ACCS * blk + h));
                     if (h == ACCS - 1) tc_commit_to(bar(L::EMPTY + s));
                 }
@@ -662,13 +698,13 @@ struct Grad {
     static constexpr int BOX = TN * ROWB, TILE = BOXES * BOX, STAGES = 8;
     static constexpr int ON = DIN < 64 ? DIN : 64;     // columns of O that one product covers: a box
     static constexpr int OFF_STEP = STAGES * TILE, STEP = TN * 32, OFF_NUM = OFF_STEP + STAGES * STEP, NUM = TN * 4, OFF_SUM = OFF_NUM + STAGES * NUM,
-                         OFF_BAR = OFF_SUM + BLOCKS * 128 * 4;
+                         OFF_ONES = OFF_SUM + BLOCKS * 128 * 4, OFF_BAR = OFF_ONES + TN * 32;
     enum { FULL = 0, EMPTY = STAGES, SFULL = 2 * STAGES, OFULL = SFULL + 2 * BLOCKS, COUNT = OFULL + BLOCKS };
     static constexpr int OFF_ABORT = OFF_BAR + COUNT * 8, SMEM = OFF_ABORT + 16;
-    static_assert(SMEM <= 226 * 1024 && BOX % 1024 == 0, "shared memory");
+    static_assert(SMEM <= 226 * 1024 && BOX % 1024 == 0 && OFF_ONES % 16 == 0 && OFF_BAR % 8 == 0, "shared memory");
     static constexpr uint32_t COL_O = 2 * TN, COL_A = COL_O + DIN, COL_BLOCK = COL_A + DIN / 2,  // a block's: two buffers, O, inputs
-                              COL_ONES = BLOCKS * COL_BLOCK;
-    static_assert(COL_ONES + 8 <= 512, "TMEM columns");
+                              COL_ONES = BLOCKS * COL_BLOCK, COL_OWN = COL_ONES + 8;  // (8 of each block)
+    static_assert(COL_OWN + 8 * BLOCKS <= 512, "TMEM columns");
     static_assert(kSweepPad % TN == 0, "numbers are copied a tile at a time");
 };
 
@@ -710,6 +746,7 @@ __device__ __forceinline__ void grad_block(const CUtensorMap& map, const SweepAr
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    if (kEntriesStand) put_ones(sm + L::OFF_ONES, TN);
     if (warp == L::ISSUE_WARP) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -720,8 +757,10 @@ __device__ __forceinline__ void grad_block(const CUtensorMap& map, const SweepAr
     grid_dependency_wait();
     const uint32_t tmem = tmem_slot, tblock = tmem + (uint32_t)e * L::COL_BLOCK;
     if (warp < 4) store_ones(tmem + lane_base + L::COL_ONES);
-    if (warp < 8 * n_blocks && buf == 0)
+    if (warp < 8 * n_blocks && buf == 0) {
+        if (kEntriesStand) store_parts(tmem + lane_base + L::COL_OWN + 8 * e, in ? a.b[of_group * a.mp + row] : 0.f);
         load_inputs<DIN>(tblock + lane_base + L::COL_A, (kEntriesStand ? a.W + ((int64_t)of_group * a.m + row) * DIN : a.x + row * DIN), in);
+    }
     if (warp < L::LOAD_WARP) {  // (the loading warp is on its way)
         tc_before();
         asm volatile("bar.sync 1, %0;" ::"n"(L::LOAD_WARP * 32) : "memory");
@@ -732,13 +771,16 @@ __device__ __forceinline__ void grad_block(const CUtensorMap& map, const SweepAr
     if (warp < L::READ_WARPS) {
         // ------------------------------------------------------------ weights, thread = standing row, every second tile
         int g = first_group, in_group = first_tile;
-        auto own0 = [&] { return !in ? -CUDART_INF_F : (kEntriesStand ? a.b[g * a.mp + row] : a.nl[g * a.np + row]) * kLog2e; };
-        auto own1 = [&] { return !in ? 0.f : kEntriesStand ? a.h[g * a.mp + row] : a.nr[g * a.np + row]; };
-        float log_own = 0.f, h_own = 0.f;
-        if (n_tiles > 0) {
-            log_own = own0();
-            h_own = own1();
-        }
+        // log2 of a weight is  (s + by) log2(e) + log_own, of which one is zero
+        float by = 0.f, log_own = 0.f, h_own = 0.f;
+        bool far = false;
+        auto take_own = [&] {
+            h_own = !in ? 0.f : kEntriesStand ? a.h[g * a.mp + row] : a.nr[g * a.np + row];
+            by = !in ? -CUDART_INF_F : kEntriesStand ? 0.f : a.nl[g * a.np + row];
+            far = is_far(by);
+            log_own = far ? 0.f : by * kLog2e;
+        };
+        if (n_tiles > 0) take_own();
         const uint32_t ts = tblock + lane_base + (uint32_t)(TN * buf);
         if (buf == 1) ++in_group;
         bool ok = true;
@@ -748,8 +790,7 @@ __device__ __forceinline__ void grad_block(const CUtensorMap& map, const SweepAr
                     in_group -= per_group;
                     ++g;
                 } while (in_group >= per_group);
-                log_own = own0();
-                h_own = own1();
+                take_own();
             }
             const int s = t % L::STAGES;
             ok = ok && bar_wait(bar(L::SFULL + 2 * e + buf), (t >> 1) & 1, abort_flag);
@@ -765,6 +806,7 @@ __device__ __forceinline__ void grad_block(const CUtensorMap& map, const SweepAr
                 uint32_t v[32], w[16];
                 ld32(ts + 32 * c, v);
                 wait_ld32(v);
+                if (!kEntriesStand && far) move(v, by);
                 const float4* n1 = reinterpret_cast<const float4*>(num + 32 * c);
                 F2 part{0.f, 0.f};
 #pragma unroll
@@ -817,6 +859,7 @@ __device__ __forceinline__ void grad_block(const CUtensorMap& map, const SweepAr
 #pragma unroll
                 for (int ks = 0; ks < DIN / 16; ++ks)
                     mma_ts(tb + (uint32_t)(TN * (nxt & 1)), tb + L::COL_A + 8 * ks, w + (uint64_t)(((ks & 3) * 32 + (ks >> 2) * L::BOX) >> 4), idesc_s, ks > 0);
+                if (kEntriesStand) mma_ts(tb + (uint32_t)(TN * (nxt & 1)), tmem + L::COL_OWN + 8 * blk, step_desc(sb + L::OFF_ONES), idesc_s, 1u);
                 mma_ts(tb + (uint32_t)(TN * (nxt & 1)), tmem + L::COL_ONES, step_desc(sb + L::OFF_STEP + (nxt % L::STAGES) * L::STEP), idesc_s, 1u);
                 tc_commit_to(bar(L::SFULL + 2 * blk + (nxt & 1)));
             }

@@ -1,0 +1,77 @@
+"""Inputs of the training-side calls at the edges of what their documentation allows, against the oracle.
+
+Tolerances as in test_fit.py: a rounding to fp32 is off by 2^-24 of the value, to bf16 by 2^-8; S is the size of a score.
+"""
+import numpy as np
+import pytest
+
+from oracle import fit_oracle as F
+from test_fit import _check_grad, _close, _dev, _host, _loss_case, _router
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("d", [32, 64, 128])
+@pytest.mark.parametrize("high", [1e5, 1e6, 1e7, 1e9, 1e10, 1e30, 3e38])
+def test_an_entry_forced_in_by_its_bias_takes_all_weight(d, high):
+    """One entry's bias outweighs all others': its softmax weight is one.  A score rounded to fp32 less itself is zero, whose exponential is off
+    by 1.6e-7 at most (the passes' polynomial), and a mean of such weights by two roundings more."""
+    import paper_2601_19178_b200 as ckv
+    n, m, G = 500, 700, 3
+    x, W, b, idx = _router(21, n, m, G, d, pad=0.1)
+    at = [0, 130, 699]
+    for g in range(G):
+        b[g, at[g]] = high
+    idx[idx[:, 0] >= 0, 0] = at[0]
+    real = idx >= 0
+    rows = real.sum(0)
+    got = [_host(t) for t in _loss_case(x, W, b, idx)]
+    one = 1.6e-7 + 2 * 2.0 ** -23
+    want = F.route_loss(x, W, b, idx)
+    assert np.isfinite(got[1]).all()
+    _close(got[1], want[1], (d + 2) * 2.0 ** -23 * np.abs(want[1]), "lse")
+    others = np.ones((G, m), bool)
+    for g in range(G):
+        _close(got[3][g, at[g]], 1.0, one, "mean")
+        others[g, at[g]] = False
+    assert not got[3][others].any()
+    _close(got[0][:, 0], np.log(m), one * (1 + np.log(m)) + 2.0 ** -23 * np.log(m), "balance")
+    # the gradient: T vanishes, the picked entries' terms stay
+    w_peak = 0.5
+    d_score = (np.random.default_rng(1).standard_normal((n, G)) / n).astype(np.float32)
+    f32 = [v.astype(np.float32) for v in got[1:]]
+    order = ckv.sort_indices(_dev(idx), m)
+    grads = ckv.route_loss_grad(_dev(x), _dev(W), _dev(b), _dev(idx), order, *[_dev(v) for v in f32], 1.0, w_peak, _dev(d_score))
+    dx, dW, db, size = F.route_loss_grad(x, W, b, idx, want[3], 1.0, w_peak, d_score.astype(np.float64))
+    # what the picked entries' coefficients are made of, before it cancels: the sigmoid is off by 2^-21 and by a quarter of its score's error
+    whole = F.route_loss_grad(x, W, b, idx, want[3], 0.0, -w_peak, np.abs(d_score).astype(np.float64))[3]
+    es = (d + 2) * 2.0 ** -23 * np.abs(F.f64(x)[:, None, None, :] * F.f64(W)[None, :, ::7]).sum(3).max() * 2
+    X, Wf = np.abs(F.f64(x)), np.abs(F.f64(W))
+    # |T| of the forced entry: |p (h - r)| with p and sum p h off by 1e-4 (the polynomial of degree 3) at most
+    T = 4 * 1e-4 * np.log(m) / rows
+    left = {"dx": sum(real[:, g, None] * T[g] * Wf[g, at[g]][None] for g in range(G)), "dW": np.zeros((G, m, d)), "db": np.zeros((G, m))}
+    for g in range(G):
+        left["dW"][g, at[g]] = T[g] * X[real[:, g]].sum(0)
+        left["db"][g, at[g]] = T[g] * rows[g]
+    for name, g, w in (("dx", grads[0], dx), ("dW", grads[1], dW), ("db", grads[2], db)):
+        half = 2.0 ** -8 if name != "db" else 0
+        _close(_host(g), w, left[name] * (1 + 2 * half) + half * np.abs(w) + (2.0 ** -18 + es / 4) * whole[name][2] + 1e-37, name)
+
+
+@pytest.mark.parametrize("d", [32, 64, 128])
+@pytest.mark.parametrize("shift", [2000.0, 1e5, -1e5, -1e6])
+def test_a_shift_of_all_biases_changes_only_their_rounding(d, shift):
+    """Scores of size S are off by 2^-23 S for each of the bias' three parts and of their own rounding, lse by one rounding more, and a weight
+    by both."""
+    n, m, G = 300, 500, 2
+    x, W, b, idx = _router(22, n, m, G, d, pad=0.1)
+    b = (b + np.float32(shift)).astype(np.float32)
+    got = [_host(t) for t in _loss_case(x, W, b, idx)]
+    want = F.route_loss(x, W, b, idx)
+    S = np.abs(want[1]).max()
+    es = 4 * 2.0 ** -23 * S + (d + 2) * 2.0 ** -23 * np.abs(F.scores(x, W, None, 0)).max() * 8
+    assert np.isfinite(got[1]).all()
+    _close(got[1], want[1], es + 2.0 ** -23 * S + 2.0 ** -21, "lse")
+    e = np.expm1(2 * es + 2.0 ** -23 * S + 2.0 ** -19)
+    _close(got[3], want[3], e * want[3] + 1e-37, "mean")
+    _check_grad(x, W, b, idx, what=f"shift {shift}")
