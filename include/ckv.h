@@ -294,7 +294,8 @@ CKV_API ckv_status ckv_project(int32_t device, int32_t n, int32_t n_groups, int3
  *     ckv_route -> ckv_route_loss -> ckv_gather -> (the model) -> ckv_sort_indices -> ckv_gather_grad -> ckv_route_loss_grad
  * and the pool goes back into service with ckv_pool_load.  They need no context, allocate nothing, are stream-ordered and can
  * be captured into a graph.  `idx` is what ckv_route writes, int32 [n][n_groups]; an index outside [0, n_entries) marks a
- * position without an entry (padding): it takes no part in the losses and gradients of its group, whatever its inputs hold.
+ * position without an entry (padding): it takes no part in the losses and gradients of its group, whatever its inputs hold.  (Inputs
+ * that are not finite make NaN in the groups that the position takes part in, and in its row of dx.)
  * Results are the same bits from call to call.  Array arguments are device memory of `device` (or managed), aligned to
  * their elements, W and d_out to 16 bytes.  `workspace` is device memory on a 256-byte boundary of at least the size that the _bytes
  * function of the call gives (NULL where that is 0), of any contents; calls that may overlap on the GPU, captured graphs among them, need one each.

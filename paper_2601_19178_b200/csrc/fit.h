@@ -98,7 +98,7 @@ struct SweepArgs {
     // LSE, MEAN: indices, scores, results; per block of kSweepPad positions and group the positions that take part, those of them that have
     // a weight (scores that are not all -inf) and the sum of -log sigmoid(score); per block of as many entries the balance loss's part
     const int32_t* idx;
-    const float* score;
+    const float *score, *spoilt;  // spoilt [n]: NaN where lse is to be that, else 0
     float *lse, *mean, *loss;
     int32_t *rows_part, *live_part;
     double *peak_part, *balance_part;

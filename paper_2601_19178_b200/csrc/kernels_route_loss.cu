@@ -34,7 +34,8 @@ struct Space {
     // by position, [G][np]: -lse, -inf for a position that takes no part; -r
     float *nl, *nr;
     uint16_t *b_step, *nl_step;  // b and nl as operands of a product
-    uint16_t* xs;        // x with zeros for a position that takes part in no group
+    uint16_t* xs;        // x with zeros for a position that takes part in no group, see prepare_kernel
+    float* spoilt;       // forward, by position: NaN where its inputs are not numbers and are zeros in xs, else 0
     float* part;         // partial results of a pass
     float *part_dw, *part2;
     int32_t *rows_part, *live_part;  // forward, see SweepArgs
@@ -65,6 +66,7 @@ Space layout(void* ws, int64_t n, int G, int d, int64_t m, bool grad)
     s.nl_step = c.take<uint16_t>(G * np * 16);
     s.xs = c.take<uint16_t>(n * d);
     if (!grad) {
+        s.spoilt = c.take<float>(n);
         s.rows_part = c.take<int32_t>(sweep_blocks(n) * G);
         s.live_part = c.take<int32_t>(sweep_blocks(n) * G);
         s.peak_part = c.take<double>(sweep_blocks(n) * G);
@@ -103,7 +105,8 @@ __device__ __forceinline__ void prepare_entry(const RouteLossArgs& a, const Rout
     s.h[g * mp + j] = u > 0.f ? b.w_balance / (float)max(rows, 1) * logf(u) : 0.f;
 }
 
-// Positions: x for the passes (zeros for one that takes part in no group, whose inputs may be anything); forward: the picked entry's
+// Positions: x for the passes (zeros for one that takes part in no group, whose inputs may be anything; also for one that takes part in some groups
+// and not in others if its inputs are not finite: they spoil the former by its lse, which is not a number, and not the latter); forward: the picked entry's
 // score (rows of W by index, 32768 positions x 4 groups x 128 bytes 22 us: latency); gradient: -lse and the picked entry's coefficient (13 us).  A position to D / 8 lanes, 16 bytes of it to each.  The first
 // `entry_blocks` blocks, as many for each group, prepare the entries instead.
 template <int D, bool GRAD>
@@ -133,14 +136,25 @@ __global__ void __launch_bounds__(256) prepare_kernel(const RouteLossArgs a, con
         }
     }
     const uint32_t xw[4] = {raw.x, raw.y, raw.z, raw.w};
-    int any = 0;
+    // what all lanes of the position have found: bit 0, it takes part in a group; 1, not in another one; 2, inputs that are not finite
+    int found = 0;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) found |= (xw[q] & 0x7f80u) == 0x7f80u || (xw[q] & 0x7f800000u) == 0x7f800000u ? 4 : 0;
+    auto share = [&] {
+#pragma unroll
+        for (int d = LANES / 2; d > 0; d /= 2) found |= __shfl_xor_sync(0xffffffffu, found, d);
+    };
     if (GRAD) {
         for (int g = sub; g < a.G; g += LANES) {
             const int32_t k = there ? ld(a.idx + i * a.G + g) : -1;
+            found |= k >= 0 && k < a.m ? 1 : 2;
+        }
+        share();
+        for (int g = sub; g < a.G; g += LANES) {
+            const int32_t k = there ? ld(a.idx + i * a.G + g) : -1;
             const bool real = k >= 0 && k < a.m;
-            any |= real;
             if (i < np) {
-                const float lse = real ? ld(a.lse + i * a.G + g) : -CUDART_INF_F;
+                const float lse = !real ? -CUDART_INF_F : found == 7 ? CUDART_NAN_F : ld(a.lse + i * a.G + g);
                 const float nl = lse == -CUDART_INF_F ? lse : -lse;
                 s.nl[g * np + i] = nl;
                 put_step(s.nl_step, g * np + i, nl);
@@ -155,14 +169,12 @@ __global__ void __launch_bounds__(256) prepare_kernel(const RouteLossArgs a, con
                 s.ds[i * a.G + g] = v;
             }
         }
-#pragma unroll
-        for (int d = LANES / 2; d > 0; d /= 2) any |= __shfl_xor_sync(0xffffffffu, any, d);
     } else {
 #pragma unroll 2
         for (int g = 0; g < a.G; ++g) {
             const int32_t k = there ? ld(a.idx + i * a.G + g) : -1;
             const bool real = k >= 0 && k < a.m;
-            any |= real;
+            found |= real ? 1 : 2;
             float sc = 0.f;
             if (real) {
                 const uint4 w = ld(reinterpret_cast<const uint4*>((const uint16_t*)a.W + ((int64_t)g * a.m + k) * D) + sub);
@@ -177,8 +189,10 @@ __global__ void __launch_bounds__(256) prepare_kernel(const RouteLossArgs a, con
             for (int d = LANES / 2; d > 0; d /= 2) sc += __shfl_xor_sync(0xffffffffu, sc, d);
             if (sub == 0 && there) a.score[i * a.G + g] = real && a.bias ? sc + ld(a.bias + (int64_t)g * a.m + k) : sc;
         }
+        share();
+        if (sub == 0 && there) s.spoilt[i] = found == 7 ? CUDART_NAN_F : 0.f;
     }
-    if (there) reinterpret_cast<uint4*>(s.xs + i * D)[sub] = any ? raw : make_uint4(0, 0, 0, 0);
+    if (there) reinterpret_cast<uint4*>(s.xs + i * D)[sub] = (found & 1) && found != 7 ? raw : make_uint4(0, 0, 0, 0);
 }
 
 // ---- joins
@@ -261,6 +275,7 @@ SweepArgs pass_args(const RouteLossArgs& a, const Space& s)
     p.x = s.xs, p.W = (const uint16_t*)a.W;
     p.b = s.b, p.h = s.h, p.nl = s.nl, p.nr = s.nr, p.b_step = s.b_step, p.nl_step = s.nl_step;
     p.part = s.part, p.part_dw = s.part_dw, p.part2 = s.part2;
+    p.spoilt = s.spoilt;
     p.idx = a.idx, p.score = a.score, p.lse = a.lse, p.mean = a.mean, p.loss = a.loss;
     p.rows_part = s.rows_part, p.live_part = s.live_part, p.peak_part = s.peak_part, p.balance_part = s.balance_part;
     p.ds = s.ds, p.sum = s.sum, p.wsum = s.wsum;

@@ -342,10 +342,11 @@ __device__ __forceinline__ void join_lse(const SweepArgs& a, int g, int64_t row0
         for (int z = 0; z < a.splits; ++z) {
             const float2 v = __ldcg(part + z * step);
             const float both = fmaxf(top, v.x);
-            if (both > -CUDART_INF_F) sum = sum * expf(top - both) + v.y * expf(v.x - both);
+            sum = both > -CUDART_INF_F ? sum * expf(top - both) + v.y * expf(v.x - both) : sum + v.y;
             top = both;
         }
-        if (top == -CUDART_INF_F) lse = top;  // every entry's score is -inf: no weight anywhere
+        sum += ld(a.spoilt + i);
+        if (top == -CUDART_INF_F && sum == 0.f) lse = top;  // every entry's score is -inf: no weight anywhere
         else {
             lse = top + logf(sum);
             neg = -lse;

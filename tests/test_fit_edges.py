@@ -75,3 +75,33 @@ def test_a_shift_of_all_biases_changes_only_their_rounding(d, shift):
     e = np.expm1(2 * es + 2.0 ** -23 * S + 2.0 ** -19)
     _close(got[3], want[3], e * want[3] + 1e-37, "mean")
     _check_grad(x, W, b, idx, what=f"shift {shift}")
+
+
+@pytest.mark.parametrize("d", [32, 64, 128])
+@pytest.mark.parametrize("bad", [0x7fc0, 0x7f80, 0xff80])  # NaN, infinities of either sign
+def test_inputs_that_are_no_numbers_stay_in_the_groups_that_take_part(d, bad):
+    """Positions with an entry in group 1 alone, whose inputs are not finite: groups 0 and 2 have the same bits as if they were padding."""
+    import paper_2601_19178_b200 as ckv
+    n, m, G = 400, 300, 3
+    x, W, b, idx = _router(23, n, m, G, d, pad=0.1)
+    some = np.arange(3, n, 50)
+    idx[some] = [-1, 7, m]
+    x[some[::2]], x[some[1::2], 1] = bad, bad              # the whole row, or one number of it
+    results = []
+    for one in (idx, np.where(np.isin(np.arange(n), some)[:, None], -1, idx).astype(np.int32)):
+        loss, lse, score, mean = _loss_case(x, W, b, one)
+        order = ckv.sort_indices(_dev(one), m)
+        grads = ckv.route_loss_grad(_dev(x), _dev(W), _dev(b), _dev(one), order, lse, score, mean, 1.0, 0.1)
+        results.append([_host(t) for t in (loss, lse.t(), score.t(), mean, grads[1], grads[2])])
+    for got, want in zip(*results):
+        for g in (0, 2):
+            assert np.isfinite(want[g]).all() and np.array_equal(got[g], want[g])
+    assert np.isnan(results[0][0][1, 0]) and np.isnan(results[0][1][1, some]).all() and np.isnan(results[0][3][1]).all()
+
+
+def test_scores_that_are_no_numbers_make_lse_none():
+    x, W, b, idx = _router(24, 200, 300, 2, 64)
+    x[5] = 0x7fc0
+    loss, lse, score, mean = [_host(t) for t in _loss_case(x, W, b, idx)]
+    other = np.arange(200) != 5
+    assert np.isnan(lse[5]).all() and np.isfinite(lse[other]).all() and np.isnan(score[5]).all() and np.isnan(mean).all() and np.isnan(loss[:, 0]).all()
