@@ -1,5 +1,7 @@
 """Fitting the router and the pool, for torch users: the training-side calls of the C ABI with their outputs and workspaces
-allocated.  Work goes to the current stream of the tensors' device; no arithmetic here.
+allocated.  Work goes to the current stream of the tensors' device; no arithmetic here.  The results are no part of an autograd
+graph: while gradients are recorded, tensors that require them are refused; call under `torch.no_grad()` (or with detached tensors) and
+take the gradients from the calls that end in `_grad`.
 
 A step of one side (keys or values), behind `ckv_route`:
 
@@ -33,6 +35,13 @@ def _refuse(name: str, t: torch.Tensor, shape, dtype, device):
 def _check(name: str, t: Optional[torch.Tensor], shape, dtype, device: int) -> None:
     if t is not None and (t.shape != shape or t.dtype is not dtype or t.get_device() != device):
         _refuse(name, t, shape, dtype, device)
+
+
+def _no_graph(*tensors: Optional[torch.Tensor]) -> None:
+    for t in tensors:
+        if t is not None and t.requires_grad and torch.is_grad_enabled():
+            raise ValueError("a tensor requires a gradient, which this call does not record: call it under torch.no_grad() and take the "
+                             "gradients from route_loss_grad and gather_grad")
 
 
 def _where(t: torch.Tensor) -> Tuple[int, int]:
@@ -74,6 +83,7 @@ def _check_router(x, W, bias, idx, dev):
 def route_loss(x: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor], idx: torch.Tensor):
     """loss [G][2] (load balance, peak), lse [n][G], score [n][G], mean [G][m], all fp32, of router inputs x [n][d_in] and
     weights W [G][m][d_in] (bf16), bias [G][m] fp32 or None and the picked entries idx [n][G]."""
+    _no_graph(x, W, bias)
     dev, stream = _where(x)
     n, d, G, m = _check_router(x, W, bias, idx, dev)
     nbytes = _loss_bytes(n, G, d, m)[0]
@@ -90,6 +100,7 @@ def route_loss_grad(x: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tenso
                     balance_weight: float, peak_weight: float, d_score: Optional[torch.Tensor] = None):
     """dx [n][d_in], dW [G][m][d_in] (bf16), dbias [G][m] (fp32) of sum_g (balance_weight balance_g + peak_weight peak_g) and of
     what else depends on the picked scores (d_score [n][G] or None); `ordered` is sort_indices(idx, m)."""
+    _no_graph(x, W, bias, lse, score, mean, d_score)
     dev, stream = _where(x)
     n, d, G, m = _check_router(x, W, bias, idx, dev)
     order, offset = ordered
@@ -117,6 +128,7 @@ def _dtype_of(pool: torch.Tensor) -> int:
 def gather(pool: torch.Tensor, idx: torch.Tensor, user: Optional[torch.Tensor], score: Optional[torch.Tensor] = None) -> torch.Tensor:
     """[n][G][d_user + d_shared]: user part (user [n][G][d_user] or None) and picked row of pool [G][m][d_shared], the latter times
     sigmoid(score [n][G]) if given; zeros for a position without an entry."""
+    _no_graph(pool, user, score)
     dev, stream = _where(pool)
     dt = _dtype_of(pool)
     G, m, ds = pool.shape
@@ -135,6 +147,7 @@ def gather(pool: torch.Tensor, idx: torch.Tensor, user: Optional[torch.Tensor], 
 def gather_grad(pool: torch.Tensor, ordered: Tuple[torch.Tensor, torch.Tensor], score: Optional[torch.Tensor], d_out: torch.Tensor):
     """d_pool [G][m][d_shared] (fp32), d_user [n][G][d_user] (None without a user part), d_score [n][G] (fp32; None without a
     gate) of `gather`, from d_out [n][G][d_user + d_shared] and `ordered` = sort_indices(idx, m)."""
+    _no_graph(pool, score, d_out)
     dev, stream = _where(pool)
     dt = _dtype_of(pool)
     G, m, ds = pool.shape

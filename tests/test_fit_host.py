@@ -83,3 +83,28 @@ def test_arrays_of_another_device_are_refused(lib2, name):
         assert fn(*args[:at], far, *args[at + 1:]) == 1, at
         if at != workspace:
             assert fn(1, *args[1:at], far, *args[at + 1:]) == 1, at      # (and the others on device 0)
+
+
+def test_tensors_of_a_graph_are_refused():
+    """The calls leave no graph behind: a tensor that wants gradients would get none without a word."""
+    import torch
+    import paper_2601_19178_b200 as ckv
+
+    z = torch.zeros
+    n, G, m, d = 3, 1, 4, 32
+    idx, order, offset = z(n, G, dtype=torch.int32), z(G, n, dtype=torch.int32), z(G, m + 1, dtype=torch.int32)
+    x, W, bias = z(n, d, dtype=torch.bfloat16), z(G, m, d, dtype=torch.bfloat16), z(G, m)
+    per, mean, pool, user, d_out = z(n, G), z(G, m), z(G, m, 30), z(n, G, 2), z(n, G, 32)
+    calls = [(ckv.route_loss, [x, W, bias, idx], (0, 1, 2)),
+             (ckv.route_loss_grad, [x, W, bias, idx, (order, offset), per, per, mean, 1.0, 1.0, per], (0, 1, 2, 5, 6, 7, 10)),
+             (ckv.gather, [pool, idx, user, per], (0, 2, 3)),
+             (ckv.gather_grad, [pool, (order, offset), per, d_out], (0, 2, 3))]
+    for fn, args, wants in calls:
+        for at in wants:
+            wanted = [a.clone().requires_grad_() if k == at else a for k, a in enumerate(args)]
+            with pytest.raises(ValueError, match="no_grad"):
+                fn(*wanted)
+            with torch.no_grad(), pytest.raises(ValueError, match="CUDA"):     # (further than that needs a GPU)
+                fn(*wanted)
+        with pytest.raises(ValueError, match="CUDA"):
+            fn(*args)
