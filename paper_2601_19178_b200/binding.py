@@ -45,6 +45,16 @@ class CkvError(RuntimeError):
         super().__init__(msg + (f" [{detail}]" if detail else ""))
 
 
+class _Int32:
+    """An argument that is refused if 32 bits do not hold it (ctypes would keep the low ones)."""
+
+    @classmethod
+    def from_param(cls, v):
+        if not -2 ** 31 <= v < 2 ** 31:
+            raise ValueError(f"{v} does not fit in 32 bits")
+        return ctypes.c_int32.from_param(v)
+
+
 def _load() -> ctypes.CDLL:
     if not os.path.exists(LIB_PATH):
         raise ImportError(
@@ -92,7 +102,7 @@ def _load() -> ctypes.CDLL:
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
-        f.restype, f.argtypes = res, args
+        f.restype, f.argtypes = res, [_Int32 if a is i32 else a for a in args]
     return L
 
 

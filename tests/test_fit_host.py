@@ -108,3 +108,15 @@ def test_tensors_of_a_graph_are_refused():
                 fn(*wanted)
         with pytest.raises(ValueError, match="CUDA"):
             fn(*args)
+
+
+@pytest.mark.parametrize("n", [2 ** 31, 2 ** 32 + 5, 2 ** 63, -2 ** 31 - 1])
+def test_sizes_of_more_than_32_bits_are_refused(n):
+    """ctypes keeps the low 32 bits of a number: 2^32 + 5 positions would be five."""
+    import paper_2601_19178_b200 as ckv
+    for call in (lambda: ckv.ckv_sort_indices_bytes(n, 1, 1), lambda: ckv.ckv_sort_indices_bytes(5, 1, n),
+                 lambda: ckv.ckv_sort_indices(0, n, 1, 1, None, None, None, None, 0, 1),
+                 lambda: ckv.ckv_route_loss_bytes(n, 1, 64, 1), lambda: ckv.ckv_gather_bytes(1, n, 1, 32, 30, 1),
+                 lambda: ckv.ckv_gather_grad_bytes(n, 1, 32), lambda: ckv.ckv_route(0, n, 1, 64, 4, None, None, None, None, stream=1)):
+        with pytest.raises((C.ArgumentError, OverflowError), match="32 bits|too large"):
+            call()
