@@ -6,7 +6,7 @@ import numpy as np
 import pytest
 
 from oracle import fit_oracle as F
-from test_fit import _check_grad, _close, _dev, _host, _loss_case, _router
+from test_fit import _check_grad, _check_loss, _close, _dev, _gather_case, _host, _loss_case, _router
 
 pytestmark = pytest.mark.gpu
 
@@ -105,3 +105,113 @@ def test_scores_that_are_no_numbers_make_lse_none():
     loss, lse, score, mean = [_host(t) for t in _loss_case(x, W, b, idx)]
     other = np.arange(200) != 5
     assert np.isnan(lse[5]).all() and np.isfinite(lse[other]).all() and np.isnan(score[5]).all() and np.isnan(mean).all() and np.isnan(loss[:, 0]).all()
+
+
+@pytest.mark.parametrize("n,m,G,d", [(20000, 300, 4, 32), (20000, 300, 4, 64), (15000, 200, 5, 128), (700, 15000, 4, 64), (300, 9000, 7, 128)])
+def test_passes_of_more_blocks_than_run_at_a_time(n, m, G, d):
+    """Partial results that a launch of their own joins: of LSE and R (more than 148 blocks of 384 positions), of MEAN (of as many entries)."""
+    x, W, b, idx = _router(n + d, n, m, G, d, pad=0.1)
+    idx[::11, 1] = m
+    _check_loss(x, W, b, idx, f"n={n} m={m} G={G} d={d}")
+    _check_grad(x, W, b, idx, what=f"n={n} m={m} G={G} d={d}")
+
+
+def _inside(t, fill):
+    """The tensor's values in the middle of a larger array of `fill`, 256 bytes from either end; the array, and its part."""
+    import torch
+    pad = 256 // t.element_size()
+    flat = torch.full((t.numel() + 2 * pad,), fill, dtype=t.dtype, device="cuda")
+    part = flat[pad:pad + t.numel()].view(t.shape)
+    part.copy_(t)
+    return flat, part
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [500, 3000])
+def test_places_outside_of_the_arrays_are_left_out(n, dtype):
+    """Positions just outside of [0, n) in a sorted order: they add nothing (NaN lies there), and nothing is written for them, around the
+    results, or for the positions that do not appear."""
+    import torch
+    import paper_2601_19178_b200 as ckv
+    G, m, D, du = 2, 40, 32, 2
+    pool, idx, user, score, d_out = _gather_case(6, dtype, n, G, m, D, du, True)
+    order, offset = F.sort_indices(idx, m)
+    rng = np.random.default_rng(n)
+    missing = np.zeros((n, G), bool)
+    for g in range(G):
+        at = rng.choice(n, 40, replace=False)
+        missing[order[g, at], g] = True
+        order[g, at] = rng.choice([-3, -1, n, n + 1, n + 5], 40)
+    nan = float("nan")
+    into = [_inside(t, 7.0) for t in (torch.full((G, m, D - du), 3.0, device="cuda"), torch.full((n, G, du), 3.0, device="cuda", dtype=_dev(pool).dtype),
+                                      torch.full((n, G), 3.0, device="cuda"))]
+    args = [_inside(_dev(pool), nan)[1], _inside(_dev(order), -1)[1], _inside(_dev(offset), -1)[1], _inside(_dev(score), nan)[1], _inside(_dev(d_out), nan)[1]]
+    need = ckv.ckv_gather_grad_bytes(n, G, D)
+    ws_flat, ws = _inside(torch.zeros(need, dtype=torch.uint8, device="cuda"), 9)
+    ckv.ckv_gather_grad(0, ckv.CKV_BF16 if dtype == "bf16" else ckv.CKV_F32, n, G, D, D - du, m, *args, *[part for _, part in into],
+                        ws if need else None, need)
+    gone = np.where(missing, -1, idx).astype(np.int32)
+    w_pool, w_user, w_score, a_pool, a_score = F.gather_grad(pool, gone, score, d_out)
+    d_pool, d_user, d_score = [_host(part) for _, part in into]
+    _close(d_pool, w_pool, (n * 2.0 ** -24 + 2.0 ** -20) * a_pool, "d_pool")
+    assert np.array_equal(d_user, np.where(missing[:, :, None], 3.0, w_user))
+    _close(d_score, np.where(missing, 3.0, w_score), (D * 2.0 ** -24 + 2.0 ** -19) * a_score, "d_score")
+    for flat, part in (*into, (ws_flat, ws)):
+        pad = 256 // flat.element_size()
+        want = 9 if flat is ws_flat else 7
+        assert (flat[:pad] == want).all() and (flat[flat.numel() - pad:] == want).all()
+
+
+@pytest.mark.parametrize("n", [500, 3000])
+def test_runs_outside_of_the_arrays_write_nothing_around_the_results(n):
+    """Offsets that are no offsets, somewhat past the ends and out of order, for both gradients."""
+    import torch
+    import paper_2601_19178_b200 as ckv
+    G, m, D, du, d = 2, 40, 32, 2, 64
+    pool, idx, user, score, d_out = [_dev(t) for t in _gather_case(8, "bf16", n, G, m, D, du, True)]
+    x, W, b, _ = [_dev(t) for t in _router(3, n, m, G, d)]
+    _, lse, s, mean = ckv.route_loss(x, W, b, idx)
+    order, offset = ckv.sort_indices(idx, m)
+    g = torch.Generator(device="cuda").manual_seed(n)
+    for wild in (torch.randint(-30, n + 30, (G, m + 1), generator=g, device="cuda", dtype=torch.int32), offset + 25, offset - 25, offset.flip(1).contiguous()):
+        into = [_inside(t, 7.0) for t in (torch.zeros((G, m, D - du), device="cuda"), torch.zeros_like(user), torch.zeros((n, G), device="cuda"),
+                                          torch.zeros_like(x), torch.zeros_like(W), torch.zeros_like(b))]
+        need, need_route = ckv.ckv_gather_grad_bytes(n, G, D), ckv.ckv_route_loss_bytes(n, G, d, m)[1]
+        ws_flat, ws = _inside(torch.zeros(max(need, need_route), dtype=torch.uint8, device="cuda"), 9)
+        o = [_inside(order, -1)[1], _inside(wild, 2 ** 30)[1]]
+        ckv.ckv_gather_grad(0, ckv.CKV_BF16, n, G, D, D - du, m, pool, *o, score, d_out, *[part for _, part in into[:3]], ws, ws.numel())
+        ckv.ckv_route_loss_grad(0, n, G, d, m, x, W, b, idx, *o, lse, s, mean, 1.0, 1.0, None, *[part for _, part in into[3:]], ws, ws.numel())
+        for flat, part in (*into, (ws_flat, ws)):
+            pad = 256 // flat.element_size()
+            want = 9 if flat is ws_flat else 7
+            assert (flat[:pad] == want).all() and (flat[flat.numel() - pad:] == want).all()
+
+
+def test_calls_from_several_threads():
+    """First calls of fresh threads, for pools of different sizes: each kernel's shared memory differs between them."""
+    import torch
+    import paper_2601_19178_b200 as ckv
+    from test_gpu_threads import _together
+    sizes = [(5000, 5000), (8000, 20000), (9000, 24000), (300, 13000), (12000, 700), (8192, 24998)]
+    threads = 24
+    inputs = []
+    for k in range(threads):
+        n, m = sizes[k % len(sizes)]
+        x, W, b, idx = _router(30 + k, n // 20 + 1, 90 + k, 2, (32, 64, 128)[k % 3])
+        rng = np.random.default_rng(k)
+        picked = rng.integers(-1, m + 1, (n, 2)).astype(np.int32)
+        inputs.append((m, picked, _dev(picked), [_dev(t) for t in (x, W, b, idx)]))
+    got, want = [None] * threads, []
+    for m, picked, _, r in inputs:
+        want.append([*F.sort_indices(picked, m), *[t.cpu() for t in ckv.route_loss(*r)]])
+    torch.cuda.synchronize()
+
+    def work(k):
+        m, _, idx, r = inputs[k]
+        for _ in range(5):
+            got[k] = [*ckv.sort_indices(idx, m), *ckv.route_loss(*r)]
+        torch.cuda.current_stream().synchronize()
+
+    _together(threads, work)
+    for g, w in zip(got, want):
+        assert all(np.array_equal(a.cpu().numpy(), np.asarray(c)) for a, c in zip(g, w))
