@@ -5,6 +5,7 @@ import re
 import subprocess
 import threading
 
+import numpy as np
 import pytest
 
 from test_fit import OPTIONAL, REQUIRED, _calls
@@ -120,3 +121,22 @@ def test_sizes_of_more_than_32_bits_are_refused(n):
                  lambda: ckv.ckv_gather_grad_bytes(n, 1, 32), lambda: ckv.ckv_route(0, n, 1, 64, 4, None, None, None, None, stream=1)):
         with pytest.raises((C.ArgumentError, OverflowError), match="32 bits|too large"):
             call()
+
+
+def test_polynomials_of_the_exponential_have_the_errors_stated_beside_them():
+    """The coefficients as the kernels have them, 2^f on [-1/2, 1/2] in 64 bits; degree 5, which the losses' sums take, on average as well."""
+    src = open(os.path.join(ROOT, "paper_2601_19178_b200", "csrc", "kernels_route_sweep.cu")).read()
+    body = src[src.index("struct Exp2"):]
+    body = body[:body.index("scale = {")]
+    stated = [float(v) for v in re.search(r"\((\S+), (\S+), (\S+) for degrees 3 to 5", src).groups()]
+    f = np.linspace(-0.5, 0.5, 20001)
+    forms = [[np.float32(c) for c in re.findall(r"both\(([\d.]+)f\)", line)] for line in re.findall(r"p = (fma2.*?);", body, re.S)]
+    assert sorted(len(c) for c in forms) == [4, 5, 6]
+    for coefficients in forms:
+        p = 0.0
+        for c in coefficients:
+            p = p * f + np.float64(c)
+        error = p / np.exp2(f) - 1
+        assert abs(error).max() <= stated[len(coefficients) - 4] * 1.01, len(coefficients) - 1
+        if len(coefficients) == 6:
+            assert abs(error.mean()) <= 2e-8
