@@ -215,3 +215,19 @@ def test_calls_from_several_threads():
     _together(threads, work)
     for g, w in zip(got, want):
         assert all(np.array_equal(a.cpu().numpy(), np.asarray(c)) for a, c in zip(g, w))
+
+
+@pytest.mark.parametrize("n", [300, 3000])
+@pytest.mark.parametrize("dtype,D,du", [("bf16", 64, 1), ("bf16", 64, 4), ("bf16", 64, 8), ("bf16", 128, 27), ("bf16", 16, 3), ("f32", 32, 1), ("f32", 32, 4), ("f32", 128, 13)])
+def test_user_gradients_that_are_no_numbers_stay_in_d_user(n, dtype, D, du):
+    """d_score is the product with the pool's part of the row alone."""
+    import paper_2601_19178_b200 as ckv
+    pool, idx, user, score, d_out = _gather_case(n + D, dtype, n, 2, 90, D, du, True)
+    as_bits = np.asarray([0x7fc0, 0x7f80, 0xff80], np.uint16) if dtype == "bf16" else np.asarray([np.nan, np.inf, -np.inf], np.float32)
+    for k in range(3):
+        d_out[k::7, :, :du] = as_bits[k]
+    d_pool, d_user, d_score = [_host(t) for t in ckv.gather_grad(_dev(pool), ckv.sort_indices(_dev(idx), 90), _dev(score), _dev(d_out))]
+    w_pool, w_user, w_score, a_pool, a_score = F.gather_grad(pool, idx, score, d_out)
+    assert np.array_equal(d_user, w_user, equal_nan=True)
+    _close(d_pool, w_pool, (n * 2.0 ** -24 + 2.0 ** -20) * a_pool, "d_pool")
+    _close(d_score, w_score, (D * 2.0 ** -24 + 2.0 ** -19) * a_score, "d_score")
