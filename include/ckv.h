@@ -300,7 +300,8 @@ CKV_API ckv_status ckv_project(int32_t device, int32_t n, int32_t n_groups, int3
  * their elements, W and d_out to 16 bytes.  `workspace` is device memory on a 256-byte boundary of at least the size that the _bytes
  * function of the call gives (NULL where that is 0), of any contents; calls that may overlap on the GPU, captured graphs among them, need one each.
  * Errors of all of them: INVALID_ARG (sizes, null, host or misaligned pointers, workspace too small), UNSUPPORTED (d_in,
- * head_dim, more than 65535 groups or 2^32 - 2 pool rows), SHAPE (d_shared outside [1, head_dim]), CUDA.
+ * head_dim, more than 65535 groups or 2^32 - 2 pool rows), SHAPE (d_shared outside [1, head_dim]), CUDA.  The calls do not wait for their
+ * kernels: should one of the bounded waits inside the router's ever run out, its results are NaN and the status is OK all the same.
  */
 
 /*
@@ -316,7 +317,8 @@ CKV_API ckv_status ckv_sort_indices(int32_t device, int32_t n, int32_t n_groups,
 /*
  * The router's losses, with M[i][j] = x_i . W[g][j] + bias[g][j] (never written) and u = 1 / n_entries, over the `rows`
  * positions of the group that have an entry:
- *   lse   fp32 [n][n_groups]          log sum_j exp M[i][j]     (log probability of the picked entry: score - lse)
+ *   lse   fp32 [n][n_groups]          log sum_j exp M[i][j]     (log probability of the picked entry: score - lse; for a look at it, the
+ *                                     gradient below takes none by lse)
  *   score fp32 [n][n_groups]          M[i][idx[i]]              (0 in both for a position without an entry)
  *   mean  fp32 [n_groups][n_entries]  p_j = 1 / rows * sum_i softmax(M[i])_j
  *   loss  fp32 [n_groups][2]          load balance sum_j p_j log(p_j / u), peak -1 / rows * sum_i log sigmoid(score_i)
@@ -362,7 +364,8 @@ CKV_API ckv_status ckv_gather(int32_t device, int32_t dtype, int32_t n, int32_t 
 
 /*
  * Gradients of ckv_gather, d_out [n][n_groups][head_dim] of `dtype`, order and offset of ckv_sort_indices:
- *   d_pool  fp32 [n_groups][n_entries][d_shared]   fp32 sums in the order of the positions (zeros for an entry without one)
+ *   d_pool  fp32 [n_groups][n_entries][d_shared]   fp32 sums, in an order of partial sums that the sizes and the entries' runs fix (zeros for
+ *           an entry without a position)
  *   d_user  `dtype` [n][n_groups][head_dim - d_shared], or NULL
  *   d_score fp32 [n][n_groups], NULL iff score is (pool is read for it alone and may be NULL then)
  */

@@ -54,7 +54,8 @@ def build_pycall(force: bool = False) -> str:
 
 def build(force: bool = False, verbose: bool = False, bounds: bool = False) -> str:
     """bounds=True builds libckv_bounds.so instead: the same library with every index, row and shared-memory
-    offset the kernels compute range-checked into the context's error word (-DCKV_BOUNDS)."""
+    offset that the attend kernels compute range-checked into the context's error word (-DCKV_BOUNDS; the prefill and training calls
+    have no context, and are as in the other build)."""
     sources = sorted(glob.glob(os.path.join(CSRC, "*.cu")))
     headers = glob.glob(os.path.join(CSRC, "*.h")) + glob.glob(os.path.join(CSRC, "*.cuh")) + \
         glob.glob(os.path.join(ROOT, "include", "*.h"))

@@ -1,7 +1,7 @@
 // Gated lookup of pool rows (Eq. Kc, training branch) and its gradient.
 //
 //   out[i][g]   = (user[i][g] | s_i pool[g][I_i]),  s = sigmoid(score) or 1; a position without an entry gets zeros
-//   d_pool[g][j] = sum over the positions of entry j, in their order, of s_i d_out[i][g][skip:]
+//   d_pool[g][j] = sum over the positions of entry j of s_i d_out[i][g][skip:], in a fixed order of partial sums
 //   d_user = d_out[:skip],  d_score_i = s_i (1 - s_i) <pool[g][I_i], d_out[i][g][skip:]>
 #include <cuda_bf16.h>
 
@@ -140,8 +140,8 @@ __global__ void __launch_bounds__(256) gather_kernel(int64_t rows, int G, int lo
 // The sorted positions of a group are cut into chunks of equal length, whatever the entries.  LANES lanes walk a chunk, 16 bytes of
 // a row each.  A run that lies inside the chunk is written; the one that began before it and the one that goes on behind it leave a
 // partial sum (head, tail), which the block joins in the order of its chunks, and of the blocks join_kernel.  Nothing
-// depends on the order in which warps run.  1048576 x 4 rows of 128 bytes with gate, d_score and d_user: 217 us, the
-// bare sums some two thirds of it; neither memory (2.8 TB/s) nor issue (43 %) is full: the turns' chains of loads, shuffles and shared memory
+// depends on the order in which warps run.  1048576 x 4 rows of 128 bytes with gate, d_score and d_user: 222 us again and
+// again on the same arrays, 262 on other ones each time, the bare sums some two thirds of it; neither memory (2.8 TB/s) nor issue (47 %) is full: the turns' chains of loads, shuffles and shared memory
 // bind, at the 20 warps per SM that their registers and stages leave, next to three sectors per row of which a few bytes are
 // wanted.  20011 x 4 rows: 13 us and the join, all latency (search of the first entry 3, rows 1, runs of few positions 4).
 constexpr int kSegThreads = 128;

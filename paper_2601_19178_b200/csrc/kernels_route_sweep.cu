@@ -13,8 +13,8 @@
 //                                same tile once more, now as MN-major operand:  O += T tile.  Two blocks per CTA (one at d_in =
 //                                128), each with two score buffers whose turns belong to four warps each.
 // Bound by the special-function unit, 16 exponentials per clock and SM, and the FMA pipe, which takes its share of them: 32768 positions x 16384
-// entries x 4 groups (2.1e9 scores, whose exponentials would take that unit alone 477 us per pass), d_in = 64: LSE 503 us, MEAN 466, R 525
-// to 545, DX and DW 1280 to 1355; special-function unit 67 to 76 % busy, issue slots 57 to 65 %, tensor cores 31 to 46 %.
+// entries x 4 groups (2.1e9 scores, whose exponentials would take that unit alone 477 us per pass), d_in = 64: LSE 503 us, MEAN 467, R 528
+// to 545, DX and DW 1300 to 1355; special-function unit 66 to 76 % busy, issue slots 57 to 65 %, tensor cores 32 to 48 %.
 // Every wait is bounded: a time-out raises the CTA's abort flag, which ends all others; the CTA waits for its copies and
 // products in flight, frees its TMEM, and its results are NaN.
 #include <cuda_bf16.h>
@@ -264,8 +264,8 @@ __device__ __forceinline__ F2 weight(F2 u, bool fma)
     return mul2(p.p, p.scale);
 }
 
-// The exponent of a weight is s log2(e) - c with c = lse log2(e) rounded once, which is off by as much as lse is as an fp32 number: at 10^7 a weight by a
-// seventh, at 10^10 by its whole range.  MEAN, R and DW have the difference s - lse from the tensor core, where it is exact if small.  LSE, whose c is top
+// The exponent of a weight is s log2(e) - c with c = lse log2(e) rounded once, which is off by as much as lse is as an fp32 number: at 10^6 a weight by a
+// thirtieth, at 10^7 by most of itself, at 10^10 by its whole range.  MEAN, R and DW have the difference s - lse from the tensor core, where it is exact if small.  LSE, whose c is top
 // log2(e), takes its residue top log2(e) - c, which one fused operation gives exactly, out of the sum.  DX takes the difference first where lse is far from zero: a branch per 32 scores, which few rows take.
 constexpr float kFar = 1024.f;
 __device__ __forceinline__ bool is_far(float reference) { return fabsf(reference) > kFar && reference > -CUDART_INF_F; }

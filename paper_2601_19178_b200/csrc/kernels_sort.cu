@@ -33,7 +33,7 @@ struct Pass {
 };
 __device__ __forceinline__ int digit_of(uint32_t key, const Pass& p) { return (int)(key >> p.shift) & p.mask & 0x7fff; }
 
-// Bound by shared-memory atomics (the data pipe 65 % busy) and the strided indices: 1048576 x 8 positions, 4096 entries 26 us.
+// Bound by shared-memory atomics (the data pipe 65 % busy) and the strided indices: 1048576 x 8 positions, 4096 entries 24 us.
 __global__ void __launch_bounds__(256) count_kernel(const Pass p, int32_t* table)
 {
     extern __shared__ int32_t bins[];
@@ -140,7 +140,7 @@ __device__ __forceinline__ int32_t take_places(volatile int32_t* next, int d, un
 
 // A chunk's positions to their places, by one warp (the block's others help to fetch next[]).  Bound by its turns, of which a match
 // instruction is the longest part (its time grows with the number of different keys in the warp; 0.3 us a turn): 1048576 x 8
-// positions, 4096 entries 73 us of 112.  (Lanes that find each other through a word per key, as in block_sort_kernel, halve a turn, but with
+// positions, 4096 entries 68 us of 109.  (Lanes that find each other through a word per key, as in block_sort_kernel, halve a turn, but with
 // half as many warps to an SM: 85; two to eight warps with a part of a larger chunk each, whose parts the block counts first, no
 // less, for the match instructions of an SM take turns; votes on the 13 bits of a key instead of the match 113.)
 __global__ void __launch_bounds__(128) place_kernel(const Pass p, const int32_t* table, const int32_t* base)
@@ -286,8 +286,8 @@ int stride_of(int64_t m) { return (bins_of(m) + 3) & ~3; }
 bool by_block(int64_t n, int64_t m) { return n <= kBlockSort && passes_of(m) == 1; }
 // Positions of a chunk, a power of two: the number with the shortest run, in microseconds.  A turn of 32 positions takes a warp 0.3, an SM holds as
 // many chunks as their counts leave room for (at most 16), a chunk's counts are written, read, written and read, at some 1.5 TB/s,
-// and adding up sixteen chunks of a group takes 1.  (1048576 x 8 positions, 4000 entries: 147 us with chunks of 8192, 172 with 4096; 200000
-// x 2, 1000 entries: 24 with 1024, 29 with 512; 50000 x 4, 5000 entries: 24 with 1024, 34 with 4096.)
+// and adding up sixteen chunks of a group takes 1.  (1048576 x 8 positions, 4000 entries: 111 us with chunks of 8192, 133 with 4096, 168
+// with 16384; 200000 x 2, 1000 entries: 24 with 1024, 27 with 2048; 50000 x 4, 5000 entries: 25 with 1024, 42 with 4096.)
 int64_t chunk_of(int64_t n, int G, int64_t m)
 {
     int64_t best = 512;
